@@ -312,6 +312,140 @@ int fastmax_fwd_noalloc(const void *q, const void *k, const void *v, void *out,
                         float *g, int B, int H, int N, int D, int p, int causal,
                         float qk_scale, fastmax_dtype_t dt, hipStream_t stream);
 
+/*
+ * Around the attention: positions, shared heads, a paged cache.
+ *
+ * A model's projections give token rows: q [B, N, Hq, D] and k, v
+ * [B, N, Hkv, D], often side by side in one buffer; Hkv divides Hq and query
+ * head h shares key head h / (Hq / Hkv).  fastmax_rope_fwd turns them into
+ * what fastmax_fwd takes, fastmax_rope_bwd takes the gradients back.  While
+ * serving, fastmax_cache_append puts new tokens into a paged cache and
+ * fastmax_paged_fwd attends over it.
+ *
+ * Conventions of these calls, beside those at the top: B*N (or T), Hq and Hkv
+ * as ints with B*N*Hq*D < 2^62, Hq <= 2^16; token rows have D contiguous and
+ * the strides given, which (like every pointer to rows, tables or weights)
+ * must keep rows 16-byte aligned (FASTMAX_EALIGN); pos, slots, page tables and
+ * lengths are aligned to their type.  Sums and statistics are float32; rows
+ * whose squares pass float32's range are not handled.
+ */
+
+/* Strides in elements; `batch` is not read where there is no batch. */
+typedef struct {
+    long long batch, token, head;
+} fastmax_strides_t;
+
+/*
+ * Norm and rotation of query and key rows.
+ *   norm: y = w x / sqrt(mean x^2 + eps) over the D channels, wq for queries
+ *     and wk for keys, float32 [D]; both NULL: no norm.  eps >= 0.
+ *   rotation of the first rot channels (a multiple of 16, <= D; 0: none): the
+ *     pair j of channels (j, j + rot/2), or (2j, 2j + 1) if interleaved, turns
+ *     by the angle whose cosine and sine stand in row pos of the float32
+ *     tables cos, sin [table_rows, rot/2], column j.  pos is int32
+ *     [tokens, axes]: with several axes (time, height, width), pairs
+ *     0 .. sections[0] - 1 turn by the first, the next sections[1] by the
+ *     second, ...; the sections sum to rot/2 (one axis: sections unread).
+ *   A position outside the table gives NaN in the rotated channels (nothing
+ *   outside the table is read).
+ */
+typedef struct {
+    const float *cos, *sin;
+    const int32_t *pos;
+    int table_rows;
+    int rot;
+    int axes;          /* 1 .. 4 */
+    int sections[4];
+    int interleaved;   /* 0 or 1 */
+    const float *wq, *wk;
+    float eps;
+} fastmax_rope_t;
+
+/*
+ * Token rows to heads.
+ *   q, k, v    : [B, N, Hq | Hkv, D] with strides[0 | 1 | 2] (host memory;
+ *                NULL: contiguous)
+ *   oq, ok, ov : [B, Hq, N, D] contiguous: normed and rotated q; normed and
+ *                rotated k and v itself, each key head once per query head
+ *                that shares it
+ */
+int fastmax_rope_fwd(const void *q, const void *k, const void *v,
+                     const fastmax_strides_t *strides, void *oq, void *ok, void *ov, int B, int N,
+                     int Hq, int Hkv, int D, const fastmax_rope_t *rope, fastmax_dtype_t dt,
+                     hipStream_t stream);
+
+/*
+ * Its backward.
+ *   q, k          : the forward's rows, strides[0 | 1]; read only with a norm
+ *                   (NULL otherwise)
+ *   gq, gk, gv    : gradients of oq, ok, ov [B, Hq, N, D] contiguous
+ *   dq, dk, dv    : gradients of q, k, v with dstrides[0 | 1 | 2] (NULL:
+ *                   contiguous; no two rows may share memory); those of
+ *                   shared heads are sums over the heads that share them
+ *   dwq, dwk      : float32 [D], with a norm (NULL otherwise)
+ *   workspace     : fastmax_rope_workspace_bytes (0 without a norm)
+ * Sums run in a fixed order: equal calls give equal bits.
+ */
+size_t fastmax_rope_workspace_bytes(int B, int N, int Hq, int Hkv, int D, int norm);
+int fastmax_rope_bwd(const void *q, const void *k, const fastmax_strides_t *strides,
+                     const void *gq, const void *gk, const void *gv, void *dq, void *dk, void *dv,
+                     const fastmax_strides_t *dstrides, float *dwq, float *dwk, int B, int N,
+                     int Hq, int Hkv, int D, const fastmax_rope_t *rope, fastmax_dtype_t dt,
+                     void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * New tokens into a paged cache.  Queries and keys are normed and rotated as
+ * above and then standardised as fastmax_fwd standardises its rows (mean 0,
+ * population standard deviation 1, no epsilon: a constant row is not finite).
+ *   q, k, v          : [T, Hq | Hkv, D], strides[0 | 1 | 2] (batch unread)
+ *   q_out            : [T, Hq, D] contiguous, q^
+ *   k_cache, v_cache : `pages` pages of page_size tokens (a power of two,
+ *                      16 .. 1024) of Hkv heads, both with the strides `cache`
+ *                      (batch: from page to page; NULL: [pages, Hkv,
+ *                      page_size, D] contiguous); k^ and v go in
+ *   slots            : int64 [T]: page * page_size + place in the page; a
+ *                      token whose slot is outside the cache (-1: padding)
+ *                      is not written, its q_out row is.  No two tokens may
+ *                      have the same slot.
+ */
+int fastmax_cache_append(const void *q, const void *k, const void *v,
+                         const fastmax_strides_t *strides, void *q_out, void *k_cache,
+                         void *v_cache, const fastmax_strides_t *cache, const int64_t *slots,
+                         int T, int Hq, int Hkv, int D, int pages, int page_size,
+                         const fastmax_rope_t *rope, fastmax_dtype_t dt, hipStream_t stream);
+
+/*
+ * Attention of new tokens over the cache.  Sequence s has lens[s] tokens in
+ * the cache, token n in page table[s][n / page_size]; its new tokens are the
+ * last of them.  The new token at position i of its sequence gets
+ *     O_i = sum_n w_in v_n / sum_n w_in,  w_in = f_p(qk_scale q^_i . k^_n)
+ * over n <= i and, if window > 0, i - window < n or n < sinks.  q^ and k^ are
+ * taken as they are (fastmax_cache_append standardises them).
+ *   q        : q^ [T, Hq, D], *q_strides (batch unread; NULL: contiguous)
+ *   table    : int32 [S, table_cols]; lens: int32 [S]
+ *   q_start  : int32 [S + 1], sequence s has the rows q_start[s] ..
+ *              q_start[s + 1] - 1 of q; NULL: T = S, one row each
+ *   max_q    : most rows of one sequence, max_len: longest sequence.  They
+ *              size the grid; larger true values cost time, not correctness.
+ *   out      : [T, Hq, D] contiguous
+ *   workspace: fastmax_paged_workspace_bytes with the same sizes
+ * A row that sees no key (lens[s] smaller than its new tokens) is 0.  What
+ * lies in slots that no row of a sequence sees is not used, whatever it
+ * holds; entries of the page table past lens[s] or behind the window are not
+ * read.  If an entry that is read is not a page, or lens[s] is more than
+ * table_cols pages hold, the rows that it concerns are NaN.
+ * table_cols * page_size <= 2^30, S <= 65535.
+ */
+size_t fastmax_paged_workspace_bytes(int S, int T, int Hq, int Hkv, int D, int max_q, int max_len,
+                                     int window, int sinks, fastmax_dtype_t dt);
+int fastmax_paged_fwd(const void *q, const fastmax_strides_t *q_strides, const void *k_cache,
+                      const void *v_cache, const fastmax_strides_t *cache, const int32_t *table,
+                      const int32_t *lens, const int32_t *q_start, void *out, int S, int T, int Hq,
+                      int Hkv, int D, int pages, int page_size, int table_cols, int max_q,
+                      int max_len, int p, float qk_scale, int window, int sinks,
+                      fastmax_dtype_t dt, void *workspace, size_t workspace_bytes,
+                      hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

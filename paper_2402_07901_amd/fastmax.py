@@ -30,6 +30,20 @@ EHIP = -6
 _lib = None
 
 
+class Strides(ctypes.Structure):
+    """fastmax_strides_t: strides in elements."""
+    _fields_ = [("batch", ctypes.c_longlong), ("token", ctypes.c_longlong),
+                ("head", ctypes.c_longlong)]
+
+
+class Rope(ctypes.Structure):
+    """fastmax_rope_t: norm and rotation of query and key rows."""
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("table_rows", ctypes.c_int), ("rot", ctypes.c_int), ("axes", ctypes.c_int),
+                ("sections", ctypes.c_int * 4), ("interleaved", ctypes.c_int),
+                ("wq", ctypes.c_void_p), ("wk", ctypes.c_void_p), ("eps", ctypes.c_float)]
+
+
 class FastmaxError(RuntimeError):
     def __init__(self, code: int, what: str):
         super().__init__(f"{what}: {strerror(code)} (code {code})")
@@ -75,6 +89,22 @@ def lib():
         L.fastmax_fwd_noalloc.restype = i
         L.fastmax_set_scan_segments.argtypes = [i]
         L.fastmax_set_scan_segments.restype = i
+        st, rope = ctypes.POINTER(Strides), ctypes.POINTER(Rope)
+        L.fastmax_rope_fwd.argtypes = [vp, vp, vp, st, vp, vp, vp, i, i, i, i, i, rope, i, vp]
+        L.fastmax_rope_fwd.restype = i
+        L.fastmax_rope_workspace_bytes.argtypes = [i, i, i, i, i, i]
+        L.fastmax_rope_workspace_bytes.restype = sz
+        L.fastmax_rope_bwd.argtypes = [vp, vp, st, vp, vp, vp, vp, vp, vp, st, vp, vp, i, i, i, i,
+                                       i, rope, i, vp, sz, vp]
+        L.fastmax_rope_bwd.restype = i
+        L.fastmax_cache_append.argtypes = [vp, vp, vp, st, vp, vp, vp, st, vp, i, i, i, i, i, i,
+                                           rope, i, vp]
+        L.fastmax_cache_append.restype = i
+        L.fastmax_paged_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i, i, i]
+        L.fastmax_paged_workspace_bytes.restype = sz
+        L.fastmax_paged_fwd.argtypes = [vp, st, vp, vp, st, vp, vp, vp, vp, i, i, i, i, i, i, i, i,
+                                        i, i, i, f, i, i, i, vp, sz, vp]
+        L.fastmax_paged_fwd.restype = i
         L.fastmax_strerror.argtypes = [i]
         L.fastmax_strerror.restype = ctypes.c_char_p
         L.fastmax_version.restype = ctypes.c_char_p
@@ -382,3 +412,256 @@ def fastmax_bwd_dropout(q, k, v, out, dout, g, bits, rate, causal=False, scale=N
     if rc != OK:
         raise FastmaxError(rc, "fastmax_bwd_dropout")
     return dq, dk, dv
+
+
+# ---------------------------------------------------------------------------
+# Around the attention: norm and rotation of a projection's rows, shared heads,
+# a paged cache and the attention of new tokens over it.
+# ---------------------------------------------------------------------------
+def _rows_of(name, t, like, shape):
+    """Checks token rows: ``like``'s dtype and device, the given shape, D
+    contiguous (the library checks the other strides)."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != like.dtype:
+        raise ValueError(f"{name} must be {like.dtype}, got {t.dtype}")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    if t.stride(-1) != 1:
+        raise ValueError(f"{name}'s channels must be contiguous")
+
+
+def _whole(name, t, dtype, device, shape=None):
+    """Checks a contiguous tensor of a given dtype (and shape)."""
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _strides(*tensors):
+    """fastmax_strides_t array of [(B,) N, H, D] tensors."""
+    out = (Strides * len(tensors))()
+    for s, t in zip(out, tensors):
+        st = t.stride()
+        s.batch, s.token, s.head = (st[0] if len(st) == 4 else 0), st[-3], st[-2]
+    return out
+
+
+def _rope_of(q, tokens, pos, cos, sin, wq, wk, eps, sections, interleaved):
+    """The fastmax_rope_t of a call whose rows are q's; ``tokens``: q's
+    leading sizes."""
+    import torch
+    D, device = q.shape[-1], q.device
+    r = Rope()
+    r.interleaved, r.eps = int(bool(interleaved)), float(eps)
+    if (cos is None) != (sin is None) or (cos is None) != (pos is None):
+        raise ValueError("pos, cos and sin go together")
+    if cos is not None:
+        _whole("cos", cos, torch.float32, device)
+        if cos.dim() != 2:
+            raise ValueError(f"cos must be [rows, rot / 2], got shape {tuple(cos.shape)}")
+        _whole("sin", sin, torch.float32, device, cos.shape)
+        if pos.dim() == len(tokens):
+            pos = pos.unsqueeze(-1)
+        axes = pos.shape[-1]
+        _whole("pos", pos, torch.int32, device, (*tokens, axes))
+        if not 1 <= axes <= 4:
+            raise ValueError(f"1 to 4 axes of positions, got {axes}")
+        r.cos, r.sin, r.pos = cos.data_ptr(), sin.data_ptr(), pos.data_ptr()
+        r.table_rows, r.rot, r.axes = cos.shape[0], 2 * cos.shape[1], axes
+        if axes > 1:
+            if sections is None or len(sections) != axes:
+                raise ValueError(f"{axes} axes of positions need as many sections")
+            r.sections[:axes] = [int(n) for n in sections]
+    if (wq is None) != (wk is None):
+        raise ValueError("wq and wk go together")
+    if wq is not None:
+        _whole("wq", wq, torch.float32, device, (D,))
+        _whole("wk", wk, torch.float32, device, (D,))
+        r.wq, r.wk = wq.data_ptr(), wk.data_ptr()
+    return r
+
+
+def _on_gpu(q, dims, what):
+    if q.dim() != dims:
+        raise ValueError(f"q must be {what}, got shape {tuple(q.shape)}")
+    if q.device.type != "cuda":
+        raise ValueError(f"the tensors must be on a GPU, q is on {q.device}")
+
+
+def fastmax_rope_fwd(q, k, v, pos, cos, sin, wq=None, wk=None, eps=1e-6, sections=None,
+                     interleaved=False, out=None, stream=None):
+    """A projection's rows q [B, N, Hq, D], k and v [B, N, Hkv, D] (strided
+    views; D contiguous) as the attention takes them: RMS norm with weights wq
+    and wk (None: no norm), rotation by position (cos, sin [rows, rot / 2]; pos
+    int32 [B, N] or [B, N, axes] with ``sections`` pairs per axis; all None: no
+    rotation), key and value heads repeated.  Returns three contiguous
+    [B, Hq, N, D] tensors (``out``: the same, the caller's)."""
+    import torch
+    _on_gpu(q, 4, "[B, N, Hq, D]")
+    B, N, Hq, D = q.shape
+    Hkv = k.shape[2] if k.dim() == 4 else 0
+    _rows_of("q", q, q, q.shape)
+    _rows_of("k", k, q, (B, N, Hkv, D))
+    _rows_of("v", v, q, (B, N, Hkv, D))
+    dt = _dtype_code(q)
+    rope = _rope_of(q, (B, N), pos, cos, sin, wq, wk, eps, sections, interleaved)
+    if out is None:
+        out = tuple(torch.empty((B, Hq, N, D), dtype=q.dtype, device=q.device) for _ in range(3))
+    else:
+        for name, t in zip(("out[0]", "out[1]", "out[2]"), out):
+            _whole(name, t, q.dtype, q.device, (B, Hq, N, D))
+    with _on(q.device):
+        rc = lib().fastmax_rope_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), _strides(q, k, v),
+                                    out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), B, N,
+                                    Hq, Hkv, D, rope, dt, _stream(_stream_of(stream, q.device)))
+    if rc != OK:
+        raise FastmaxError(rc, "fastmax_rope_fwd")
+    return tuple(out)
+
+
+def rope_workspace_bytes(B, N, Hq, Hkv, D, norm) -> int:
+    return int(lib().fastmax_rope_workspace_bytes(B, N, Hq, Hkv, D, int(bool(norm))))
+
+
+def fastmax_rope_bwd(q, k, gq, gk, gv, pos, cos, sin, wq=None, wk=None, eps=1e-6, sections=None,
+                     interleaved=False, out=None, workspace=None, stream=None):
+    """Backward of fastmax_rope_fwd: gq, gk, gv [B, Hq, N, D] are the gradients
+    of its outputs; q and k its inputs (their shapes count; they are read with a
+    norm only).  Returns (dq, dk, dv, dwq, dwk), dq [B, N, Hq, D], dk and dv
+    [B, N, Hkv, D] (``out``: these three, the caller's, strided as they like),
+    dwq and dwk float32 [D] (None without a norm)."""
+    import torch
+    _on_gpu(q, 4, "[B, N, Hq, D]")
+    B, N, Hq, D = q.shape
+    Hkv = k.shape[2] if k.dim() == 4 else 0
+    _rows_of("q", q, q, q.shape)
+    _rows_of("k", k, q, (B, N, Hkv, D))
+    for name, t in (("gq", gq), ("gk", gk), ("gv", gv)):
+        _whole(name, t, q.dtype, q.device, (B, Hq, N, D))
+    dt = _dtype_code(q)
+    rope = _rope_of(q, (B, N), pos, cos, sin, wq, wk, eps, sections, interleaved)
+    if out is None:
+        out = tuple(torch.empty((B, N, h, D), dtype=q.dtype, device=q.device)
+                    for h in (Hq, Hkv, Hkv))
+    else:
+        for name, t, h in zip(("out[0]", "out[1]", "out[2]"), out, (Hq, Hkv, Hkv)):
+            _rows_of(name, t, q, (B, N, h, D))
+    dwq = dwk = None
+    if wq is not None:
+        dwq, dwk = torch.empty((2, D), dtype=torch.float32, device=q.device).unbind(0)
+    if workspace is None:
+        workspace = _alloc_ws(rope_workspace_bytes(B, N, Hq, Hkv, D, wq is not None), q.device)
+    ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    with _on(q.device):
+        rc = lib().fastmax_rope_bwd(q.data_ptr(), k.data_ptr(), _strides(q, k), gq.data_ptr(),
+                                    gk.data_ptr(), gv.data_ptr(), out[0].data_ptr(),
+                                    out[1].data_ptr(), out[2].data_ptr(), _strides(*out),
+                                    _ptr(dwq), _ptr(dwk), B, N, Hq, Hkv, D, rope, dt,
+                                    _ptr(workspace), ws_n, _stream(_stream_of(stream, q.device)))
+    if rc != OK:
+        raise FastmaxError(rc, "fastmax_rope_bwd")
+    return (*out, dwq, dwk)
+
+
+def _cache_of(q, k_cache, v_cache, Hkv):
+    """(pages, page size, strides) of the caches [pages, Hkv, page, D]."""
+    if k_cache.dim() != 4:
+        raise ValueError(f"k_cache must be [pages, Hkv, page, D], got shape {tuple(k_cache.shape)}")
+    pages, _, page, _ = k_cache.shape
+    _rows_of("k_cache", k_cache, q, (pages, Hkv, page, q.shape[-1]))
+    _rows_of("v_cache", v_cache, q, k_cache.shape)
+    if v_cache.stride() != k_cache.stride():
+        raise ValueError(f"k_cache and v_cache must have the same strides, got "
+                         f"{k_cache.stride()} and {v_cache.stride()}")
+    st = k_cache.stride()
+    return pages, page, Strides(st[0], st[2], st[1])
+
+
+def fastmax_cache_append(q, k, v, k_cache, v_cache, slots, pos, cos, sin, wq=None, wk=None,
+                         eps=1e-6, sections=None, interleaved=False, q_out=None, stream=None):
+    """New tokens q [T, Hq, D], k and v [T, Hkv, D] (strided views; D
+    contiguous): norm and rotation as in fastmax_rope_fwd, then the attention's
+    standardisation.  k^ and v go to the slots (int64 [T], page * page size +
+    place; -1: none) of the caches [pages, Hkv, page, D]; returns q^ [T, Hq, D]."""
+    import torch
+    _on_gpu(q, 3, "[T, Hq, D]")
+    T, Hq, D = q.shape
+    Hkv = k.shape[1] if k.dim() == 3 else 0
+    _rows_of("q", q, q, q.shape)
+    _rows_of("k", k, q, (T, Hkv, D))
+    _rows_of("v", v, q, (T, Hkv, D))
+    pages, page, cache = _cache_of(q, k_cache, v_cache, Hkv)
+    _whole("slots", slots, torch.int64, q.device, (T,))
+    dt = _dtype_code(q)
+    rope = _rope_of(q, (T,), pos, cos, sin, wq, wk, eps, sections, interleaved)
+    if q_out is None:
+        q_out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+    else:
+        _whole("q_out", q_out, q.dtype, q.device, (T, Hq, D))
+    with _on(q.device):
+        rc = lib().fastmax_cache_append(q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                        _strides(q, k, v), q_out.data_ptr(), k_cache.data_ptr(),
+                                        v_cache.data_ptr(), cache, slots.data_ptr(), T, Hq, Hkv, D,
+                                        pages, page, rope, dt,
+                                        _stream(_stream_of(stream, q.device)))
+    if rc != OK:
+        raise FastmaxError(rc, "fastmax_cache_append")
+    return q_out
+
+
+def paged_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window, sinks, dt) -> int:
+    return int(lib().fastmax_paged_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window,
+                                                   sinks, dt))
+
+
+def fastmax_paged_fwd(q, k_cache, v_cache, table, lens, q_start=None, max_q=None, max_len=None,
+                      p=2, scale=None, window=0, sinks=0, out=None, workspace=None, stream=None):
+    """Fastmax attention of new tokens over a paged cache.  q: q^ [T, Hq, D];
+    caches [pages, Hkv, page, D]; table int32 [S, cols] of pages; lens int32 [S]
+    tokens per sequence, its new ones last; q_start int32 [S + 1] where each
+    sequence's rows of q begin (None: one row each).  max_q and max_len: the most
+    rows and the most tokens of a sequence (None: T, or what the table holds).
+    window > 0: the last ``window`` keys and the first ``sinks`` only.  Returns
+    O [T, Hq, D]."""
+    import torch
+    _on_gpu(q, 3, "[T, Hq, D]")
+    T, Hq, D = q.shape
+    Hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
+    _rows_of("q", q, q, q.shape)
+    pages, page, cache = _cache_of(q, k_cache, v_cache, Hkv)
+    if table.dim() != 2:
+        raise ValueError(f"table must be [S, cols], got shape {tuple(table.shape)}")
+    S, cols = table.shape
+    _whole("table", table, torch.int32, q.device)
+    _whole("lens", lens, torch.int32, q.device, (S,))
+    if q_start is not None:
+        _whole("q_start", q_start, torch.int32, q.device, (S + 1,))
+    dt = _dtype_code(q)
+    if max_q is None:
+        max_q = 1 if q_start is None else T
+    if max_len is None:
+        max_len = cols * page
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+    else:
+        _whole("out", out, q.dtype, q.device, (T, Hq, D))
+    if workspace is None:
+        workspace = _alloc_ws(paged_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window,
+                                                    sinks, dt), q.device)
+    ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    with _on(q.device):
+        rc = lib().fastmax_paged_fwd(q.data_ptr(), _strides(q), k_cache.data_ptr(),
+                                     v_cache.data_ptr(), cache, table.data_ptr(), lens.data_ptr(),
+                                     _ptr(q_start), out.data_ptr(), S, T, Hq, Hkv, D, pages, page,
+                                     cols, max_q, max_len, p, 1.0 if scale is None else scale,
+                                     window, sinks, dt, _ptr(workspace), ws_n,
+                                     _stream(_stream_of(stream, q.device)))
+    if rc != OK:
+        raise FastmaxError(rc, "fastmax_paged_fwd")
+    return out
