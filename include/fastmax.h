@@ -401,8 +401,8 @@ int fastmax_rope_bwd(const void *q, const void *k, const fastmax_strides_t *stri
  *   q_out            : [T, Hq, D] contiguous, q^
  *   k_cache, v_cache : `pages` pages of page_size tokens (a power of two,
  *                      16 .. 1024) of Hkv heads, both with the strides `cache`
- *                      (batch: from page to page; NULL: [pages, Hkv,
- *                      page_size, D] contiguous); k^ and v go in
+ *                      (batch: from page to page, token <= 2^26; NULL: [pages,
+ *                      Hkv, page_size, D] contiguous); k^ and v go in
  *   slots            : int64 [T]: page * page_size + place in the page; a
  *                      token whose slot is outside the cache (-1: padding)
  *                      is not written, its q_out row is.  No two tokens may

@@ -101,6 +101,7 @@ int check_cache(const fastmax_strides_t *s, int Hkv, int D, int pages, int page_
         *out = {(long long)Hkv * page_size * D, D, (long long)page_size * D};
         return FASTMAX_OK;
     }
+    if (s->token > (1 << 26)) return FASTMAX_EINVAL;   // a tile's places are 32-bit offsets
     return check_strides(s, pages, page_size, Hkv, D, dt, rows_apart, out);
 }
 
@@ -133,7 +134,7 @@ int check_paged(int S, int T, int Hq, int Hkv, int D, int max_q, int max_len, in
     const int rc = check_sizes(T, Hq, Hkv, D, dt);
     if (rc != FASTMAX_OK) return rc;
     if (S < 1 || S > 65535 || max_q < 1 || max_q > T || max_len < 1 || max_len > (1 << 30)) return FASTMAX_EINVAL;
-    if (window < 0 || sinks < 0) return FASTMAX_EINVAL;
+    if (window < 0 || sinks < 0 || (long long)T * Hq > INT_MAX / 2) return FASTMAX_EINVAL;
     return FASTMAX_OK;
 }
 

@@ -17,89 +17,25 @@
 // neighbouring channels of the 8 keys whose weights it holds, and what MFMA
 // wants transposed is transposed within the lane.  Nothing goes through LDS
 // until the waves of a workgroup, which take key tiles in turn, add up.
-//
-// Every key that is loaded is one that some row of the tile sees: lanes whose
-// key is past the end, or in the gap behind the window, read such a key
-// instead and get weight 0, so what lies in unused or evicted slots never
-// enters a product.
+// Chunks of prompts with many rows go to fm_paged_chunk.hip.
 #include <hip/hip_runtime.h>
 
 #include "fm_internal.h"
+#include "fm_paged.h"
 #include "fm_rows.h"
 #include "fm_serve.h"
 
 namespace fm {
 namespace {
 
+using namespace paged;
+
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
-constexpr int THREADS = 256, WAVES = THREADS / 64;
-constexpr int KT = 16;   // keys per tile
-
-// The key tiles that a range of query positions [first, last] reads, in
-// order: `sink_tiles` from the start of the sequence, then from tile `low` on.
-struct Span {
-    int end;          // keys before this one exist for some row
-    int low_key;      // window: the lowest key the first position sees (0: no gap)
-    int sinks;        // first tokens that stay visible
-    int sink_tiles, low, tiles;
-    __device__ __forceinline__ int tile(int i) const { return i < sink_tiles ? i : i - sink_tiles + low; }
-    // The key to read in place of key n of the tile that ends at `last`: n
-    // itself unless no row sees it.
-    __device__ __forceinline__ int read(int n, int last) const
-    {
-        if (n >= sinks && n < low_key) n = low_key <= last ? low_key : sinks - 1;
-        return min(n, end - 1);
-    }
-};
-
-__device__ __forceinline__ Span span_of(int first, int last, int window, int sinks)
-{
-    Span s;
-    s.end = last + 1;
-    s.sinks = min(sinks, s.end);
-    s.low_key = max(0, first - window + 1);
-    if (s.low_key <= s.sinks) s.low_key = 0;
-    s.low = s.low_key / KT;
-    s.sink_tiles = s.low_key ? (s.sinks + KT - 1) / KT : 0;
-    if (s.sink_tiles >= s.low) s.sink_tiles = s.low = 0;
-    s.tiles = last < 0 ? 0 : s.sink_tiles + (s.end + KT - 1) / KT - s.low;
-    return s;
-}
-
-__device__ __forceinline__ bool visible(int n, int pos, int window, int sinks)
-{
-    return n <= pos && (n > pos - window || n < sinks);
-}
-
-// A sequence's new tokens: rows [t0, t0 + count) of q, the last at len - 1.
-struct Seq {
-    int t0, count, len;
-    bool cut;   // longer than its row of the page table
-};
-
-__device__ __forceinline__ Seq seq_of(const PagedArgs &a, int s)
-{
-    Seq q;
-    q.t0 = a.q_start ? min(max(a.q_start[s], 0), a.T) : s;
-    q.count = a.q_start ? min(max(a.q_start[s + 1], q.t0), a.T) - q.t0 : 1;
-    const long long room = (long long)a.table_cols << a.page_shift;
-    q.len = max(a.lens[s], 0);
-    q.cut = q.len > room;
-    q.len = (int)min((long long)q.len, room);
-    return q;
-}
-
-// Positions of the row tile [r0, r0 + 16 RT) of a sequence.
-__device__ __forceinline__ Span span_of_rows(const PagedArgs &a, const Seq &q, int r0, int rows)
-{
-    const int first = q.len - q.count + r0 / a.group;
-    const int last = q.len - q.count + min(q.count - 1, (r0 + rows - 1) / a.group);
-    return span_of(first, last, a.window, a.sinks);
-}
+constexpr int WAVES = 4, THREADS = 64 * WAVES;
 
 template <typename T, int D> struct Mat;
 
@@ -256,27 +192,31 @@ template <int D> struct Mat<float, D> {
 // MULTI: rows of several tokens may share a tile, so a key can be visible to
 // some rows of a tile and not to others.
 template <typename T, int D, int RT, bool MULTI>
-__global__ __launch_bounds__(THREADS) void paged_kernel(PagedArgs a, PagedPlan plan, float *part)
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && RT == 1 ? 3 : 1) void paged_kernel(PagedArgs a, PagedPlan plan, float *part)
 {
     using M = Mat<T, D>;
     constexpr int VW = M::VW, ROWS = 16 * RT, RS = D + 4;
     __shared__ float red[WAVES][16][RS];
     __shared__ float gred[WAVES][16];
 
+    // Splits last: later ones are empty in shorter sequences, and workgroups are
+    // dealt out to the XCDs in turn.
     int id = blockIdx.x;
-    const int split = id % plan.splits;
-    id /= plan.splits;
-    const int tile0 = id % plan.tiles;
-    id /= plan.tiles;
-    const int head = id % a.Hkv, s = id / a.Hkv;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, h = lane / 16, r16 = lane % 16;
+    const int head = id % a.Hkv;
+    id /= a.Hkv;
+    const int s = id % a.S;
+    id /= a.S;
+    const int tile0 = id % plan.tiles, split = id / plan.tiles;
+    const int wave = scalar(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 16, r16 = lane % 16;
     const Seq seq = seq_of(a, s);
     const int rows = seq.count * a.group, page_mask = (1 << a.page_shift) - 1;
     const T *kc = (const T *)a.k + head * a.cache.head, *vc = (const T *)a.v + head * a.cache.head;
+    const int32_t *table = a.table + (size_t)s * a.table_cols;
+    const int token = (int)a.cache.token;
 
     // max_q sets the grid; a sequence with more new tokens goes round again
     for (int r0 = tile0 * ROWS; r0 < rows; r0 += plan.tiles * ROWS) {
-        const Span sp = span_of_rows(a, seq, r0, ROWS);
+        const Span sp = scalar(span_of_rows(a, seq, r0, ROWS));
         const int begin = split * plan.chunk;
         const int end = split == plan.splits - 1 ? sp.tiles : min(sp.tiles, begin + plan.chunk);
         if (begin >= sp.tiles && split > 0) continue;   // the join knows
@@ -299,78 +239,96 @@ __global__ __launch_bounds__(THREADS) void paged_kernel(PagedArgs a, PagedPlan p
 #pragma unroll
             for (int j = 0; j < VW; ++j) acc[r][j] = f4{0.f, 0.f, 0.f, 0.f};
         }
-        const int first = seq.len - seq.count + r0 / a.group, last = sp.end - 1;
+        const int first = scalar(seq.len - seq.count + r0 / a.group), last = sp.end - 1;
+        // Key tiles [whole, whole_end) exist in full and every row sees all their
+        // keys; elsewhere keys are clamped and weights masked.
+        const int shift = sp.low - sp.sink_tiles;   // from a tile's number here to its own
+        const int whole = a.window < sp.end ? max(sp.sink_tiles, (last - a.window) / KT + 1 - shift) : 0;
+        const int whole_end = min(end, (first + 1) / KT - shift);
         bool bad = seq.cut;
 
-        for (int i0 = begin + 2 * wave; i0 < end; i0 += 2 * WAVES) {
-            typename M::K k[2];
-            typename M::V v;
-            int base[2];
-            bool all = i0 + 1 < end;   // every row sees every key of the step
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int tile = sp.tile(min(i0 + i, end - 1));
-                const int n0 = tile * KT;
-                base[i] = i0 + i < end ? n0 : INT32_MAX - KT;   // past every position
-                all &= n0 + KT - 1 <= first && (n0 > last - a.window || n0 + KT <= a.sinks);
-                int page = a.table[(size_t)s * a.table_cols + (n0 >> a.page_shift)];
-                if ((unsigned)page >= (unsigned)a.pages) {
-                    bad = true;
-                    page = 0;
-                }
-                const int nk = sp.read(n0 + r16, n0 + KT - 1);
-                const T *kp = kc + page * a.cache.batch, *vp = vc + page * a.cache.batch;
-                M::ld_row(kp + (nk & page_mask) * a.cache.token, h, k[i].x);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int nv = sp.read(n0 + 4 * h + j, n0 + KT - 1);
-                    M::ld_v(vp + (nv & page_mask) * a.cache.token, r16, v.x[4 * i + j]);
-                }
+        // The wave's steps of two key tiles, 32 steps at a time: where they begin
+        // in the cache, a tile to a lane, so that no step waits for the page
+        // table.
+        for (int b0 = begin + 2 * wave; b0 < end; b0 += 64 * WAVES) {
+            const int mine = sp.tile(min(b0 + lane / 2 * (2 * WAVES) + lane % 2, end - 1)) * KT;
+            int page = table[mine >> a.page_shift];
+            if ((unsigned)page >= (unsigned)a.pages) {
+                bad = true;
+                page = 0;
             }
-            // A value that is infinite or NaN takes the step out of MFMA: a row
-            // whose weight is 0 because it does not see the key would get NaN,
-            // and so would infinity times a weight's second part.
-            const bool odd = (M::PARTS || (MULTI && !all)) && __any(M::odd(v));
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                f4 w[2];
+            const long long at = page * a.cache.batch + (mine & page_mask) * a.cache.token;
+            for (int n = 0; n < 32; ++n) {
+                const int i0 = b0 + n * (2 * WAVES);
+                if (i0 >= end) break;
+                typename M::K k[2];
+                typename M::V v;
+                const bool all = i0 >= whole && i0 + 2 <= whole_end;
+                int base[2];   // of the key tiles; past every position if there is none
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const f4 x = M::scores(k[i], q[r]);
+                    const long long from =
+                        (long long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(at >> 32), 2 * n + i) << 32 |
+                                    (uint32_t)__builtin_amdgcn_readlane((int)at, 2 * n + i));
+                    const T *kp = kc + from, *vp = vc + from;
+                    const int n0 = sp.tile(min(i0 + i, end - 1)) * KT;
+                    base[i] = i0 + i < end ? n0 : INT32_MAX - KT;
+                    int kr = r16, vr[4] = {4 * h, 4 * h + 1, 4 * h + 2, 4 * h + 3};
+                    if (!all) {
+                        kr = sp.read(n0 + kr, n0 + KT - 1) - n0;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        w[i][j] = fmaf(fmaf(x[j], a.c2, a.c1), x[j], 1.0f);
-                        if (!all && !visible(base[i] + 4 * h + j, pos[r], a.window, a.sinks)) w[i][j] = 0.f;
-                        g[r] += w[i][j];
+                        for (int j = 0; j < 4; ++j) vr[j] = sp.read(n0 + vr[j], n0 + KT - 1) - n0;
                     }
-                }
-                if (!odd) {
-                    M::add(acc[r], v, w);
-                    continue;
-                }
-                // each row adds the keys it sees, one by one
+                    M::ld_row(kp + kr * token, h, k[i].x);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    for (int hh = 0; hh < 4; ++hh) {
-                        const float wk = __shfl(w[i / 4][i % 4], 16 * hh + r16);
-                        const int n = base[i / 4] + 4 * hh + i % 4;
-                        if (!visible(n, pos[r], a.window, a.sinks)) continue;
-                        const int page = a.table[(size_t)s * a.table_cols + (n >> a.page_shift)];
-                        if ((unsigned)page >= (unsigned)a.pages) continue;
-                        const T *vp = vc + page * a.cache.batch + (n & page_mask) * a.cache.token + h * (D / 4);
+                    for (int j = 0; j < 4; ++j) M::ld_v(vp + vr[j] * token, r16, v.x[4 * i + j]);
+                }
+                // A value that is infinite or NaN takes the step out of MFMA: a row
+                // whose weight is 0 because it does not see the key would get NaN,
+                // and so would infinity times a weight's second part.
+                const bool odd = (M::PARTS || (MULTI && !all)) && __any(M::odd(v));
 #pragma unroll
-                        for (int d = 0; d < D / 4; ++d)
-                            acc[r][d % VW][d / VW] = fmaf(wk, io<T>::ld(vp, d), acc[r][d % VW][d / VW]);
+                for (int r = 0; r < RT; ++r) {
+                    f4 w[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const f4 x = M::scores(k[i], q[r]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            w[i][j] = fmaf(fmaf(x[j], a.c2, a.c1), x[j], 1.0f);
+                            if (!all && !visible(base[i] + 4 * h + j, pos[r], a.window, a.sinks)) w[i][j] = 0.f;
+                            g[r] += w[i][j];
+                        }
+                    }
+                    if (!odd) {
+                        M::add(acc[r], v, w);
+                        continue;
+                    }
+                    // each row adds the keys it sees, one by one
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        for (int hh = 0; hh < 4; ++hh) {
+                            const float wk = __shfl(w[i / 4][i % 4], 16 * hh + r16);
+                            const int key = base[i / 4] + 4 * hh + i % 4;
+                            if (!visible(key, pos[r], a.window, a.sinks)) continue;
+                            const int pg = table[key >> a.page_shift];
+                            if ((unsigned)pg >= (unsigned)a.pages) continue;
+                            const T *vp = vc + pg * a.cache.batch + (key & page_mask) * a.cache.token + h * (D / 4);
+#pragma unroll
+                            for (int d = 0; d < D / 4; ++d)
+                                acc[r][d % VW][d / VW] = fmaf(wk, io<T>::ld(vp, d), acc[r][d % VW][d / VW]);
+                        }
                     }
                 }
             }
         }
+        bad = __any(bad);
 
         // the waves' sums, one row tile at a time
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            __syncthreads();
             const float gs = rows4_sum(g[r]);
+            __syncthreads();
             if (h == 0) gred[wave][r16] = bad ? __builtin_nanf("") : gs;
 #pragma unroll
             for (int d = 0; d < D / 4; ++d) red[wave][r16][h * (D / 4) + d] = acc[r][d % VW][d / VW];
@@ -404,32 +362,48 @@ __global__ __launch_bounds__(THREADS) void paged_kernel(PagedArgs a, PagedPlan p
     }
 }
 
-// Adds the splits' sums: 16 lanes a row.
+// Adds the splits' sums: a row to a wave, 16 lanes side by side over its
+// channels and four of these over its splits, four splits in flight in each.
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS) void join_kernel(PagedArgs a, PagedPlan plan, const float *part)
 {
-    constexpr int VW = D / 16;
+    constexpr int VW = D / 16, U = 4;
     const int s = blockIdx.y;
     const Seq seq = seq_of(a, s);
     const long long n = (long long)seq.count * a.Hq;
-    const int c = threadIdx.x % 16 * VW;
+    const int c = threadIdx.x % 16 * VW, l = threadIdx.x / 16 % 4;
     const float *gpart = part + (size_t)a.T * a.Hq * plan.splits * D;
-    for (long long i = (long long)blockIdx.x * (THREADS / 16) + threadIdx.x / 16; i < n;
-         i += (long long)gridDim.x * (THREADS / 16)) {
+    for (long long i = (long long)blockIdx.x * WAVES + threadIdx.x / 64; i < n; i += (long long)gridDim.x * WAVES) {
         const int t = (int)(i / a.Hq), head = (int)(i - (long long)t * a.Hq);
-        const int row = t * a.group + head % a.group, rows = 16 * plan.row_tiles;
-        const Span sp = span_of_rows(a, seq, row / rows * rows, rows);
+        const int row = t * a.group + head % a.group;
+        const Span sp = span_of_rows(a, seq, row / plan.rows * plan.rows, plan.rows);
         const int used = max(1, min(plan.splits, (sp.tiles + plan.chunk - 1) / plan.chunk));
         const size_t o = (size_t)(seq.t0 + t) * a.Hq + head;
+        const float *p = part + o * plan.splits * D + c, *gp = gpart + o * plan.splits;
         float f[VW], g = 0.f;
 #pragma unroll
         for (int j = 0; j < VW; ++j) f[j] = 0.f;
-        for (int k = 0; k < used; ++k) {
-            const float *p = part + (o * plan.splits + k) * D + c;
-            g += gpart[o * plan.splits + k];
+        for (int k = l; k < used; k += 4 * U) {
+            float x[U][VW], y[U];
 #pragma unroll
-            for (int j = 0; j < VW; ++j) f[j] += p[j];
+            for (int u = 0; u < U; ++u) {
+                const int at = min(k + 4 * u, used - 1);
+                y[u] = gp[at];
+#pragma unroll
+                for (int j = 0; j < VW; ++j) x[u][j] = p[(size_t)at * D + j];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (k + 4 * u >= used) break;
+                g += y[u];
+#pragma unroll
+                for (int j = 0; j < VW; ++j) f[j] += x[u][j];
+            }
         }
+        g = rows4_sum(g);
+#pragma unroll
+        for (int j = 0; j < VW; ++j) f[j] = rows4_sum(f[j]);
+        if (l) continue;
         const bool none = seq.len - seq.count + t < 0;
         T *out = (T *)a.out + o * D + c;
 #pragma unroll
@@ -438,37 +412,38 @@ __global__ __launch_bounds__(THREADS) void join_kernel(PagedArgs a, PagedPlan pl
 }
 
 template <typename T, int D, int RT>
-hipError_t launch(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
+hipError_t launch_rt(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
 {
     const long long blocks = (long long)plan.splits * plan.tiles * a.Hkv * a.S;
-    if (!grid_fits(blocks, THREADS) || a.S > 65535) return hipErrorInvalidConfiguration;
+    if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
     if (a.q_start) paged_kernel<T, D, RT, true><<<(unsigned)blocks, THREADS, 0, st>>>(a, plan, part);
     else paged_kernel<T, D, RT, false><<<(unsigned)blocks, THREADS, 0, st>>>(a, plan, part);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || plan.splits == 1) return e;
-    const int rows = 16 * RT * plan.tiles / a.group * a.Hq;
-    const dim3 grid((unsigned)((rows + 15) / 16), (unsigned)a.S);
-    join_kernel<T, D><<<grid, THREADS, 0, st>>>(a, plan, part);
     return hipGetLastError();
 }
 
 template <typename T, int D>
-hipError_t launch_rt(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
+hipError_t launch(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
 {
-    switch (plan.row_tiles) {
-    case 1: return launch<T, D, 1>(a, plan, part, st);
-    case 2: return launch<T, D, 2>(a, plan, part, st);
-    default: return launch<T, D, 4>(a, plan, part, st);
-    }
+    hipError_t e;
+    if (plan.chunk_kernel) e = paged_chunk(a, plan, D, part, st);
+    else if (plan.rows == 16) e = launch_rt<T, D, 1>(a, plan, part, st);
+    else if (plan.rows == 32) e = launch_rt<T, D, 2>(a, plan, part, st);
+    else e = launch_rt<T, D, 4>(a, plan, part, st);
+    if (e != hipSuccess || plan.splits == 1) return e;
+    const long long rows = (long long)plan.rows * plan.tiles / a.group * a.Hq;
+    const long long most = (long long)a.T * a.Hq;   // of one sequence
+    const dim3 grid((unsigned)(((rows < most ? rows : most) + WAVES - 1) / WAVES), (unsigned)a.S);
+    join_kernel<T, D><<<grid, THREADS, 0, st>>>(a, plan, part);
+    return hipGetLastError();
 }
 
 template <typename T> hipError_t launch_d(const PagedArgs &a, const PagedPlan &plan, int D, float *part, hipStream_t st)
 {
     switch (D) {
-    case 16: return launch_rt<T, 16>(a, plan, part, st);
-    case 32: return launch_rt<T, 32>(a, plan, part, st);
-    case 64: return launch_rt<T, 64>(a, plan, part, st);
-    default: return launch_rt<T, 128>(a, plan, part, st);
+    case 16: return launch<T, 16>(a, plan, part, st);
+    case 32: return launch<T, 32>(a, plan, part, st);
+    case 64: return launch<T, 64>(a, plan, part, st);
+    default: return launch<T, 128>(a, plan, part, st);
     }
 }
 
@@ -479,18 +454,39 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
 {
     PagedPlan plan;
     const long long rows = (long long)max_q * (Hq / Hkv);
-    plan.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const long long per = 16 * plan.row_tiles, tiles = (rows + per - 1) / per;
+    // Several tokens of a sequence and more than one MFMA tile of rows: the
+    // chunk kernel (8 sequences of 4096 keys, D = 128, 4 query heads to a key
+    // head: 36 against 46 us for 6 tokens, 37 against 71 for 16).  Single
+    // tokens stay here whatever their heads: their weights keep two parts.
+    plan.chunk_kernel = is_bf16 && D >= 32 && max_q > 1 && rows > 16;
+    plan.rows = plan.chunk_kernel ? CHUNK_ROWS : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    const long long tiles = (rows + plan.rows - 1) / plan.rows;
     // the most key tiles that a row tile can see
-    const long long tokens = per * Hkv / Hq + 2;
+    const long long tokens = (long long)plan.rows * Hkv / Hq + 2;
     const long long seen = (long long)window + tokens + 2 * KT + sinks;
     const long long keys = max_len < seen ? max_len : seen;
     const long long key_tiles = (keys + KT - 1) / KT;
-    // about 1024 workgroups, 256 keys in each at least
+    // Splits, where (sequence, head, row tile) leave CUs idle: toward 2048
+    // workgroups (512 of the chunk kernel's, which are two to a CU) while
+    // 1024 keys (float32: 512) are left for each, toward 512 below that, down
+    // to 256 keys.  Less costs more in partial sums than the CUs gain: one
+    // sequence of 131072 keys, 8 heads, D = 128: 112 us in 1024 workgroups,
+    // 127 in 2048; 4 of 16384: 29 us in 512, 39 in 2048; 61 of up to 8192:
+    // 155 us in up to 2440, 171 in 1464.
     const long long base = tiles * Hkv * S;
-    long long splits = (1024 + base - 1) / base;
-    const long long most = (key_tiles + 15) / 16;
-    splits = splits < most ? splits : most;
+    const auto toward = [&](long long target, long long least) {
+        const long long by_target = (target + base - 1) / base, by_size = key_tiles / least;
+        return by_target < by_size ? by_target : by_size;
+    };
+    long long splits = 1;
+    if (plan.chunk_kernel) {
+        splits = toward(512, 32);
+    } else if (base < 1024) {
+        splits = toward(2048, is_bf16 ? 64 : 32);
+        const long long few = toward(512, 16);
+        if (splits * base < 512 && splits < few) splits = few;
+    }
+    if (splits < 1) splits = 1;
     long long chunk = (key_tiles + splits - 1) / splits;
     chunk = (chunk + 2 * WAVES - 1) / (2 * WAVES) * (2 * WAVES);
     plan.tiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);

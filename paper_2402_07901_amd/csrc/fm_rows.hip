@@ -252,25 +252,33 @@ __global__ __launch_bounds__(THREADS) void rope_bwd_kernel(RowsBwdArgs a, int pe
     }
 }
 
-// dwq (block row 0) and dwk (1): sums of their partial rows, 16 channels a
-// workgroup, in double precision so that the order of a long sum does not
-// show.
-__global__ __launch_bounds__(THREADS) void weight_sum_kernel(const float *partial, float *dwq, float *dwk,
-                                                             long long nq, long long nk, int D)
+// dwq (block row 0) and dwk (1): sums of their partial rows, 16 channels and 64
+// rows side by side in a workgroup, in double precision so that the order of
+// a long sum does not show.
+constexpr int SUM_THREADS = 1024;
+__global__ __launch_bounds__(SUM_THREADS) void weight_sum_kernel(const float *partial, float *dwq, float *dwk,
+                                                                 long long nq, long long nk, int D)
 {
-    __shared__ double red[THREADS];
+    __shared__ double red[SUM_THREADS];
+    constexpr int LANES = SUM_THREADS / 16, U = 8;
     const bool keys = blockIdx.y;
-    const float *p = partial + (keys ? nq * D : 0);
     const long long rows = keys ? nk : nq;
     const int ch = blockIdx.x * 16 + threadIdx.x % 16;
+    const float *p = partial + (keys ? nq * D : 0) + ch;
     double s = 0.0;
-    for (long long r = threadIdx.x / 16; r < rows; r += THREADS / 16) s += (double)p[r * D + ch];
-    red[threadIdx.x] = s;
-    __syncthreads();
-    if (threadIdx.x < 16) {
-        for (int i = 1; i < THREADS / 16; ++i) s += red[threadIdx.x + 16 * i];
-        (keys ? dwk : dwq)[ch] = (float)s;
+    for (long long r = threadIdx.x / 16; r < rows; r += LANES * U) {
+        float x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = r + LANES * u < rows ? p[(r + LANES * u) * D] : 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) s += (double)x[u];
     }
+    red[threadIdx.x] = s;
+    for (int o = LANES / 2; o; o /= 2) {
+        __syncthreads();
+        if (threadIdx.x < 16 * o) red[threadIdx.x] = s = s + red[threadIdx.x + 16 * o];
+    }
+    if (threadIdx.x < 16) (keys ? dwk : dwq)[ch] = (float)s;
 }
 
 long long token_blocks(long long tokens, int D) { return (tokens * (D / 16) + THREADS - 1) / THREADS; }
@@ -345,7 +353,7 @@ hipError_t rope_bwd(const RowsBwdArgs &a, int D, int is_bf16, void *ws, hipStrea
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.rope.wq) return e;
     const long long nq = blocks * ((a.Hq + per - 1) / per), nk = blocks * ((a.Hkv + per - 1) / per);
-    weight_sum_kernel<<<dim3(D / 16, 2), THREADS, 0, st>>>(partial, a.dwq, a.dwk, nq, nk, D);
+    weight_sum_kernel<<<dim3(D / 16, 2), SUM_THREADS, 0, st>>>(partial, a.dwq, a.dwk, nq, nk, D);
     return hipGetLastError();
 }
 

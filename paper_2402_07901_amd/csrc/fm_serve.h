@@ -62,7 +62,8 @@ struct PagedArgs {
 };
 // How a call is cut: rows of a (sequence, key head) in tiles, keys in splits.
 struct PagedPlan {
-    int row_tiles;                 // tiles of 16 rows a wave holds
+    bool chunk_kernel;             // fm_paged_chunk.hip, else fm_paged.hip
+    int rows;                      // rows of a row tile
     int tiles;                     // row tiles in the grid
     int chunk;                     // key tiles of 16 per split
     int splits;
@@ -72,5 +73,7 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
 size_t paged_workspace(const PagedPlan &plan, int T, int Hq, int D);
 hipError_t paged_fwd(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, void *ws,
                      hipStream_t st);
+constexpr int CHUNK_ROWS = 128;    // rows of a workgroup of the chunk kernel
+hipError_t paged_chunk(const PagedArgs &a, const PagedPlan &plan, int D, float *part, hipStream_t st);
 
 }  // namespace fm
