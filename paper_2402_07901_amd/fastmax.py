@@ -418,80 +418,92 @@ def fastmax_bwd_dropout(q, k, v, out, dout, g, bits, rate, causal=False, scale=N
 # Around the attention: norm and rotation of a projection's rows, shared heads,
 # a paged cache and the attention of new tokens over it.
 # ---------------------------------------------------------------------------
+# The usual arguments pass one comparison each; what is wrong is found out after.
 def _rows_of(name, t, like, shape):
     """Checks token rows: ``like``'s dtype and device, the given shape, D
     contiguous (the library checks the other strides)."""
+    if (t.shape == shape and t.dtype == like.dtype and t.get_device() == like.get_device()
+            and t.stride(-1) == 1):
+        return
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype != like.dtype:
         raise ValueError(f"{name} must be {like.dtype}, got {t.dtype}")
     if t.device != like.device:
         raise ValueError(f"{name} is on {t.device}, not on {like.device}")
-    if t.stride(-1) != 1:
-        raise ValueError(f"{name}'s channels must be contiguous")
+    raise ValueError(f"{name}'s channels must be contiguous")
 
 
-def _whole(name, t, dtype, device, shape=None):
-    """Checks a contiguous tensor of a given dtype (and shape)."""
-    if shape is not None and tuple(t.shape) != tuple(shape):
+def _whole(name, t, dtype, like, shape):
+    """Checks a contiguous tensor of a given dtype and shape on ``like``'s device."""
+    if (t.shape == shape and t.dtype == dtype and t.get_device() == like.get_device()
+            and t.is_contiguous()):
+        return
+    if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
+    raise ValueError(f"{name} must be contiguous")
 
 
-def _strides(*tensors):
-    """fastmax_strides_t array of [(B,) N, H, D] tensors."""
-    out = (Strides * len(tensors))()
-    for s, t in zip(out, tensors):
-        st = t.stride()
-        s.batch, s.token, s.head = (st[0] if len(st) == 4 else 0), st[-3], st[-2]
-    return out
+_S1, _S2, _S3 = Strides, Strides * 2, Strides * 3
+
+
+def _stride4(t):
+    st = t.stride()
+    return st[0], st[1], st[2]
+
+
+def _stride3(t):
+    st = t.stride()
+    return 0, st[0], st[1]
 
 
 def _rope_of(q, tokens, pos, cos, sin, wq, wk, eps, sections, interleaved):
     """The fastmax_rope_t of a call whose rows are q's; ``tokens``: q's
     leading sizes."""
     import torch
-    D, device = q.shape[-1], q.device
-    r = Rope()
-    r.interleaved, r.eps = int(bool(interleaved)), float(eps)
+    p = c = s = gq = gk = None
+    rows = rot = 0
+    axes = 1
     if (cos is None) != (sin is None) or (cos is None) != (pos is None):
         raise ValueError("pos, cos and sin go together")
     if cos is not None:
-        _whole("cos", cos, torch.float32, device)
         if cos.dim() != 2:
             raise ValueError(f"cos must be [rows, rot / 2], got shape {tuple(cos.shape)}")
-        _whole("sin", sin, torch.float32, device, cos.shape)
-        if pos.dim() == len(tokens):
-            pos = pos.unsqueeze(-1)
-        axes = pos.shape[-1]
-        _whole("pos", pos, torch.int32, device, (*tokens, axes))
+        _whole("cos", cos, torch.float32, q, cos.shape)
+        _whole("sin", sin, torch.float32, q, cos.shape)
+        if pos.dim() > len(tokens):
+            axes = pos.shape[-1]
+            _whole("pos", pos, torch.int32, q, (*tokens, axes))
+        else:
+            _whole("pos", pos, torch.int32, q, tokens)
         if not 1 <= axes <= 4:
             raise ValueError(f"1 to 4 axes of positions, got {axes}")
-        r.cos, r.sin, r.pos = cos.data_ptr(), sin.data_ptr(), pos.data_ptr()
-        r.table_rows, r.rot, r.axes = cos.shape[0], 2 * cos.shape[1], axes
-        if axes > 1:
-            if sections is None or len(sections) != axes:
-                raise ValueError(f"{axes} axes of positions need as many sections")
-            r.sections[:axes] = [int(n) for n in sections]
+        if axes > 1 and (sections is None or len(sections) != axes):
+            raise ValueError(f"{axes} axes of positions need as many sections")
+        p, c, s = pos.data_ptr(), cos.data_ptr(), sin.data_ptr()
+        rows, rot = cos.shape[0], 2 * cos.shape[1]
     if (wq is None) != (wk is None):
         raise ValueError("wq and wk go together")
     if wq is not None:
-        _whole("wq", wq, torch.float32, device, (D,))
-        _whole("wk", wk, torch.float32, device, (D,))
-        r.wq, r.wk = wq.data_ptr(), wk.data_ptr()
-    return r
+        D = q.shape[-1:]
+        _whole("wq", wq, torch.float32, q, D)
+        _whole("wk", wk, torch.float32, q, D)
+        gq, gk = wq.data_ptr(), wk.data_ptr()
+    parts = tuple(sections) if axes > 1 else ()
+    return Rope(c, s, p, rows, rot, axes, parts, 1 if interleaved else 0, gq, gk, eps)
 
 
 def _on_gpu(q, dims, what):
     if q.dim() != dims:
         raise ValueError(f"q must be {what}, got shape {tuple(q.shape)}")
-    if q.device.type != "cuda":
+    if not q.is_cuda:
         raise ValueError(f"the tensors must be on a GPU, q is on {q.device}")
+    if q.stride(-1) != 1:
+        raise ValueError("q's channels must be contiguous")
 
 
 def fastmax_rope_fwd(q, k, v, pos, cos, sin, wq=None, wk=None, eps=1e-6, sections=None,
@@ -506,7 +518,6 @@ def fastmax_rope_fwd(q, k, v, pos, cos, sin, wq=None, wk=None, eps=1e-6, section
     _on_gpu(q, 4, "[B, N, Hq, D]")
     B, N, Hq, D = q.shape
     Hkv = k.shape[2] if k.dim() == 4 else 0
-    _rows_of("q", q, q, q.shape)
     _rows_of("k", k, q, (B, N, Hkv, D))
     _rows_of("v", v, q, (B, N, Hkv, D))
     dt = _dtype_code(q)
@@ -515,9 +526,10 @@ def fastmax_rope_fwd(q, k, v, pos, cos, sin, wq=None, wk=None, eps=1e-6, section
         out = tuple(torch.empty((B, Hq, N, D), dtype=q.dtype, device=q.device) for _ in range(3))
     else:
         for name, t in zip(("out[0]", "out[1]", "out[2]"), out):
-            _whole(name, t, q.dtype, q.device, (B, Hq, N, D))
+            _whole(name, t, q.dtype, q, (B, Hq, N, D))
     with _on(q.device):
-        rc = lib().fastmax_rope_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), _strides(q, k, v),
+        rc = lib().fastmax_rope_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                    _S3(_stride4(q), _stride4(k), _stride4(v)),
                                     out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), B, N,
                                     Hq, Hkv, D, rope, dt, _stream(_stream_of(stream, q.device)))
     if rc != OK:
@@ -540,10 +552,9 @@ def fastmax_rope_bwd(q, k, gq, gk, gv, pos, cos, sin, wq=None, wk=None, eps=1e-6
     _on_gpu(q, 4, "[B, N, Hq, D]")
     B, N, Hq, D = q.shape
     Hkv = k.shape[2] if k.dim() == 4 else 0
-    _rows_of("q", q, q, q.shape)
     _rows_of("k", k, q, (B, N, Hkv, D))
     for name, t in (("gq", gq), ("gk", gk), ("gv", gv)):
-        _whole(name, t, q.dtype, q.device, (B, Hq, N, D))
+        _whole(name, t, q.dtype, q, (B, Hq, N, D))
     dt = _dtype_code(q)
     rope = _rope_of(q, (B, N), pos, cos, sin, wq, wk, eps, sections, interleaved)
     if out is None:
@@ -559,9 +570,9 @@ def fastmax_rope_bwd(q, k, gq, gk, gv, pos, cos, sin, wq=None, wk=None, eps=1e-6
         workspace = _alloc_ws(rope_workspace_bytes(B, N, Hq, Hkv, D, wq is not None), q.device)
     ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
     with _on(q.device):
-        rc = lib().fastmax_rope_bwd(q.data_ptr(), k.data_ptr(), _strides(q, k), gq.data_ptr(),
-                                    gk.data_ptr(), gv.data_ptr(), out[0].data_ptr(),
-                                    out[1].data_ptr(), out[2].data_ptr(), _strides(*out),
+        rc = lib().fastmax_rope_bwd(q.data_ptr(), k.data_ptr(), _S2(_stride4(q), _stride4(k)),
+                                    gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), out[0].data_ptr(),
+                                    out[1].data_ptr(), out[2].data_ptr(), _S3(*map(_stride4, out)),
                                     _ptr(dwq), _ptr(dwk), B, N, Hq, Hkv, D, rope, dt,
                                     _ptr(workspace), ws_n, _stream(_stream_of(stream, q.device)))
     if rc != OK:
@@ -593,20 +604,20 @@ def fastmax_cache_append(q, k, v, k_cache, v_cache, slots, pos, cos, sin, wq=Non
     _on_gpu(q, 3, "[T, Hq, D]")
     T, Hq, D = q.shape
     Hkv = k.shape[1] if k.dim() == 3 else 0
-    _rows_of("q", q, q, q.shape)
     _rows_of("k", k, q, (T, Hkv, D))
     _rows_of("v", v, q, (T, Hkv, D))
     pages, page, cache = _cache_of(q, k_cache, v_cache, Hkv)
-    _whole("slots", slots, torch.int64, q.device, (T,))
+    _whole("slots", slots, torch.int64, q, (T,))
     dt = _dtype_code(q)
     rope = _rope_of(q, (T,), pos, cos, sin, wq, wk, eps, sections, interleaved)
     if q_out is None:
         q_out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
     else:
-        _whole("q_out", q_out, q.dtype, q.device, (T, Hq, D))
+        _whole("q_out", q_out, q.dtype, q, (T, Hq, D))
     with _on(q.device):
         rc = lib().fastmax_cache_append(q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                        _strides(q, k, v), q_out.data_ptr(), k_cache.data_ptr(),
+                                        _S3(_stride3(q), _stride3(k), _stride3(v)),
+                                        q_out.data_ptr(), k_cache.data_ptr(),
                                         v_cache.data_ptr(), cache, slots.data_ptr(), T, Hq, Hkv, D,
                                         pages, page, rope, dt,
                                         _stream(_stream_of(stream, q.device)))
@@ -633,15 +644,14 @@ def fastmax_paged_fwd(q, k_cache, v_cache, table, lens, q_start=None, max_q=None
     _on_gpu(q, 3, "[T, Hq, D]")
     T, Hq, D = q.shape
     Hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
-    _rows_of("q", q, q, q.shape)
     pages, page, cache = _cache_of(q, k_cache, v_cache, Hkv)
     if table.dim() != 2:
         raise ValueError(f"table must be [S, cols], got shape {tuple(table.shape)}")
     S, cols = table.shape
-    _whole("table", table, torch.int32, q.device)
-    _whole("lens", lens, torch.int32, q.device, (S,))
+    _whole("table", table, torch.int32, q, table.shape)
+    _whole("lens", lens, torch.int32, q, (S,))
     if q_start is not None:
-        _whole("q_start", q_start, torch.int32, q.device, (S + 1,))
+        _whole("q_start", q_start, torch.int32, q, (S + 1,))
     dt = _dtype_code(q)
     if max_q is None:
         max_q = 1 if q_start is None else T
@@ -650,13 +660,13 @@ def fastmax_paged_fwd(q, k_cache, v_cache, table, lens, q_start=None, max_q=None
     if out is None:
         out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
     else:
-        _whole("out", out, q.dtype, q.device, (T, Hq, D))
+        _whole("out", out, q.dtype, q, (T, Hq, D))
     if workspace is None:
         workspace = _alloc_ws(paged_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window,
                                                     sinks, dt), q.device)
     ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
     with _on(q.device):
-        rc = lib().fastmax_paged_fwd(q.data_ptr(), _strides(q), k_cache.data_ptr(),
+        rc = lib().fastmax_paged_fwd(q.data_ptr(), _S1(*_stride3(q)), k_cache.data_ptr(),
                                      v_cache.data_ptr(), cache, table.data_ptr(), lens.data_ptr(),
                                      _ptr(q_start), out.data_ptr(), S, T, Hq, Hkv, D, pages, page,
                                      cols, max_q, max_len, p, 1.0 if scale is None else scale,
