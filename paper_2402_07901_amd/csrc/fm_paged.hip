@@ -425,10 +425,11 @@ template <typename T, int D>
 hipError_t launch(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
 {
     hipError_t e;
-    if (plan.chunk_kernel) e = paged_chunk(a, plan, D, part, st);
+    if (plan.chunk_kernel) e = paged_chunk(a, plan, D, sizeof(T) == 2, part, st);
     else if (plan.rows == 16) e = launch_rt<T, D, 1>(a, plan, part, st);
     else if (plan.rows == 32) e = launch_rt<T, D, 2>(a, plan, part, st);
-    else e = launch_rt<T, D, 4>(a, plan, part, st);
+    else if constexpr (sizeof(T) * D <= 256) e = launch_rt<T, D, 4>(a, plan, part, st);
+    else e = hipErrorInvalidValue;   // no plan has such rows
     if (e != hipSuccess || plan.splits == 1) return e;
     const long long rows = (long long)plan.rows * plan.tiles / a.group * a.Hq;
     const long long most = (long long)a.T * a.Hq;   // of one sequence
@@ -458,8 +459,8 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
     // chunk kernel (8 sequences of 4096 keys, D = 128, 4 query heads to a key
     // head: 36 against 46 us for 6 tokens, 37 against 71 for 16).  Single
     // tokens stay here whatever their heads: their weights keep two parts.
-    plan.chunk_kernel = is_bf16 && D >= 32 && max_q > 1 && rows > 16;
-    plan.rows = plan.chunk_kernel ? CHUNK_ROWS : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    plan.chunk_kernel = D >= 32 && max_q > 1 && rows > 16;
+    plan.rows = plan.chunk_kernel ? CHUNK_ROWS : rows <= 16 ? 16 : rows <= 32 || (!is_bf16 && D == 128) ? 32 : 64;
     const long long tiles = (rows + plan.rows - 1) / plan.rows;
     // the most key tiles that a row tile can see
     const long long tokens = (long long)plan.rows * Hkv / Hq + 2;
@@ -467,7 +468,7 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
     const long long keys = max_len < seen ? max_len : seen;
     const long long key_tiles = (keys + KT - 1) / KT;
     // Splits, where (sequence, head, row tile) leave CUs idle: toward 2048
-    // workgroups (512 of the chunk kernel's, which are two to a CU) while
+    // workgroups (1024 of the chunk kernel's, which are two to a CU) while
     // 1024 keys (float32: 512) are left for each, toward 512 below that, down
     // to 256 keys.  Less costs more in partial sums than the CUs gain: one
     // sequence of 131072 keys, 8 heads, D = 128: 112 us in 1024 workgroups,
@@ -480,7 +481,11 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
     };
     long long splits = 1;
     if (plan.chunk_kernel) {
-        splits = toward(512, 32);
+        splits = toward(1024, 64);
+        for (const int t : {512, 256}) {
+            const long long few = toward(t, t / 16);
+            if (splits * base < t && splits < few) splits = few;
+        }
     } else if (base < 1024) {
         splits = toward(2048, is_bf16 ? 64 : 32);
         const long long few = toward(512, 16);

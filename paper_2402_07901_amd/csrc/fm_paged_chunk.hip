@@ -1,8 +1,8 @@
-// Paged attention of many rows of a sequence (chunks of prompts), bf16.
+// Paged attention of many rows of a sequence (chunks of prompts).
 //
 // MFMA bounds it, so keys and values are staged in LDS for a workgroup's 128
-// rows, 64 keys at a time, and each of its four waves works on 32 rows with
-// 32x32x16 tiles:
+// rows, 64 keys at a time (float32 at D = 128: 32), and each of its four waves
+// works on 32 rows with 32x32 tiles.  bf16, 32x32x16:
 //   S^T = K Q^T    A: 32 keys (one 16-byte LDS read per lane and 16 channels),
 //                  B: q^ of 32 rows, in registers throughout
 //   O^T += V^T W^T B: the weights, which the accumulator layout of S^T holds
@@ -10,17 +10,21 @@
 //                  {4h..4h+3, 8+4h..8+4h+3} for the lanes of half h; A: the
 //                  same keys of 32 channels, through the transposing LDS read
 // (lane = 32 h + c32; accumulator register i: column c32, row 8 (i/4) + 4 h + i%4).
-// The next 64 keys go straight to the other LDS buffer (global_load_lds) while
+// float32, 32x32x2: the lanes of half h hold channels h D/2 .. (h + 1) D/2 of
+// K and Q, 16 bytes at a time; the weights of accumulator register i are B of
+// the step with keys 8 (i/4) + i%4 and 4 more, and with channel c32 D/32 + d in
+// row c32 of A for product d a lane reads D/32 neighbouring channels of a key.
+// The next keys go straight to the other LDS buffer (global_load_lds) while
 // these are worked on.  Registers: two waves on a SIMD, from two workgroups,
 // whose products and weights overlap.  64 rows per wave read LDS half as often
 // but leave one wave on a SIMD at D = 128: 904 against 1003 TFLOP/s.
 //
-// LDS rows are D channels with no padding; the 16-byte piece c of row r lies
+// LDS rows have no padding; the 16-byte piece c of row r lies
 // at piece c ^ swizzle(r), which puts 8 consecutive rows' piece c (score
 // operands) and pieces c, c + 1 of 4 consecutive rows (value operands) on
 // distinct banks.
 //
-// The weights enter as bf16, and the row's sum adds the rounded ones: what is
+// In bf16 the weights enter as bf16, and the row's sum adds the rounded ones: what is
 // rounded is the weights of an average, whose errors of 2^-9 each largely
 // cancel, below the rounding of the output itself; two parts, as in the
 // register kernel, would add half the MFMA work.
@@ -39,17 +43,17 @@ using namespace paged;
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef short s4 __attribute__((ext_vector_type(4)));
+typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-typedef unsigned short us2 __attribute__((ext_vector_type(2)));
 
 constexpr int THREADS = 256;
-constexpr int KB = 64;   // keys per LDS buffer
 constexpr int WAIT_LOADS = 0x0f70;   // vmcnt(0), the other counters at their most
 
-template <int D> __device__ __forceinline__ int swizzle(int r)
+// C: 16-byte pieces of a row
+template <int C> __device__ __forceinline__ int swizzle(int r)
 {
-    if constexpr (D >= 64) return (r & 3) << 1 | (r >> 2 & 1);
+    if constexpr (C >= 8) return (r & 3) << 1 | (r >> 2 & 1);
     else return (r >> 1 & 1) << 1 | (r >> 2 & 1);   // two rows to a line of banks
 }
 
@@ -73,12 +77,125 @@ __device__ __forceinline__ void to_lds(const void *from, void *to)
     __builtin_amdgcn_global_load_lds((gp)from, (lp)to, 16, 0, 0);
 }
 
-template <int D>
+// What a wave does with 32 keys `kb` of a buffer: scores of its 32 rows, weights
+// from scores (and their sum: rounded where they are), values under them.
+template <typename T, int D> struct Wave;
+
+template <int D> struct Wave<bf16_t, D> {
+    static constexpr int C = D / 8, KC = D / 16, DT = D / 32;
+    u4 q[KC], va[2][DT];
+
+    __device__ __forceinline__ void load_q(const bf16_t *p, int hh)
+    {
+#pragma unroll
+        for (int k = 0; k < KC; ++k) q[k] = *(const u4 *)(p + 16 * k + 8 * hh);
+    }
+    __device__ __forceinline__ f16v scores(const u4 *kl, int kb, int hh, int c32) const
+    {
+        u4 k[KC];
+#pragma unroll
+        for (int i = 0; i < KC; ++i) k[i] = kl[(32 * kb + c32) * C + ((2 * i + hh) ^ swizzle<C>(c32))];
+        f16v x = f16v{};
+#pragma unroll
+        for (int i = 0; i < KC; ++i) x = mma(k[i], q[i], x);
+        return x;
+    }
+    // The value operands are read ahead of the weights.
+    __device__ __forceinline__ void read(const u4 *vl, int kb, int lane)
+    {
+        const s4 *v = (const s4 *)vl;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                typedef s4 __attribute__((address_space(3))) *lp;
+                const int j = lane >> 2 & 3, hh = lane >> 5, r = 32 * kb + 16 * m + 4 * hh + j;
+                const int c = 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+                const int at = 2 * (r * C + (c ^ swizzle<C>(4 * hh + j))) + (lane & 1);
+                const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(v + at));
+                const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(v + at + 2 * 8 * C));
+                const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
+                va[m][d] = u4{l.x, l.y, h.x, h.y};
+            }
+        }
+    }
+    __device__ __forceinline__ void add(f16v *acc, float &g, const f16v &w, const u4 *, int, int, int) const
+    {
+        u4 p[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t u = rows::pack2(w[2 * i], w[2 * i + 1]);
+            p[i / 4][i % 4] = u;
+            const b2 one = {(__bf16)1.0f, (__bf16)1.0f};
+            g = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, u), one, g, false);
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] = mma(va[m][d], p[m], acc[d]);
+    }
+    // channel of register i of accumulator d
+    static __device__ __forceinline__ int channel(int d, int i, int hh) { return 32 * d + 8 * (i / 4) + 4 * hh + i % 4; }
+};
+
+template <int D> struct Wave<float, D> {
+    static constexpr int C = D / 4, DT = D / 32;
+    f4 q[D / 8];
+
+    __device__ __forceinline__ void load_q(const float *p, int hh)
+    {
+#pragma unroll
+        for (int j = 0; j < C / 2; ++j) q[j] = *(const f4 *)(p + hh * (D / 2) + 4 * j);
+    }
+    __device__ __forceinline__ f16v scores(const u4 *kl, int kb, int hh, int c32) const
+    {
+        f16v x = f16v{};
+#pragma unroll
+        for (int j = 0; j < C / 2; ++j) {
+            const f4 k = __builtin_bit_cast(f4, kl[(32 * kb + c32) * C + ((hh * (C / 2) + j) ^ swizzle<C>(c32))]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i], q[j][i], x, 0, 0, 0);
+        }
+        return x;
+    }
+    __device__ __forceinline__ void read(const u4 *, int, int) {}
+    __device__ __forceinline__ void add(f16v *acc, float &g, const f16v &w, const u4 *vl, int kb, int hh, int c32) const
+    {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = 32 * kb + 8 * (i / 4) + 4 * hh + i % 4, ch = c32 * DT;
+            const float *v = (const float *)(vl + r * C + ((ch / 4) ^ swizzle<C>(r))) + ch % 4;
+            g += w[i];
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[d], w[i], acc[d], 0, 0, 0);
+        }
+    }
+    static __device__ __forceinline__ int channel(int d, int i, int hh) { return (8 * (i / 4) + 4 * hh + i % 4) * DT + d; }
+};
+
+// N neighbouring channels
+template <int N> __device__ __forceinline__ void put(float *p, const float *f)
+{
+    if constexpr (N == 4) *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
+    else if constexpr (N == 2) *(float2 *)p = make_float2(f[0], f[1]);
+    else *p = *f;
+}
+template <int N> __device__ __forceinline__ void put(bf16_t *p, const float *f)
+{
+    static_assert(N == 4, "a register quad");
+    *(uint2 *)p = make_uint2(rows::pack2(f[0], f[1]), rows::pack2(f[2], f[3]));
+}
+
+__device__ __forceinline__ bool odd_bits(bf16_t v) { return (v & 0x7f80) == 0x7f80; }
+__device__ __forceinline__ bool odd_bits(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
+
+template <typename T, int D>
 __global__ __launch_bounds__(THREADS, 2) void chunk_kernel(PagedArgs a, PagedPlan plan, float *part)
 {
     constexpr int ROWS = CHUNK_ROWS, WR = ROWS / 4;   // rows of a workgroup, of a wave
-    constexpr int C = D / 8;                       // 16-byte pieces of a row
-    constexpr int KC = D / 16, DT = D / 32;
+    using W = Wave<T, D>;
+    constexpr int C = W::C, DT = W::DT, P = 16 / sizeof(T);   // 16-byte pieces of a row, channels of a piece
+    constexpr int KB = C > 16 ? 32 : 64;           // keys of an LDS buffer: two workgroups to a CU
     constexpr int LR = 64 / C;                     // rows that a wave's load covers
     constexpr int LN = KB / LR / 4;                // loads of a wave, of keys and of values
     // two buffers
@@ -102,14 +219,14 @@ __global__ __launch_bounds__(THREADS, 2) void chunk_kernel(PagedArgs a, PagedPla
     const int lane = threadIdx.x % 64, hh = lane / 32, c32 = lane % 32;
     const Seq seq = seq_of(a, s);
     const int rows = seq.count * a.group, page_mask = (1 << a.page_shift) - 1;
-    const bf16_t *kc = (const bf16_t *)a.k + head * a.cache.head, *vc = (const bf16_t *)a.v + head * a.cache.head;
+    const T *kc = (const T *)a.k + head * a.cache.head, *vc = (const T *)a.v + head * a.cache.head;
     const int32_t *table = a.table + (size_t)s * a.table_cols;
 
     uint32_t lane_at[LN];   // bytes from a tile's first row to what the lane loads
 #pragma unroll
     for (int i = 0; i < LN; ++i) {
         const int r = (wave + 4 * i) * LR + lane / C;
-        lane_at[i] = 2 * (r % KT * (int)a.cache.token + 8 * (lane % C ^ swizzle<D>(r)));
+        lane_at[i] = (uint32_t)sizeof(T) * (r % KT * (uint32_t)a.cache.token + P * (lane % C ^ swizzle<C>(r)));
     }
 
     for (int r0 = row_tile * ROWS; r0 < rows; r0 += plan.tiles * ROWS) {
@@ -123,17 +240,14 @@ __global__ __launch_bounds__(THREADS, 2) void chunk_kernel(PagedArgs a, PagedPla
         const int row = r0 + wave * WR + c32;           // the lane's own
         const int t = min(row, rows - 1) / a.group, pos = pos0 + t;
         const int q_head = head * a.group + min(row, rows - 1) - t * a.group;
-        u4 q[KC];
+        W wv;
+        wv.load_q((const T *)a.q + (seq.t0 + t) * a.q_token + q_head * a.q_head, hh);
         f16v acc[DT];
         float g = 0.f;
-        {
-            const bf16_t *p = (const bf16_t *)a.q + (seq.t0 + t) * a.q_token + q_head * a.q_head + 8 * hh;
 #pragma unroll
-            for (int k = 0; k < KC; ++k) q[k] = *(const u4 *)(p + 16 * k);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) acc[d] = f16v{};
-        }
-        bool bad = seq.cut;
+        for (int d = 0; d < DT; ++d) acc[d] = f16v{};
+
+        bool bad = seq.cut, met_odd = false;
         // Key tiles [whole, whole_end) exist in full and every row sees all their
         // keys; elsewhere keys are clamped and weights masked.
         const int shift = sp.low - sp.sink_tiles;   // from a tile's number here to its own
@@ -165,7 +279,7 @@ __global__ __launch_bounds__(THREADS, 2) void chunk_kernel(PagedArgs a, PagedPla
                 uint32_t off = lane_at[i];
                 if (!all) {
                     const int n0 = sp.tile(min(i0 + it, end - 1)) * KT, r = l0 + lane / C;
-                    off = 2 * ((sp.read(n0 + r % KT, n0 + KT - 1) - n0) * (int)a.cache.token + 8 * (lane % C ^ swizzle<D>(r)));
+                    off = (uint32_t)sizeof(T) * ((sp.read(n0 + r % KT, n0 + KT - 1) - n0) * (uint32_t)a.cache.token + P * (lane % C ^ swizzle<C>(r)));
                 }
                 to_lds((const char *)(kc + from) + off, kd + l0 * C);
                 to_lds((const char *)(vc + from) + off, vd + l0 * C);
@@ -178,96 +292,39 @@ __global__ __launch_bounds__(THREADS, 2) void chunk_kernel(PagedArgs a, PagedPla
         const auto screen = [&](int i0, u4 *vd) {
 #pragma unroll 1
             for (int piece = threadIdx.x; piece < KB * C; piece += THREADS) {
-                const u4 y = vd[piece];
-                us2 most = {0, 0};   // largest exponent, sign shifted out
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, (uint32_t)y[j]) << 1);
-                if (most[0] < 0xff00 && most[1] < 0xff00) continue;
-                const int r = piece / C, c = piece % C ^ swizzle<D>(r);
-                bf16_t *x = (bf16_t *)&vd[piece];
+                const int r = piece / C, c = piece % C ^ swizzle<C>(r);
+                T *x = (T *)&vd[piece];
 #pragma unroll 1
-                for (int e = 0; e < 8; ++e) {
-                    const bf16_t v = x[e];
-                    if ((v & 0x7f80) != 0x7f80) continue;
+                for (int e = 0; e < P; ++e) {
+                    const T v = x[e];
+                    if (!odd_bits(v)) continue;
                     x[e] = 0;
+                    met_odd = true;
                     if (i0 + r / KT >= end) continue;
                     const int n = sp.tile(i0 + r / KT) * KT + r % KT;
 #pragma unroll 1
                     for (int i = 0; i < ROWS && r0 + i < rows; ++i) {
                         const int t = (r0 + i) / a.group;
                         if (!visible(n, pos0 + t, a.window, a.sinks)) continue;
-                        const bool nan = (v & 0x7f) != 0;
-                        bool neg = v >> 15;
+                        const bool nan = isnan(io<T>::ld(&v, 0));
+                        bool neg = io<T>::ld(&v, 0) < 0.f;
                         if (!nan && a.c2 == 0.f) {   // first order: the weight has a sign
-                            const bf16_t *qp = (const bf16_t *)a.q + (seq.t0 + t) * a.q_token +
-                                               (head * a.group + r0 + i - t * a.group) * a.q_head;
+                            const T *qp = (const T *)a.q + (seq.t0 + t) * a.q_token +
+                                          (head * a.group + r0 + i - t * a.group) * a.q_head;
                             const int page = min((unsigned)table[n >> a.page_shift], (unsigned)a.pages - 1);
-                            const bf16_t *kp = kc + page * a.cache.batch + (n & page_mask) * a.cache.token;
+                            const T *kp = kc + page * a.cache.batch + (n & page_mask) * a.cache.token;
                             float dot = 0.f;
 #pragma unroll 1
-                            for (int d = 0; d < D; ++d) dot = fmaf(bf16_to_f32(qp[d]), bf16_to_f32(kp[d]), dot);
+                            for (int d = 0; d < D; ++d) dot = fmaf(io<T>::ld(qp, d), io<T>::ld(kp, d), dot);
                             neg ^= fmaf(dot, a.c1, 1.0f) < 0.f;
                         }
-                        const int ch = 8 * c + e;
+                        const int ch = P * c + e;
                         if (nan || !neg) atomicOr(&flags[0][i][ch / 32], 1u << (ch % 32));
                         if (nan || neg) atomicOr(&flags[1][i][ch / 32], 1u << (ch % 32));
                     }
                 }
             }
             __syncthreads();
-        };
-
-        // Operands from LDS: 32 keys kb for the scores, and under the weights.
-        const auto keys_of = [&](const u4 *kl, int kb, u4 *k) {
-#pragma unroll
-            for (int i = 0; i < KC; ++i)
-                k[i] = kl[(32 * kb + c32) * C + ((2 * i + hh) ^ swizzle<D>(c32))];
-        };
-        const auto values_of = [&](const u4 *vb, int kb, u4 (&v)[2][DT]) {
-            const s4 *vl = (const s4 *)vb;
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    typedef s4 __attribute__((address_space(3))) *lp;
-                    const int j = lane >> 2 & 3, r = 32 * kb + 16 * m + 4 * hh + j;
-                    const int c = 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-                    const int at = 2 * (r * C + (c ^ swizzle<D>(4 * hh + j))) + (lane & 1);
-                    const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(vl + at));
-                    const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(vl + at + 2 * 8 * C));
-                    const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
-                    v[m][d] = u4{l.x, l.y, h.x, h.y};
-                }
-            }
-        };
-        const auto score = [&](const u4 *k) {
-            f16v x = f16v{};
-#pragma unroll
-            for (int i = 0; i < KC; ++i) x = mma(k[i], q[i], x);
-            return x;
-        };
-        // Weights from scores, rounded, and summed so.
-        const auto weigh = [&](const f16v &x, u4 (&w)[2], auto &&seen) {
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                float y[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float z = x[i + j];
-                    y[j] = seen(i + j) ? fmaf(fmaf(z, a.c2, a.c1), z, 1.0f) : 0.f;
-                }
-                const uint32_t u = rows::pack2(y[0], y[1]);
-                w[i / 8][i / 2 % 4] = u;
-                const b2 one = {(__bf16)1.0f, (__bf16)1.0f};
-                g = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, u), one, g, false);
-            }
-        };
-        const auto add = [&](const u4 (&v)[2][DT], const u4 (&w)[2]) {
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) acc[d] = mma(v[m][d], w[m], acc[d]);
         };
 
         for (int i = threadIdx.x; i < 2 * ROWS * DT; i += THREADS) (&flags[0][0][0])[i] = 0;
@@ -282,24 +339,22 @@ __global__ __launch_bounds__(THREADS, 2) void chunk_kernel(PagedArgs a, PagedPla
                 const int page = page_of(i0 + 2 * STEP);
 #pragma unroll
                 for (int kb = 0; kb < KB / 32; ++kb) {
-                    u4 ka[KC], va[2][DT], w[2];
-                    keys_of(k, kb, ka);
-                    const f16v x = score(ka);
-                    values_of(v, kb, va);
-                    if (all) {
-                        weigh(x, w, [](int) { return true; });
-                    } else {
+                    f16v x = wv.scores(k, kb, hh, c32);
+                    wv.read(v, kb, lane);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = fmaf(fmaf(x[i], a.c2, a.c1), x[i], 1.0f);
+                    if (!all) {
                         int base[2];
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             const int it = i0 + 2 * kb + i;
                             base[i] = it < end ? sp.tile(it) * KT : INT32_MAX - KT;   // past every position
                         }
-                        weigh(x, w, [&](int i) {
-                            return visible(base[i / 8] + 8 * (i / 4 % 2) + 4 * hh + i % 4, pos, a.window, a.sinks);
-                        });
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (!visible(base[i / 8] + 8 * (i / 4 % 2) + 4 * hh + i % 4, pos, a.window, a.sinks)) x[i] = 0.f;
                     }
-                    add(va, w);
+                    wv.add(acc, g, x, v, kb, hh, c32);
                 }
                 // the next keys are there, and these buffers are free
                 __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
@@ -321,6 +376,7 @@ __global__ __launch_bounds__(THREADS, 2) void chunk_kernel(PagedArgs a, PagedPla
         };
         walk(keys0, keys1, values0, values1);
         bad = __syncthreads_or(bad);
+        met_odd = __syncthreads_or(met_odd);
 
         float gs = halves_sum(g);
         if (bad) gs = __builtin_nanf("");
@@ -328,30 +384,34 @@ __global__ __launch_bounds__(THREADS, 2) void chunk_kernel(PagedArgs a, PagedPla
         const size_t o = (size_t)(seq.t0 + t) * a.Hq + q_head;
         if (row < rows) {
             if (plan.splits > 1 && hh == 0) part[(size_t)a.T * a.Hq * plan.splits * D + o * plan.splits + split] = gs;
+            if (met_odd) {
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                f16v f = acc[d];
-                const uint32_t plus = flags[0][wave * WR + c32][d], minus = flags[1][wave * WR + c32][d];
-                if (plus | minus) {
+                for (int d = 0; d < DT; ++d) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int bit = 8 * (i / 4) + 4 * hh + i % 4;
-                        if (plus >> bit & 1) f[i] += __builtin_inff();
-                        if (minus >> bit & 1) f[i] -= __builtin_inff();
+                        const int ch = W::channel(d, i, hh), fr = wave * WR + c32;
+                        if (flags[0][fr][ch / 32] >> (ch % 32) & 1) acc[d][i] += __builtin_inff();
+                        if (flags[1][fr][ch / 32] >> (ch % 32) & 1) acc[d][i] -= __builtin_inff();
                     }
                 }
+            }
+            // N neighbouring channels at a time
+            constexpr int N = sizeof(T) == 2 || DT == 4 ? 4 : DT;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int ch = 32 * d + 8 * e + 4 * hh;
-                    if (plan.splits > 1) {
-                        *(float4 *)(part + (o * plan.splits + split) * D + ch) =
-                            make_float4(f[4 * e], f[4 * e + 1], f[4 * e + 2], f[4 * e + 3]);
-                    } else {
-                        const uint32_t lo = rows::pack2(f[4 * e] * inv, f[4 * e + 1] * inv);
-                        const uint32_t hi = rows::pack2(f[4 * e + 2] * inv, f[4 * e + 3] * inv);
-                        // a row before the sequence sees no key
-                        *(uint2 *)((bf16_t *)a.out + o * D + ch) = pos < 0 ? make_uint2(0, 0) : make_uint2(lo, hi);
-                    }
+            for (int n = 0; n < 16 * DT / N; ++n) {
+                float f[N];
+                // bf16: a register quad of one accumulator; float32: a register of
+                // every accumulator
+                const int d0 = sizeof(T) == 2 ? n / 4 : 0, i0 = sizeof(T) == 2 ? n % 4 * 4 : n;
+#pragma unroll
+                for (int j = 0; j < N; ++j) f[j] = sizeof(T) == 2 ? acc[d0][i0 + j] : acc[j][i0];
+                const int ch = W::channel(d0, i0, hh);
+                if (plan.splits > 1) {
+                    put<N>(part + (o * plan.splits + split) * D + ch, f);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) f[j] = pos < 0 ? 0.f : f[j] * inv;   // pos < 0: sees no key
+                    put<N>((T *)a.out + o * D + ch, f);
                 }
             }
         }
@@ -359,24 +419,29 @@ __global__ __launch_bounds__(THREADS, 2) void chunk_kernel(PagedArgs a, PagedPla
     }
 }
 
-template <int D> hipError_t launch(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
+template <typename T, int D> hipError_t launch(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
 {
     const long long pairs = ((long long)a.S * a.Hkv + 7) / 8 * 8;
     const long long blocks = pairs * plan.tiles * plan.splits;
     if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
-    chunk_kernel<D><<<(unsigned)blocks, THREADS, 0, st>>>(a, plan, part);
+    chunk_kernel<T, D><<<(unsigned)blocks, THREADS, 0, st>>>(a, plan, part);
     return hipGetLastError();
+}
+
+template <typename T> hipError_t launch_d(const PagedArgs &a, const PagedPlan &plan, int D, float *part, hipStream_t st)
+{
+    switch (D) {
+    case 32: return launch<T, 32>(a, plan, part, st);
+    case 64: return launch<T, 64>(a, plan, part, st);
+    default: return launch<T, 128>(a, plan, part, st);
+    }
 }
 
 }  // namespace
 
-hipError_t paged_chunk(const PagedArgs &a, const PagedPlan &plan, int D, float *part, hipStream_t st)
+hipError_t paged_chunk(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, float *part, hipStream_t st)
 {
-    switch (D) {
-    case 32: return launch<32>(a, plan, part, st);
-    case 64: return launch<64>(a, plan, part, st);
-    default: return launch<128>(a, plan, part, st);
-    }
+    return is_bf16 ? launch_d<bf16_t>(a, plan, D, part, st) : launch_d<float>(a, plan, D, part, st);
 }
 
 }  // namespace fm

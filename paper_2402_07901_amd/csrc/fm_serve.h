@@ -74,6 +74,7 @@ size_t paged_workspace(const PagedPlan &plan, int T, int Hq, int D);
 hipError_t paged_fwd(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, void *ws,
                      hipStream_t st);
 constexpr int CHUNK_ROWS = 128;    // rows of a workgroup of the chunk kernel
-hipError_t paged_chunk(const PagedArgs &a, const PagedPlan &plan, int D, float *part, hipStream_t st);
+hipError_t paged_chunk(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, float *part,
+                       hipStream_t st);
 
 }  // namespace fm
