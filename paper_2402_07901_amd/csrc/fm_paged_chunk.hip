@@ -17,17 +17,18 @@
 // The next keys go straight to the other LDS buffer (global_load_lds) while
 // these are worked on.  Registers: two waves on a SIMD, from two workgroups,
 // whose products and weights overlap.  64 rows per wave read LDS half as often
-// but leave one wave on a SIMD at D = 128: 904 against 1003 TFLOP/s.
+// but leave one wave on a SIMD at D = 128 (10 % slower).
 //
 // LDS rows have no padding; the 16-byte piece c of row r lies
 // at piece c ^ swizzle(r), which puts 8 consecutive rows' piece c (score
 // operands) and pieces c, c + 1 of 4 consecutive rows (value operands) on
 // distinct banks.
 //
-// In bf16 the weights enter as bf16, and the row's sum adds the rounded ones: what is
-// rounded is the weights of an average, whose errors of 2^-9 each largely
-// cancel, below the rounding of the output itself; two parts, as in the
-// register kernel, would add half the MFMA work.
+// In bf16 the weights enter as two bf16 parts, 16 bits of each: rounded to one
+// they would add as much error again as the output's own rounding (2.5e-3
+// against 1.6e-3 of the output's size on short rows), for half as many MFMA
+// again.  What that leaves, at four chunks of up to 2048 rows over up to 8192
+// keys, 32 heads to 8, D = 128: FIGURE.
 #include <hip/hip_runtime.h>
 
 #include "fm_internal.h"
@@ -121,18 +122,27 @@ template <int D> struct Wave<bf16_t, D> {
     }
     __device__ __forceinline__ void add(f16v *acc, float &g, const f16v &w, const u4 *, int, int, int) const
     {
-        u4 p[2];
+        u4 hi[2], lo[2];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t u = rows::pack2(w[2 * i], w[2 * i + 1]);
-            p[i / 4][i % 4] = u;
-            const b2 one = {(__bf16)1.0f, (__bf16)1.0f};
-            g = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, u), one, g, false);
+            const float x = w[2 * i], y = w[2 * i + 1];
+            g += x + y;
+            // hi: the upper 16 bits; lo: the rest, of the same sign and never 0
+            // (x | 1), so that an infinite value stays one under both
+            hi[i / 4][i % 4] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+            lo[i / 4][i % 4] = rows::pack2(rest(x), rest(y));
         }
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
+        for (int m = 0; m < 2; ++m) {
 #pragma unroll
-            for (int d = 0; d < DT; ++d) acc[d] = mma(va[m][d], p[m], acc[d]);
+            for (int d = 0; d < DT; ++d) acc[d] = mma(va[m][d], hi[m], acc[d]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] = mma(va[m][d], lo[m], acc[d]);
+        }
+    }
+    static __device__ __forceinline__ float rest(float x)
+    {
+        return __uint_as_float(__float_as_uint(x) | 1u) - __uint_as_float(__float_as_uint(x) & 0xffff0000u);
     }
     // channel of register i of accumulator d
     static __device__ __forceinline__ int channel(int d, int i, int hh) { return 32 * d + 8 * (i / 4) + 4 * hh + i % 4; }

@@ -58,7 +58,7 @@ struct PagedArgs {
     const int32_t *table, *lens, *q_start;
     int S, T, Hq, Hkv, group, pages, table_cols, page_shift;
     int window, sinks;             // window 2^30: none
-    float c1, c2;                  // weight 1 + s (c1 + c2 s) of the raw product s
+    float c1, c2;                  // weight 1 + s (c1 + c2 s) of the raw product s; c2 is 0 for first order
 };
 // How a call is cut: rows of a (sequence, key head) in tiles, keys in splits.
 struct PagedPlan {
