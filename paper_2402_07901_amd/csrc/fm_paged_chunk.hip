@@ -200,7 +200,7 @@ __device__ __forceinline__ bool odd_bits(bf16_t v) { return (v & 0x7f80) == 0x7f
 __device__ __forceinline__ bool odd_bits(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
 
 template <typename T, int D>
-__global__ __launch_bounds__(THREADS, 2) void chunk_kernel(PagedArgs a, PagedPlan plan, float *part)
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 64 ? 3 : 2) void chunk_kernel(PagedArgs a, PagedPlan plan, float *part)
 {
     constexpr int ROWS = CHUNK_ROWS, WR = ROWS / 4;   // rows of a workgroup, of a wave
     using W = Wave<T, D>;
@@ -354,15 +354,18 @@ __global__ __launch_bounds__(THREADS, 2) void chunk_kernel(PagedArgs a, PagedPla
 #pragma unroll
                     for (int i = 0; i < 16; ++i) x[i] = fmaf(fmaf(x[i], a.c2, a.c1), x[i], 1.0f);
                     if (!all) {
-                        int base[2];
+                        // key n0 + e of a tile is seen if e <= lim and (e > lim - window
+                        // or it is a first token)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int it = i0 + 2 * kb + i;
-                            base[i] = it < end ? sp.tile(it) * KT : INT32_MAX - KT;   // past every position
+                        for (int j = 0; j < 2; ++j) {
+                            const int it = i0 + 2 * kb + j, n0 = sp.tile(min(it, end - 1)) * KT + 4 * hh;
+                            const int lim = it < end ? max(pos, -1) - n0 : -1, low = lim - a.window, sinks = a.sinks - n0;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const int e = 8 * (i / 4) + i % 4;
+                                if (e > lim || (e <= low && e >= sinks)) x[8 * j + i] = 0.f;
+                            }
                         }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (!visible(base[i / 8] + 8 * (i / 4 % 2) + 4 * hh + i % 4, pos, a.window, a.sinks)) x[i] = 0.f;
                     }
                     wv.add(acc, g, x, v, kb, hh, c32);
                 }
