@@ -429,6 +429,8 @@ int fastmax_cache_append(const void *q, const void *k, const void *v,
  *              size the grid; larger true values cost time, not correctness.
  *   out      : [T, Hq, D] contiguous
  *   workspace: fastmax_paged_workspace_bytes with the same sizes
+ * Weights are float32, in bf16 as two bf16 parts; sums are float32 and must fit
+ * it (sum w |v| < 3e38).
  * A row that sees no key (lens[s] smaller than its new tokens) is 0.  What
  * lies in slots that no row of a sequence sees is not used, whatever it
  * holds; entries of the page table past lens[s] or behind the window are not

@@ -506,6 +506,18 @@ def _on_gpu(q, dims, what):
         raise ValueError("q's channels must be contiguous")
 
 
+def _owner(stream, device):
+    """Context in which what a call allocates belongs to the stream it runs on:
+    memory that another stream still uses is not handed to it, nor its own to
+    others while it runs."""
+    if stream is None:
+        return _HERE_ALREADY
+    import torch
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    return torch.cuda.stream(stream)
+
+
 def fastmax_rope_fwd(q, k, v, pos, cos, sin, wq=None, wk=None, eps=1e-6, sections=None,
                      interleaved=False, out=None, stream=None):
     """A projection's rows q [B, N, Hq, D], k and v [B, N, Hkv, D] (strided
@@ -523,7 +535,9 @@ def fastmax_rope_fwd(q, k, v, pos, cos, sin, wq=None, wk=None, eps=1e-6, section
     dt = _dtype_code(q)
     rope = _rope_of(q, (B, N), pos, cos, sin, wq, wk, eps, sections, interleaved)
     if out is None:
-        out = tuple(torch.empty((B, Hq, N, D), dtype=q.dtype, device=q.device) for _ in range(3))
+        with _owner(stream, q.device):
+            out = tuple(torch.empty((B, Hq, N, D), dtype=q.dtype, device=q.device)
+                        for _ in range(3))
     else:
         for name, t in zip(("out[0]", "out[1]", "out[2]"), out):
             _whole(name, t, q.dtype, q, (B, Hq, N, D))
@@ -558,16 +572,18 @@ def fastmax_rope_bwd(q, k, gq, gk, gv, pos, cos, sin, wq=None, wk=None, eps=1e-6
     dt = _dtype_code(q)
     rope = _rope_of(q, (B, N), pos, cos, sin, wq, wk, eps, sections, interleaved)
     if out is None:
-        out = tuple(torch.empty((B, N, h, D), dtype=q.dtype, device=q.device)
-                    for h in (Hq, Hkv, Hkv))
+        with _owner(stream, q.device):
+            out = tuple(torch.empty((B, N, h, D), dtype=q.dtype, device=q.device)
+                        for h in (Hq, Hkv, Hkv))
     else:
         for name, t, h in zip(("out[0]", "out[1]", "out[2]"), out, (Hq, Hkv, Hkv)):
             _rows_of(name, t, q, (B, N, h, D))
     dwq = dwk = None
-    if wq is not None:
-        dwq, dwk = torch.empty((2, D), dtype=torch.float32, device=q.device).unbind(0)
-    if workspace is None:
-        workspace = _alloc_ws(rope_workspace_bytes(B, N, Hq, Hkv, D, wq is not None), q.device)
+    with _owner(stream, q.device):
+        if wq is not None:
+            dwq, dwk = torch.empty((2, D), dtype=torch.float32, device=q.device).unbind(0)
+        if workspace is None:
+            workspace = _alloc_ws(rope_workspace_bytes(B, N, Hq, Hkv, D, wq is not None), q.device)
     ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
     with _on(q.device):
         rc = lib().fastmax_rope_bwd(q.data_ptr(), k.data_ptr(), _S2(_stride4(q), _stride4(k)),
@@ -611,7 +627,8 @@ def fastmax_cache_append(q, k, v, k_cache, v_cache, slots, pos, cos, sin, wq=Non
     dt = _dtype_code(q)
     rope = _rope_of(q, (T,), pos, cos, sin, wq, wk, eps, sections, interleaved)
     if q_out is None:
-        q_out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+        with _owner(stream, q.device):
+            q_out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
     else:
         _whole("q_out", q_out, q.dtype, q, (T, Hq, D))
     with _on(q.device):
@@ -657,13 +674,14 @@ def fastmax_paged_fwd(q, k_cache, v_cache, table, lens, q_start=None, max_q=None
         max_q = 1 if q_start is None else T
     if max_len is None:
         max_len = cols * page
-    if out is None:
-        out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
-    else:
+    if out is not None:
         _whole("out", out, q.dtype, q, (T, Hq, D))
-    if workspace is None:
-        workspace = _alloc_ws(paged_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window,
-                                                    sinks, dt), q.device)
+    with _owner(stream, q.device):
+        if out is None:
+            out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+        if workspace is None:
+            workspace = _alloc_ws(paged_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window,
+                                                        sinks, dt), q.device)
     ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
     with _on(q.device):
         rc = lib().fastmax_paged_fwd(q.data_ptr(), _S1(*_stride3(q)), k_cache.data_ptr(),

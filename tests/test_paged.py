@@ -340,3 +340,72 @@ def test_agrees_with_the_attention_itself():
                                         torch.tensor([i + 1], dtype=torch.int32, device="cuda")))
     got = torch.cat(got)
     assert (got - want).abs().max() <= 1e-4 * want.abs().max()   # float32 tolerance
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("size", [1e-30, 1e-6, 1e6, 1e25])
+def test_values_of_any_size(D, size):
+    """bf16 and float32 values far from 1, some a million times the others: the
+    sums keep them (nothing shares a scale) while sum w |v|, up to 1e10 times
+    ``size`` here, is a float32 number."""
+    import torch
+    for dtype in ("bf16", "f32"):
+        c = Cache([200, 90], [70, 1], 4, 2, D, 32, dtype, seed=3)
+        for s, n in enumerate(c.lens_h):
+            grow = torch.ones(n, 1, D, device="cuda")
+            grow[::7, :, ::3] = 2.0 ** 20
+            idx = torch.arange(n, device="cuda")
+            pg = c.table[s].long()[idx // 32]
+            v = (torch.from_numpy(c.v_h[s]).cuda().float() * grow * size).to(c.v.dtype)
+            c.v[pg, :, idx % 32] = v
+            c.v_h[s] = su.np64(v)
+        c.check(c.run(max_q=70), (D, size, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_any_size(dtype):
+    """q^ and k^ are taken as they are: large ones, whose weights reach 1e12,
+    small ones, whose weights are 1."""
+    import torch
+    for size in (1e3, 1e-20):
+        for starts in (True, False):
+            news = [60, 1, 33] if starts else [1, 1, 1]
+            c = Cache([100, 40, 33], news, 4, 2, 64, 16, dtype, seed=4)
+            c.q = (c.q.float() * size).to(c.q.dtype)
+            c.check(c.run(starts=starts, max_q=60 if starts else 1), (size, starts), starts=starts)
+
+
+def test_infinities_in_every_channel_of_one_token():
+    """A whole token of infinities (and one of NaN) behind rows that see it and
+    rows that do not, in chunks and single tokens."""
+    import torch
+    for D in (16, 64, 128):
+        c = Cache([130], [130], 2, 1, D, 64, "bf16")
+        page = int(c.table_h[0, 1])
+        c.v[page, 0, 6] = float("-inf")          # token 70
+        out = c.run(max_q=130)
+        assert torch.isfinite(out[:70]).all()
+        assert (out[70:] == float("-inf")).all()
+        c.v[page, 0, 8] = float("nan")           # token 72
+        out = c.run(max_q=130)
+        assert (out[70:72] == float("-inf")).all() and torch.isnan(out[72:]).all()
+        one = fm.fastmax_paged_fwd(c.q[:1], c.k, c.v, c.table,
+                                   torch.tensor([72], dtype=torch.int32, device="cuda"))
+        assert (one == float("-inf")).all()
+
+
+def test_allocations_belong_to_the_stream():
+    """Calls on a stream given as an object or as a handle, with the binding's
+    own outputs and workspaces, while the current stream reuses memory."""
+    import torch
+    c = Cache([3000, 500], [1, 1], 8, 2, 64, 64, "bf16")
+    want = c.run(starts=False)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = []
+    for i in range(8):
+        got.append(c.run(starts=False, stream=side if i % 2 else side.cuda_stream))
+        torch.empty(1 << 20, device="cuda").fill_(float("nan"))
+    torch.cuda.synchronize()
+    for g in got:
+        assert torch.equal(g, want)
