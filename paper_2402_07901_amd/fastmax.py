@@ -89,7 +89,7 @@ def lib():
         L.fastmax_fwd_noalloc.restype = i
         L.fastmax_set_scan_segments.argtypes = [i]
         L.fastmax_set_scan_segments.restype = i
-        st, rope = ctypes.POINTER(Strides), ctypes.POINTER(Rope)
+        st, rope = vp, ctypes.POINTER(Rope)     # fastmax_strides_t arrays, NULL: contiguous
         L.fastmax_rope_fwd.argtypes = [vp, vp, vp, st, vp, vp, vp, i, i, i, i, i, rope, i, vp]
         L.fastmax_rope_fwd.restype = i
         L.fastmax_rope_workspace_bytes.argtypes = [i, i, i, i, i, i]
@@ -418,82 +418,81 @@ def fastmax_bwd_dropout(q, k, v, out, dout, g, bits, rate, causal=False, scale=N
 # Around the attention: norm and rotation of a projection's rows, shared heads,
 # a paged cache and the attention of new tokens over it.
 # ---------------------------------------------------------------------------
-# The usual arguments pass one comparison each; what is wrong is found out after.
-def _rows_of(name, t, like, shape):
-    """Checks token rows: ``like``'s dtype and device, the given shape, D
-    contiguous (the library checks the other strides)."""
-    if (t.shape == shape and t.dtype == like.dtype and t.get_device() == like.get_device()
-            and t.stride(-1) == 1):
-        return
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype != like.dtype:
-        raise ValueError(f"{name} must be {like.dtype}, got {t.dtype}")
-    if t.device != like.device:
-        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
-    raise ValueError(f"{name}'s channels must be contiguous")
+# These calls may take less time on the GPU than on the host, so the usual
+# arguments pass one comparison each and what is wrong is found out after; a
+# tensor's dtype and device index (``dev``) are asked for once.
+_t = None   # torch, once a call has brought tensors
 
 
-def _whole(name, t, dtype, like, shape):
-    """Checks a contiguous tensor of a given dtype and shape on ``like``'s device."""
-    if (t.shape == shape and t.dtype == dtype and t.get_device() == like.get_device()
-            and t.is_contiguous()):
-        return
+def _torch():
+    global _t
+    if _t is None:
+        import torch
+        _t = torch
+    return _t
+
+
+def _wrong(name, t, shape, dtype, q):
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.device != like.device:
-        raise ValueError(f"{name} is on {t.device}, not on {like.device}")
-    raise ValueError(f"{name} must be contiguous")
+    if t.device != q.device:
+        raise ValueError(f"{name} is on {t.device}, not on {q.device}")
 
 
-_S1, _S2, _S3 = Strides, Strides * 2, Strides * 3
+def _rows_of(name, t, shape, dtype, dev, q):
+    """Checks token rows: dtype, q's device, the given shape, D contiguous (the
+    library checks the other strides)."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or t.stride(-1) != 1:
+        _wrong(name, t, shape, dtype, q)
+        raise ValueError(f"{name}'s channels must be contiguous")
 
 
-def _stride4(t):
-    st = t.stride()
-    return st[0], st[1], st[2]
+def _whole(name, t, shape, dtype, dev, q):
+    """Checks a contiguous tensor of a given dtype and shape on q's device."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
+        _wrong(name, t, shape, dtype, q)
+        raise ValueError(f"{name} must be contiguous")
 
 
-def _stride3(t):
-    st = t.stride()
-    return 0, st[0], st[1]
+_LL3, _LL6, _LL9 = (ctypes.c_longlong * n for n in (3, 6, 9))   # one, two, three strides
 
 
 def _rope_of(q, tokens, pos, cos, sin, wq, wk, eps, sections, interleaved):
     """The fastmax_rope_t of a call whose rows are q's; ``tokens``: q's
     leading sizes."""
-    import torch
+    torch, dev = _torch(), q.get_device()
     p = c = s = gq = gk = None
     rows = rot = 0
-    axes = 1
+    axes, parts = 1, ()
     if (cos is None) != (sin is None) or (cos is None) != (pos is None):
         raise ValueError("pos, cos and sin go together")
     if cos is not None:
-        if cos.dim() != 2:
-            raise ValueError(f"cos must be [rows, rot / 2], got shape {tuple(cos.shape)}")
-        _whole("cos", cos, torch.float32, q, cos.shape)
-        _whole("sin", sin, torch.float32, q, cos.shape)
+        shape = cos.shape
+        if len(shape) != 2:
+            raise ValueError(f"cos must be [rows, rot / 2], got shape {tuple(shape)}")
+        _whole("cos", cos, shape, torch.float32, dev, q)
+        _whole("sin", sin, shape, torch.float32, dev, q)
         if pos.dim() > len(tokens):
             axes = pos.shape[-1]
-            _whole("pos", pos, torch.int32, q, (*tokens, axes))
-        else:
-            _whole("pos", pos, torch.int32, q, tokens)
-        if not 1 <= axes <= 4:
-            raise ValueError(f"1 to 4 axes of positions, got {axes}")
-        if axes > 1 and (sections is None or len(sections) != axes):
-            raise ValueError(f"{axes} axes of positions need as many sections")
+            tokens = (*tokens, axes)
+        _whole("pos", pos, tokens, torch.int32, dev, q)
+        if axes != 1:
+            if not 1 <= axes <= 4:
+                raise ValueError(f"1 to 4 axes of positions, got {axes}")
+            if sections is None or len(sections) != axes:
+                raise ValueError(f"{axes} axes of positions need as many sections")
+            parts = tuple(sections)
         p, c, s = pos.data_ptr(), cos.data_ptr(), sin.data_ptr()
-        rows, rot = cos.shape[0], 2 * cos.shape[1]
-    if (wq is None) != (wk is None):
-        raise ValueError("wq and wk go together")
-    if wq is not None:
+        rows, rot = shape[0], 2 * shape[1]
+    if wq is not None and wk is not None:
         D = q.shape[-1:]
-        _whole("wq", wq, torch.float32, q, D)
-        _whole("wk", wk, torch.float32, q, D)
+        _whole("wq", wq, D, torch.float32, dev, q)
+        _whole("wk", wk, D, torch.float32, dev, q)
         gq, gk = wq.data_ptr(), wk.data_ptr()
-    parts = tuple(sections) if axes > 1 else ()
+    elif wq is not wk:
+        raise ValueError("wq and wk go together")
     return Rope(c, s, p, rows, rot, axes, parts, 1 if interleaved else 0, gq, gk, eps)
 
 
@@ -506,16 +505,42 @@ def _on_gpu(q, dims, what):
         raise ValueError("q's channels must be contiguous")
 
 
+@contextlib.contextmanager
 def _owner(stream, device):
     """Context in which what a call allocates belongs to the stream it runs on:
     memory that another stream still uses is not handed to it, nor its own to
     others while it runs."""
-    if stream is None:
-        return _HERE_ALREADY
-    import torch
+    torch = _torch()
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(stream, device=device)
-    return torch.cuda.stream(stream)
+    with torch.cuda.stream(stream):
+        yield
+
+
+def _new(q, shapes, stream, dtype=None):
+    """Uninitialised tensors like q (of ``dtype``) for a call on ``stream``; a
+    shape None gives None."""
+    if stream is None:
+        return [x if x is None else q.new_empty(x, dtype=dtype) for x in shapes]
+    with _owner(stream, q.device):
+        return [x if x is None else q.new_empty(x, dtype=dtype) for x in shapes]
+
+
+def _scratch(q, nbytes, stream):
+    return _new(q, [(nbytes,)], stream, _torch().uint8)[0] if nbytes else None
+
+
+def _run(what, fn, dev, stream, *args):
+    """fn(*args, stream) on device ``dev``, the stream None meaning its current one."""
+    torch = _torch()
+    handle = torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+    if dev == torch.cuda.current_device():
+        rc = fn(*args, handle)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, handle)
+    if rc != OK:
+        raise FastmaxError(rc, what)
 
 
 def fastmax_rope_fwd(q, k, v, pos, cos, sin, wq=None, wk=None, eps=1e-6, sections=None,
@@ -526,28 +551,23 @@ def fastmax_rope_fwd(q, k, v, pos, cos, sin, wq=None, wk=None, eps=1e-6, section
     int32 [B, N] or [B, N, axes] with ``sections`` pairs per axis; all None: no
     rotation), key and value heads repeated.  Returns three contiguous
     [B, Hq, N, D] tensors (``out``: the same, the caller's)."""
-    import torch
     _on_gpu(q, 4, "[B, N, Hq, D]")
     B, N, Hq, D = q.shape
+    dtype, dev, dt = q.dtype, q.get_device(), _dtype_code(q)
     Hkv = k.shape[2] if k.dim() == 4 else 0
-    _rows_of("k", k, q, (B, N, Hkv, D))
-    _rows_of("v", v, q, (B, N, Hkv, D))
-    dt = _dtype_code(q)
+    rows, heads = (B, N, Hkv, D), (B, Hq, N, D)
+    _rows_of("k", k, rows, dtype, dev, q)
+    _rows_of("v", v, rows, dtype, dev, q)
     rope = _rope_of(q, (B, N), pos, cos, sin, wq, wk, eps, sections, interleaved)
     if out is None:
-        with _owner(stream, q.device):
-            out = tuple(torch.empty((B, Hq, N, D), dtype=q.dtype, device=q.device)
-                        for _ in range(3))
+        out = _new(q, (heads,) * 3, stream)
     else:
         for name, t in zip(("out[0]", "out[1]", "out[2]"), out):
-            _whole(name, t, q.dtype, q, (B, Hq, N, D))
-    with _on(q.device):
-        rc = lib().fastmax_rope_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                    _S3(_stride4(q), _stride4(k), _stride4(v)),
-                                    out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), B, N,
-                                    Hq, Hkv, D, rope, dt, _stream(_stream_of(stream, q.device)))
-    if rc != OK:
-        raise FastmaxError(rc, "fastmax_rope_fwd")
+            _whole(name, t, heads, dtype, dev, q)
+    _run("fastmax_rope_fwd", lib().fastmax_rope_fwd, dev, stream,
+         q.data_ptr(), k.data_ptr(), v.data_ptr(),
+         _LL9(*q.stride()[:3], *k.stride()[:3], *v.stride()[:3]),
+         out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), B, N, Hq, Hkv, D, rope, dt)
     return tuple(out)
 
 
@@ -562,52 +582,50 @@ def fastmax_rope_bwd(q, k, gq, gk, gv, pos, cos, sin, wq=None, wk=None, eps=1e-6
     norm only).  Returns (dq, dk, dv, dwq, dwk), dq [B, N, Hq, D], dk and dv
     [B, N, Hkv, D] (``out``: these three, the caller's, strided as they like),
     dwq and dwk float32 [D] (None without a norm)."""
-    import torch
     _on_gpu(q, 4, "[B, N, Hq, D]")
     B, N, Hq, D = q.shape
+    dtype, dev, dt = q.dtype, q.get_device(), _dtype_code(q)
     Hkv = k.shape[2] if k.dim() == 4 else 0
-    _rows_of("k", k, q, (B, N, Hkv, D))
-    for name, t in (("gq", gq), ("gk", gk), ("gv", gv)):
-        _whole(name, t, q.dtype, q, (B, Hq, N, D))
-    dt = _dtype_code(q)
+    rows, heads = (B, N, Hkv, D), (B, Hq, N, D)
+    _rows_of("k", k, rows, dtype, dev, q)
+    _whole("gq", gq, heads, dtype, dev, q)
+    _whole("gk", gk, heads, dtype, dev, q)
+    _whole("gv", gv, heads, dtype, dev, q)
     rope = _rope_of(q, (B, N), pos, cos, sin, wq, wk, eps, sections, interleaved)
     if out is None:
-        with _owner(stream, q.device):
-            out = tuple(torch.empty((B, N, h, D), dtype=q.dtype, device=q.device)
-                        for h in (Hq, Hkv, Hkv))
+        out = _new(q, ((B, N, Hq, D), rows, rows), stream)
     else:
-        for name, t, h in zip(("out[0]", "out[1]", "out[2]"), out, (Hq, Hkv, Hkv)):
-            _rows_of(name, t, q, (B, N, h, D))
+        for name, t, shape in zip(("out[0]", "out[1]", "out[2]"), out, (q.shape, rows, rows)):
+            _rows_of(name, t, shape, dtype, dev, q)
     dwq = dwk = None
-    with _owner(stream, q.device):
-        if wq is not None:
-            dwq, dwk = torch.empty((2, D), dtype=torch.float32, device=q.device).unbind(0)
-        if workspace is None:
-            workspace = _alloc_ws(rope_workspace_bytes(B, N, Hq, Hkv, D, wq is not None), q.device)
+    if wq is not None:
+        dwq, dwk = _new(q, ((D,), (D,)), stream, wq.dtype)
+    if workspace is None:
+        workspace = _scratch(q, rope_workspace_bytes(B, N, Hq, Hkv, D, wq is not None), stream)
     ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    with _on(q.device):
-        rc = lib().fastmax_rope_bwd(q.data_ptr(), k.data_ptr(), _S2(_stride4(q), _stride4(k)),
-                                    gq.data_ptr(), gk.data_ptr(), gv.data_ptr(), out[0].data_ptr(),
-                                    out[1].data_ptr(), out[2].data_ptr(), _S3(*map(_stride4, out)),
-                                    _ptr(dwq), _ptr(dwk), B, N, Hq, Hkv, D, rope, dt,
-                                    _ptr(workspace), ws_n, _stream(_stream_of(stream, q.device)))
-    if rc != OK:
-        raise FastmaxError(rc, "fastmax_rope_bwd")
+    _run("fastmax_rope_bwd", lib().fastmax_rope_bwd, dev, stream,
+         q.data_ptr(), k.data_ptr(), _LL6(*q.stride()[:3], *k.stride()[:3]),
+         gq.data_ptr(), gk.data_ptr(), gv.data_ptr(),
+         out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(),
+         _LL9(*(n for t in out for n in t.stride()[:3])),
+         _ptr(dwq), _ptr(dwk), B, N, Hq, Hkv, D, rope, dt, _ptr(workspace), ws_n)
     return (*out, dwq, dwk)
 
 
 def _cache_of(q, k_cache, v_cache, Hkv):
     """(pages, page size, strides) of the caches [pages, Hkv, page, D]."""
-    if k_cache.dim() != 4:
-        raise ValueError(f"k_cache must be [pages, Hkv, page, D], got shape {tuple(k_cache.shape)}")
-    pages, _, page, _ = k_cache.shape
-    _rows_of("k_cache", k_cache, q, (pages, Hkv, page, q.shape[-1]))
-    _rows_of("v_cache", v_cache, q, k_cache.shape)
-    if v_cache.stride() != k_cache.stride():
-        raise ValueError(f"k_cache and v_cache must have the same strides, got "
-                         f"{k_cache.stride()} and {v_cache.stride()}")
+    shape = k_cache.shape
+    if len(shape) != 4:
+        raise ValueError(f"k_cache must be [pages, Hkv, page, D], got shape {tuple(shape)}")
+    pages, _, page, _ = shape
+    dtype, dev = q.dtype, q.get_device()
+    _rows_of("k_cache", k_cache, (pages, Hkv, page, q.shape[-1]), dtype, dev, q)
+    _rows_of("v_cache", v_cache, shape, dtype, dev, q)
     st = k_cache.stride()
-    return pages, page, Strides(st[0], st[2], st[1])
+    if v_cache.stride() != st:
+        raise ValueError(f"k_cache and v_cache must have the same strides, got {st} and "
+                         f"{v_cache.stride()}")
+    return pages, page, _LL3(st[0], st[2], st[1])
 
 
 def fastmax_cache_append(q, k, v, k_cache, v_cache, slots, pos, cos, sin, wq=None, wk=None,
@@ -616,30 +634,24 @@ def fastmax_cache_append(q, k, v, k_cache, v_cache, slots, pos, cos, sin, wq=Non
     contiguous): norm and rotation as in fastmax_rope_fwd, then the attention's
     standardisation.  k^ and v go to the slots (int64 [T], page * page size +
     place; -1: none) of the caches [pages, Hkv, page, D]; returns q^ [T, Hq, D]."""
-    import torch
     _on_gpu(q, 3, "[T, Hq, D]")
     T, Hq, D = q.shape
+    dtype, dev, dt = q.dtype, q.get_device(), _dtype_code(q)
     Hkv = k.shape[1] if k.dim() == 3 else 0
-    _rows_of("k", k, q, (T, Hkv, D))
-    _rows_of("v", v, q, (T, Hkv, D))
+    _rows_of("k", k, (T, Hkv, D), dtype, dev, q)
+    _rows_of("v", v, (T, Hkv, D), dtype, dev, q)
     pages, page, cache = _cache_of(q, k_cache, v_cache, Hkv)
-    _whole("slots", slots, torch.int64, q, (T,))
-    dt = _dtype_code(q)
+    _whole("slots", slots, (T,), _torch().int64, dev, q)
     rope = _rope_of(q, (T,), pos, cos, sin, wq, wk, eps, sections, interleaved)
     if q_out is None:
-        with _owner(stream, q.device):
-            q_out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+        q_out, = _new(q, ((T, Hq, D),), stream)
     else:
-        _whole("q_out", q_out, q.dtype, q, (T, Hq, D))
-    with _on(q.device):
-        rc = lib().fastmax_cache_append(q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                        _S3(_stride3(q), _stride3(k), _stride3(v)),
-                                        q_out.data_ptr(), k_cache.data_ptr(),
-                                        v_cache.data_ptr(), cache, slots.data_ptr(), T, Hq, Hkv, D,
-                                        pages, page, rope, dt,
-                                        _stream(_stream_of(stream, q.device)))
-    if rc != OK:
-        raise FastmaxError(rc, "fastmax_cache_append")
+        _whole("q_out", q_out, (T, Hq, D), dtype, dev, q)
+    _run("fastmax_cache_append", lib().fastmax_cache_append, dev, stream,
+         q.data_ptr(), k.data_ptr(), v.data_ptr(),
+         _LL9(0, *q.stride()[:2], 0, *k.stride()[:2], 0, *v.stride()[:2]),
+         q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), cache, slots.data_ptr(),
+         T, Hq, Hkv, D, pages, page, rope, dt)
     return q_out
 
 
@@ -657,39 +669,34 @@ def fastmax_paged_fwd(q, k_cache, v_cache, table, lens, q_start=None, max_q=None
     rows and the most tokens of a sequence (None: T, or what the table holds).
     window > 0: the last ``window`` keys and the first ``sinks`` only.  Returns
     O [T, Hq, D]."""
-    import torch
     _on_gpu(q, 3, "[T, Hq, D]")
     T, Hq, D = q.shape
+    dtype, dev, dt = q.dtype, q.get_device(), _dtype_code(q)
     Hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
     pages, page, cache = _cache_of(q, k_cache, v_cache, Hkv)
     if table.dim() != 2:
         raise ValueError(f"table must be [S, cols], got shape {tuple(table.shape)}")
     S, cols = table.shape
-    _whole("table", table, torch.int32, q, table.shape)
-    _whole("lens", lens, torch.int32, q, (S,))
+    int32 = _torch().int32
+    _whole("table", table, (S, cols), int32, dev, q)
+    _whole("lens", lens, (S,), int32, dev, q)
     if q_start is not None:
-        _whole("q_start", q_start, torch.int32, q, (S + 1,))
-    dt = _dtype_code(q)
+        _whole("q_start", q_start, (S + 1,), int32, dev, q)
     if max_q is None:
         max_q = 1 if q_start is None else T
     if max_len is None:
         max_len = cols * page
-    if out is not None:
-        _whole("out", out, q.dtype, q, (T, Hq, D))
-    with _owner(stream, q.device):
-        if out is None:
-            out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
-        if workspace is None:
-            workspace = _alloc_ws(paged_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window,
-                                                        sinks, dt), q.device)
+    if out is None:
+        out, = _new(q, ((T, Hq, D),), stream)
+    else:
+        _whole("out", out, (T, Hq, D), dtype, dev, q)
+    if workspace is None:
+        workspace = _scratch(q, paged_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window,
+                                                      sinks, dt), stream)
     ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    with _on(q.device):
-        rc = lib().fastmax_paged_fwd(q.data_ptr(), _S1(*_stride3(q)), k_cache.data_ptr(),
-                                     v_cache.data_ptr(), cache, table.data_ptr(), lens.data_ptr(),
-                                     _ptr(q_start), out.data_ptr(), S, T, Hq, Hkv, D, pages, page,
-                                     cols, max_q, max_len, p, 1.0 if scale is None else scale,
-                                     window, sinks, dt, _ptr(workspace), ws_n,
-                                     _stream(_stream_of(stream, q.device)))
-    if rc != OK:
-        raise FastmaxError(rc, "fastmax_paged_fwd")
+    _run("fastmax_paged_fwd", lib().fastmax_paged_fwd, dev, stream,
+         q.data_ptr(), _LL3(0, *q.stride()[:2]), k_cache.data_ptr(), v_cache.data_ptr(), cache,
+         table.data_ptr(), lens.data_ptr(), _ptr(q_start), out.data_ptr(), S, T, Hq, Hkv, D, pages,
+         page, cols, max_q, max_len, p, 1.0 if scale is None else scale, window, sinks, dt,
+         _ptr(workspace), ws_n)
     return out
