@@ -72,6 +72,22 @@ template <int D> struct Mat<bf16_t, D> {
         }
         return s;
     }
+    // A lane's part of a score (added over the rows of lanes).
+    static __device__ __forceinline__ float dot(const bf16_t *p, int h, const Q &q)
+    {
+        u4 k[QW];
+        ld_row(p, h, k);
+        float s = 0.f;
+#pragma unroll
+        for (int c = 0; c < QW; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t a = k[c][i], b = q.x[c][i];
+                s = fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16), s);
+                s = fmaf(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u), s);
+            }
+        return s;
+    }
     // key i of the lane's eight: tile i / 4, key 4 h + i % 4
     static __device__ __forceinline__ void ld_v(const bf16_t *p, int r16, uint32_t *x)
     {
@@ -153,6 +169,17 @@ template <int D> struct Mat<float, D> {
                 s = __builtin_amdgcn_mfma_f32_16x16x4f32(k.x[c][i], q.x[c][i], s, 0, 0, 0);
         return s;
     }
+    static __device__ __forceinline__ float dot(const float *p, int h, const Q &q)
+    {
+        f4 k[QW];
+        ld_row(p, h, k);
+        float s = 0.f;
+#pragma unroll
+        for (int c = 0; c < QW; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s = fmaf(k[c][i], q.x[c][i], s);
+        return s;
+    }
     static __device__ __forceinline__ void ld_v(const float *p, int r16, float *x)
     {
         p += r16 * VW;
@@ -192,7 +219,7 @@ template <int D> struct Mat<float, D> {
 // MULTI: rows of several tokens may share a tile, so a key can be visible to
 // some rows of a tile and not to others.
 template <typename T, int D, int RT, bool MULTI>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && RT == 1 ? 3 : 1) void paged_kernel(PagedArgs a, PagedPlan plan, float *part)
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 128 && RT == 1 ? 3 : 1) void paged_kernel(PagedArgs a, PagedPlan plan, float *part)
 {
     using M = Mat<T, D>;
     constexpr int VW = M::VW, ROWS = 16 * RT, RS = D + 4;
@@ -305,19 +332,20 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && RT == 1 ? 3 : 1) void pa
                         continue;
                     }
                     // each row adds the keys it sees, one by one
+#pragma unroll 1
+                    for (int i = 0; i < 2 * KT; ++i) {
+                        const int key = (i < KT ? base[0] : base[1]) + i % KT;
+                        if (key >= sp.end) continue;
+                        const int pg = table[key >> a.page_shift];
+                        if ((unsigned)pg >= (unsigned)a.pages) continue;
+                        const long long from = pg * a.cache.batch + (key & page_mask) * a.cache.token;
+                        const float x = rows4_sum(M::dot(kc + from, h, q[r]));
+                        if (!visible(key, pos[r], a.window, a.sinks)) continue;
+                        const float wk = fmaf(fmaf(x, a.c2, a.c1), x, 1.0f);
+                        const T *vp = vc + from + h * (D / 4);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        for (int hh = 0; hh < 4; ++hh) {
-                            const float wk = __shfl(w[i / 4][i % 4], 16 * hh + r16);
-                            const int key = base[i / 4] + 4 * hh + i % 4;
-                            if (!visible(key, pos[r], a.window, a.sinks)) continue;
-                            const int pg = table[key >> a.page_shift];
-                            if ((unsigned)pg >= (unsigned)a.pages) continue;
-                            const T *vp = vc + pg * a.cache.batch + (key & page_mask) * a.cache.token + h * (D / 4);
-#pragma unroll
-                            for (int d = 0; d < D / 4; ++d)
-                                acc[r][d % VW][d / VW] = fmaf(wk, io<T>::ld(vp, d), acc[r][d % VW][d / VW]);
-                        }
+                        for (int d = 0; d < D / 4; ++d)
+                            acc[r][d % VW][d / VW] = fmaf(wk, io<T>::ld(vp, d), acc[r][d % VW][d / VW]);
                     }
                 }
             }
@@ -362,18 +390,20 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && RT == 1 ? 3 : 1) void pa
     }
 }
 
-// Adds the splits' sums: a row to a wave, 16 lanes side by side over its
-// channels and four of these over its splits, four splits in flight in each.
-template <typename T, int D>
+// Adds the splits' sums: a row to RW waves, 16 lanes side by side over its
+// channels and 4 RW of these over its splits, four splits in flight in each.
+template <typename T, int D, int RW>
 __global__ __launch_bounds__(THREADS) void join_kernel(PagedArgs a, PagedPlan plan, const float *part)
 {
-    constexpr int VW = D / 16, U = 4;
+    constexpr int VW = D / 16, U = 4, L = 4 * RW, ROWS = WAVES / RW;
+    __shared__ float red[WAVES][D + 1];
     const int s = blockIdx.y;
     const Seq seq = seq_of(a, s);
     const long long n = (long long)seq.count * a.Hq;
-    const int c = threadIdx.x % 16 * VW, l = threadIdx.x / 16 % 4;
+    const int wave = threadIdx.x / 64, c = threadIdx.x % 16 * VW, l = threadIdx.x / 16 % L;
     const float *gpart = part + (size_t)a.T * a.Hq * plan.splits * D;
-    for (long long i = (long long)blockIdx.x * WAVES + threadIdx.x / 64; i < n; i += (long long)gridDim.x * WAVES) {
+    for (long long i0 = (long long)blockIdx.x * ROWS; i0 < n; i0 += (long long)gridDim.x * ROWS) {
+        const long long i = min(i0 + wave / RW, n - 1);
         const int t = (int)(i / a.Hq), head = (int)(i - (long long)t * a.Hq);
         const int row = t * a.group + head % a.group;
         const Span sp = span_of_rows(a, seq, row / plan.rows * plan.rows, plan.rows);
@@ -383,18 +413,18 @@ __global__ __launch_bounds__(THREADS) void join_kernel(PagedArgs a, PagedPlan pl
         float f[VW], g = 0.f;
 #pragma unroll
         for (int j = 0; j < VW; ++j) f[j] = 0.f;
-        for (int k = l; k < used; k += 4 * U) {
+        for (int k = l; k < used; k += L * U) {
             float x[U][VW], y[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int at = min(k + 4 * u, used - 1);
+                const int at = min(k + L * u, used - 1);
                 y[u] = gp[at];
 #pragma unroll
                 for (int j = 0; j < VW; ++j) x[u][j] = p[(size_t)at * D + j];
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                if (k + 4 * u >= used) break;
+                if (k + L * u >= used) break;
                 g += y[u];
 #pragma unroll
                 for (int j = 0; j < VW; ++j) f[j] += x[u][j];
@@ -403,7 +433,24 @@ __global__ __launch_bounds__(THREADS) void join_kernel(PagedArgs a, PagedPlan pl
         g = rows4_sum(g);
 #pragma unroll
         for (int j = 0; j < VW; ++j) f[j] = rows4_sum(f[j]);
-        if (l) continue;
+        if constexpr (RW > 1) {
+            __syncthreads();
+            if (l % 4 == 0) {
+                red[wave][D] = g;
+#pragma unroll
+                for (int j = 0; j < VW; ++j) red[wave][c + j] = f[j];
+            }
+            __syncthreads();
+            if (l == 0) {
+#pragma unroll
+                for (int w = 1; w < RW; ++w) {
+                    g += red[wave + w][D];
+#pragma unroll
+                    for (int j = 0; j < VW; ++j) f[j] += red[wave + w][c + j];
+                }
+            }
+        }
+        if (l || i0 + wave / RW >= n) continue;
         const bool none = seq.len - seq.count + t < 0;
         T *out = (T *)a.out + o * D + c;
 #pragma unroll
@@ -431,10 +478,13 @@ hipError_t launch(const PagedArgs &a, const PagedPlan &plan, float *part, hipStr
     else if constexpr (sizeof(T) * D <= 256) e = launch_rt<T, D, 4>(a, plan, part, st);
     else e = hipErrorInvalidValue;   // no plan has such rows
     if (e != hipSuccess || plan.splits == 1) return e;
+    // a workgroup to a row where there are more splits than a wave has in flight
+    const int per = plan.splits > 16 ? 1 : WAVES;
     const long long rows = (long long)plan.rows * plan.tiles / a.group * a.Hq;
     const long long most = (long long)a.T * a.Hq;   // of one sequence
-    const dim3 grid((unsigned)(((rows < most ? rows : most) + WAVES - 1) / WAVES), (unsigned)a.S);
-    join_kernel<T, D><<<grid, THREADS, 0, st>>>(a, plan, part);
+    const dim3 grid((unsigned)(((rows < most ? rows : most) + per - 1) / per), (unsigned)a.S);
+    if (per == 1) join_kernel<T, D, WAVES><<<grid, THREADS, 0, st>>>(a, plan, part);
+    else join_kernel<T, D, 1><<<grid, THREADS, 0, st>>>(a, plan, part);
     return hipGetLastError();
 }
 
@@ -455,11 +505,13 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
 {
     PagedPlan plan;
     const long long rows = (long long)max_q * (Hq / Hkv);
-    // Several tokens of a sequence and more than one MFMA tile of rows: the
-    // chunk kernel (8 sequences of 4096 keys, D = 128, 4 query heads to a key
-    // head: 36 against 46 us for 6 tokens, 37 against 71 for 16).  Single
-    // tokens stay here whatever their heads: their weights keep two parts.
-    plan.chunk_kernel = D >= 32 && max_q > 1 && rows > 16;
+    // The chunk kernel against this one, 8 sequences of 4096 keys, 8 key heads:
+    // 32 rows (8 tokens, 4 query heads to a key head) bf16 D = 128 43 against
+    // 36 us, D = 64 29 against 20, D = 32 23 against 15; 48 to 64 rows bf16
+    // D = 128 44 against 51, D = 64 31 against 36, D = 32 24 against 21, float32
+    // D = 128 154 against 129, D = 64 84 against 61; 128 rows D = 128 49 against
+    // 50 and more beyond.  Single tokens stay here whatever their heads.
+    plan.chunk_kernel = D >= 32 && max_q > 1 && (rows > 64 || (rows > 32 && is_bf16 && D >= 64));
     plan.rows = plan.chunk_kernel ? CHUNK_ROWS : rows <= 16 ? 16 : rows <= 32 || (!is_bf16 && D == 128) ? 32 : 64;
     const long long tiles = (rows + plan.rows - 1) / plan.rows;
     // the most key tiles that a row tile can see
@@ -476,7 +528,7 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
     // 155 us in up to 2440, 171 in 1464.
     const long long base = tiles * Hkv * S;
     const auto toward = [&](long long target, long long least) {
-        const long long by_target = (target + base - 1) / base, by_size = key_tiles / least;
+        const long long by_target = (target + base - 1) / base, by_size = (key_tiles + least - 1) / least;
         return by_target < by_size ? by_target : by_size;
     };
     long long splits = 1;
