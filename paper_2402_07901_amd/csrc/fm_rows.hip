@@ -252,33 +252,49 @@ __global__ __launch_bounds__(THREADS) void rope_bwd_kernel(RowsBwdArgs a, int pe
     }
 }
 
-// dwq (block row 0) and dwk (1): sums of their partial rows, 16 channels and 64
-// rows side by side in a workgroup, in double precision so that the order of
-// a long sum does not show.
+// dwq (block row 0) and dwk (1): sums of their partial rows, 16 channels of a
+// workgroup, in double precision so that the order of a long sum does not show.
+// Latency bounds it: a lane holds 4 channels, so that 256 rows stand side by
+// side and 4 of a lane's are in flight, and only the waves' sums go through LDS.
 constexpr int SUM_THREADS = 1024;
 __global__ __launch_bounds__(SUM_THREADS) void weight_sum_kernel(const float *partial, float *dwq, float *dwk,
                                                                  long long nq, long long nk, int D)
 {
-    __shared__ double red[SUM_THREADS];
-    constexpr int LANES = SUM_THREADS / 16, U = 8;
+    constexpr int ROWS = SUM_THREADS / 4, U = 4;
+    __shared__ double red[SUM_THREADS / 64][16];
     const bool keys = blockIdx.y;
     const long long rows = keys ? nk : nq;
-    const int ch = blockIdx.x * 16 + threadIdx.x % 16;
-    const float *p = partial + (keys ? nq * D : 0) + ch;
-    double s = 0.0;
-    for (long long r = threadIdx.x / 16; r < rows; r += LANES * U) {
-        float x[U];
+    const float *p = partial + (keys ? nq * D : 0) + blockIdx.x * 16 + threadIdx.x % 4 * 4;
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    for (long long r = threadIdx.x / 4; r < rows; r += ROWS * U) {
+        float4 x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = r + LANES * u < rows ? p[(r + LANES * u) * D] : 0.f;
+        for (int u = 0; u < U; ++u) {
+            const long long ru = r + ROWS * u;
+            x[u] = ru < rows ? *(const float4 *)(p + ru * D) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
 #pragma unroll
-        for (int u = 0; u < U; ++u) s += (double)x[u];
+        for (int u = 0; u < U; ++u) {
+            s[0] += (double)x[u].x;
+            s[1] += (double)x[u].y;
+            s[2] += (double)x[u].z;
+            s[3] += (double)x[u].w;
+        }
     }
-    red[threadIdx.x] = s;
-    for (int o = LANES / 2; o; o /= 2) {
-        __syncthreads();
-        if (threadIdx.x < 16 * o) red[threadIdx.x] = s = s + red[threadIdx.x + 16 * o];
+    for (int o = 4; o < 64; o *= 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] += __shfl_xor(s[i], o);
     }
-    if (threadIdx.x < 16) (keys ? dwk : dwq)[ch] = (float)s;
+    if (threadIdx.x % 64 < 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) red[threadIdx.x / 64][threadIdx.x % 4 * 4 + i] = s[i];
+    }
+    __syncthreads();
+    if (threadIdx.x >= 16) return;
+    double sum = 0.0;
+#pragma unroll
+    for (int v = 0; v < SUM_THREADS / 64; ++v) sum += red[v][threadIdx.x];
+    (keys ? dwk : dwq)[blockIdx.x * 16 + threadIdx.x] = (float)sum;
 }
 
 long long token_blocks(long long tokens, int D) { return (tokens * (D / 16) + THREADS - 1) / THREADS; }
