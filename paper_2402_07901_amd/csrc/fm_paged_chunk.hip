@@ -200,7 +200,7 @@ __device__ __forceinline__ bool odd_bits(bf16_t v) { return (v & 0x7f80) == 0x7f
 __device__ __forceinline__ bool odd_bits(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
 
 template <typename T, int D>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 64 ? 3 : 2) void chunk_kernel(PagedArgs a, PagedPlan plan, float *part)
+__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 64 ? 3 : 2) void chunk_kernel(PagedArgs a, PagedPlan plan, int pieces, float *part)
 {
     constexpr int ROWS = CHUNK_ROWS, WR = ROWS / 4;   // rows of a workgroup, of a wave
     using W = Wave<T, D>;
@@ -214,15 +214,14 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 64 ? 3 : 2) void ch
     // every row sees the key
     __shared__ uint32_t flags[2][ROWS][DT];
 
-    // Workgroups of one (sequence, key head) read the same keys: they go to the
-    // same XCD (workgroups are dealt out to the 8 XCDs in turn).  Late row
-    // tiles see the most keys and start first.
-    int id = blockIdx.x / 8;
-    const int row_tile = plan.tiles - 1 - id % plan.tiles;
-    id /= plan.tiles;
-    const int split = id % plan.splits;
-    const int pair = id / plan.splits * 8 + blockIdx.x % 8;
-    if (pair >= a.S * a.Hkv) return;
+    // Row tiles of one (sequence, key head, split) read the same keys, so every
+    // `pieces`th of them go to the same XCD (workgroups are dealt out to the 8
+    // XCDs in turn).  Late row tiles see the most keys and start first.
+    const int in_piece = (plan.tiles + pieces - 1) / pieces;
+    const int turn = blockIdx.x / 8 / in_piece, piece = turn * 8 + (blockIdx.x + turn) % 8;
+    const int row_tile = plan.tiles - 1 - (piece % pieces + pieces * (blockIdx.x / 8 % in_piece));
+    const int split = piece / pieces % plan.splits, pair = piece / pieces / plan.splits;
+    if (pair >= a.S * a.Hkv || row_tile < 0) return;
     const int head = pair % a.Hkv, s = pair / a.Hkv;
 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -434,10 +433,17 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 64 ? 3 : 2) void ch
 
 template <typename T, int D> hipError_t launch(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
 {
-    const long long pairs = ((long long)a.S * a.Hkv + 7) / 8 * 8;
-    const long long blocks = pairs * plan.tiles * plan.splits;
+    // Row tiles that share their keys stay on one XCD unless that leaves more
+    // than an eighth of the XCDs' time empty.  bf16, D = 128, 32 heads: one
+    // sequence of 8192 keys, 4096 tokens and 4 key heads 1022 us on 4 XCDs, 570
+    // in two pieces each; 32 sequences of 4096 keys, 256 tokens and 8 key heads
+    // 291 whole, 312 in two pieces.
+    const long long units = (long long)a.S * a.Hkv * plan.splits;
+    int pieces = 1;
+    while (pieces < 8 && 2 * pieces <= plan.tiles && 7 * ((units * pieces + 7) / 8) > units * pieces) pieces *= 2;
+    const long long blocks = (units * pieces + 7) / 8 * 8 * ((plan.tiles + pieces - 1) / pieces);
     if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
-    chunk_kernel<T, D><<<(unsigned)blocks, THREADS, 0, st>>>(a, plan, part);
+    chunk_kernel<T, D><<<(unsigned)blocks, THREADS, 0, st>>>(a, plan, pieces, part);
     return hipGetLastError();
 }
 
