@@ -409,3 +409,18 @@ def test_allocations_belong_to_the_stream():
     torch.cuda.synchronize()
     for g in got:
         assert torch.equal(g, want)
+
+
+@pytest.mark.parametrize("Hq,Hkv,lens,news", [(8, 1, [900], [300]), (6, 3, [700], [400]),
+                                              (5, 5, [40, 1500], [33, 257]),
+                                              (12, 12, [513], [513]),
+                                              (16, 2, [2100, 70, 3], [130, 70, 1])])
+@pytest.mark.parametrize("dtype,D", [("bf16", 32), ("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_chunks_of_few_heads(Hq, Hkv, lens, news, dtype, D):
+    """Chunks whose units (sequence, key head, split) do not divide by the XCDs,
+    uneven sequences among them; held to the bound of weights in two bf16 parts."""
+    label = f"paged chunk D={D} {dtype} H={Hq}/{Hkv} lens={lens}"
+    say(label)
+    c = Cache(lens, news, Hq, Hkv, D, 32, dtype, seed=Hq)
+    c.check(c.run(max_q=max(news)), label, starts=False)
+    c.check(c.run(max_q=max(news), p=1, scale=1.0 / D), label, p=1, tau=1.0 / D, starts=False)
