@@ -23,7 +23,7 @@
 // of 131072 keys 99 to 102 us (5.3 TB/s, join included), 61 of 4096 186 us
 // (5.5), 61 of uneven lengths up to 8192 149 to 153 us (4.9: the last
 // workgroups run alone); float32, 32 windows of 4096 keys, D = 64: 99 us (5.4).
-// One sequence of 777 keys: 8.3 us, two launches.  Chunks of prompts with many
+// One sequence of 777 keys, 12 heads of 64: 8.3 us, one launch.  Chunks of prompts with many
 // rows go to fm_paged_chunk.hip.
 #include <hip/hip_runtime.h>
 
@@ -225,8 +225,8 @@ template <int D> struct Mat<float, D> {
 
 // MULTI: rows of several tokens may share a tile, so a key can be visible to
 // some rows of a tile and not to others.
-template <typename T, int D, int RT, bool MULTI>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 128 && RT == 1 ? 3 : 1) void paged_kernel(PagedArgs a, PagedPlan plan, float *part)
+template <typename T, int D, int RT, bool MULTI, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && D == 128 && RT == 1 && WAVES == 4 ? 3 : 1) void paged_kernel(PagedArgs a, PagedPlan plan, float *part)
 {
     using M = Mat<T, D>;
     constexpr int VW = M::VW, ROWS = 16 * RT, RS = D + 4;
@@ -369,7 +369,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 128 && RT == 1 ? 3 
             for (int d = 0; d < D / 4; ++d) red[wave][r16][h * (D / 4) + d] = acc[r][d % VW][d / VW];
             __syncthreads();
             const int rr = threadIdx.x / 16, c = threadIdx.x % 16 * VW, row = r0 + 16 * r + rr;
-            if (row < rows) {
+            if (rr < 16 && row < rows) {
                 float f[VW], gg = 0.f;
 #pragma unroll
                 for (int j = 0; j < VW; ++j) f[j] = 0.f;
@@ -467,13 +467,13 @@ __global__ __launch_bounds__(THREADS) void join_kernel(PagedArgs a, PagedPlan pl
     }
 }
 
-template <typename T, int D, int RT>
+template <typename T, int D, int RT, int W = WAVES>
 hipError_t launch_rt(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
 {
     const long long blocks = (long long)plan.splits * plan.tiles * a.Hkv * a.S;
-    if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
-    if (a.q_start) paged_kernel<T, D, RT, true><<<(unsigned)blocks, THREADS, 0, st>>>(a, plan, part);
-    else paged_kernel<T, D, RT, false><<<(unsigned)blocks, THREADS, 0, st>>>(a, plan, part);
+    if (!grid_fits(blocks, 64 * W)) return hipErrorInvalidConfiguration;
+    if (a.q_start) paged_kernel<T, D, RT, true, W><<<(unsigned)blocks, 64 * W, 0, st>>>(a, plan, part);
+    else paged_kernel<T, D, RT, false, W><<<(unsigned)blocks, 64 * W, 0, st>>>(a, plan, part);
     return hipGetLastError();
 }
 
@@ -482,6 +482,7 @@ hipError_t launch(const PagedArgs &a, const PagedPlan &plan, float *part, hipStr
 {
     hipError_t e;
     if (plan.chunk_kernel) e = paged_chunk(a, plan, D, sizeof(T) == 2, part, st);
+    else if (plan.waves == 8) e = launch_rt<T, D, 1, 8>(a, plan, part, st);
     else if (plan.rows == 16) e = launch_rt<T, D, 1>(a, plan, part, st);
     else if (plan.rows == 32) e = launch_rt<T, D, 2>(a, plan, part, st);
     else if constexpr (sizeof(T) * D <= 256) e = launch_rt<T, D, 4>(a, plan, part, st);
@@ -522,6 +523,7 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
     // 50 and more beyond.  Single tokens stay here whatever their heads.
     plan.chunk_kernel = D >= 32 && max_q > 1 && (rows > 64 || (rows > 32 && is_bf16 && D >= 64));
     plan.rows = plan.chunk_kernel ? CHUNK_ROWS : rows <= 16 ? 16 : rows <= 32 || (!is_bf16 && D == 128) ? 32 : 64;
+    plan.waves = WAVES;
     const long long tiles = (rows + plan.rows - 1) / plan.rows;
     // the most key tiles that a row tile can see
     const long long tokens = (long long)plan.rows * Hkv / Hq + 2;
@@ -548,13 +550,29 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
             if (splits * base < t && splits < few) splits = few;
         }
     } else if (base < 1024) {
-        splits = toward(2048, is_bf16 ? 64 : 32);
-        const long long few = toward(512, 16);
-        if (splits * base < 512 && splits < few) splits = few;
+        // Eight waves and one launch where a second one costs more than it
+        // gives: up to a workgroup per CU while keys and values of a head are
+        // at most 256 KB, beyond that while twice the least above is not
+        // passed and the workgroups' registers fit the CUs.  bf16: one
+        // sequence of 512 keys, 12 heads of 64 7.0 us, 7.9 in two splits (and
+        // 12 against 17 a call); of 1024 keys, 8 heads of 128 13 against 9, so
+        // split; 32 of 512 keys 15 against 19; 64 of up to 512, 4 heads of 64
+        // 7.7 against 11; but 100 of up to 512, 8 heads of 128 26 against 18
+        // (four waves).  Under 256 keys four waves do: 60 keys 4.8, eight 5.4.
+        const long long least = is_bf16 ? 64 : 32, row = (is_bf16 ? 2 : 4) * D;
+        const bool one = base < 256 ? key_tiles * KT * row <= 128 << 10
+                                    : key_tiles <= 2 * least && (base <= 512 || row <= 128);
+        if (plan.rows == 16 && key_tiles > 16 && one) {
+            plan.waves = 8;
+        } else {
+            splits = toward(2048, least);
+            const long long few = toward(512, 16);
+            if (splits * base < 512 && splits < few) splits = few;
+        }
     }
     if (splits < 1) splits = 1;
     long long chunk = (key_tiles + splits - 1) / splits;
-    chunk = (chunk + 2 * WAVES - 1) / (2 * WAVES) * (2 * WAVES);
+    chunk = (chunk + 2 * plan.waves - 1) / (2 * plan.waves) * (2 * plan.waves);
     plan.tiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);
     plan.chunk = (int)chunk;
     plan.splits = (int)((key_tiles + chunk - 1) / chunk);

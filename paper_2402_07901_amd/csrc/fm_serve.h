@@ -64,6 +64,7 @@ struct PagedArgs {
 struct PagedPlan {
     bool chunk_kernel;             // fm_paged_chunk.hip, else fm_paged.hip
     int rows;                      // rows of a row tile
+    int waves;                     // of a workgroup (fm_paged.hip)
     int tiles;                     // row tiles in the grid
     int chunk;                     // key tiles of 16 per split
     int splits;
