@@ -202,6 +202,17 @@ template <int N> __device__ __forceinline__ void put(bf16_t *p, const float *f)
 
 __device__ __forceinline__ bool odd_bits(bf16_t v) { return (v & 0x7f80) == 0x7f80; }
 __device__ __forceinline__ bool odd_bits(float v) { return (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u; }
+// one among 16 bytes of them
+template <typename T> __device__ __forceinline__ bool odd_bits(u4 x)
+{
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        odd |= odd_bits(__uint_as_float(x[i]));   // bf16: the upper one
+        if constexpr (sizeof(T) == 2) odd |= odd_bits((bf16_t)x[i]);
+    }
+    return odd;
+}
 
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 64 ? 3 : 2) void chunk_kernel(PagedArgs a, PagedPlan plan, int pieces, float *part)
@@ -301,10 +312,12 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 64 ? 3 : 2) void ch
         const auto unseen = [&](int i0) { return i0 < whole || i0 + KB / KT > whole_end; };
         // An infinity or a NaN among values that some row may not see: weight 0
         // would make it NaN there, so it leaves the buffer, and the rows that
-        // do see it are marked.
+        // do see it are marked.  (Looked for 16 bytes at a time: the diagonal
+        // and a window's edges are all that a short chunk has.)
         const auto screen = [&](int i0, u4 *vd) {
-#pragma unroll 1
+#pragma unroll
             for (int piece = threadIdx.x; piece < KB * C; piece += THREADS) {
+                if (!odd_bits<T>(vd[piece])) continue;
                 const int r = piece / C, c = piece % C ^ swizzle<C>(r);
                 T *x = (T *)&vd[piece];
 #pragma unroll 1
@@ -438,13 +451,16 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 64 ? 3 : 2) void ch
 template <typename T, int D> hipError_t launch(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
 {
     // Row tiles that share their keys stay on one XCD unless that leaves more
-    // than an eighth of the XCDs' time empty.  bf16, D = 128, 32 heads: one
-    // sequence of 8192 keys, 4096 tokens and 4 key heads 1022 us on 4 XCDs, 570
-    // in two pieces each; 32 sequences of 4096 keys, 256 tokens and 8 key heads
-    // 291 whole, 312 in two pieces.
+    // than an eighth of the XCDs' time empty, or several sequences, which may be
+    // uneven, leave an XCD fewer than 8 of them.  bf16, D = 128: one sequence of
+    // 8192 keys, 4096 rows of 32 heads to 4 1022 us on 4 XCDs, 570 in two pieces
+    // each, 606 in eight; 16 sequences of up to 8192, 512 rows of 16 heads to 2
+    // 394 whole, 307 in two pieces; 32 even ones of 4096, 256 rows of 32 heads to
+    // 8 291 whole, 312 in two pieces.
     const long long units = (long long)a.S * a.Hkv * plan.splits;
+    const auto more = [&](long long n) { return 7 * ((n + 7) / 8) > n || (a.S > 1 && n < 64); };
     int pieces = 1;
-    while (pieces < 8 && 2 * pieces <= plan.tiles && 7 * ((units * pieces + 7) / 8) > units * pieces) pieces *= 2;
+    while (pieces < 8 && 2 * pieces <= plan.tiles && more(units * pieces)) pieces *= 2;
     const long long blocks = (units * pieces + 7) / 8 * 8 * ((plan.tiles + pieces - 1) / pieces);
     if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
     chunk_kernel<T, D><<<(unsigned)blocks, THREADS, 0, st>>>(a, plan, pieces, part);
