@@ -225,8 +225,12 @@ template <int D> struct Mat<float, D> {
 
 // MULTI: rows of several tokens may share a tile, so a key can be visible to
 // some rows of a tile and not to others.
+// At D = 128 registers are bounded for as many waves as pay on a SIMD: three in
+// bf16, two in float32 (61 sequences of up to 8192 keys, 8 heads, float32 309 us;
+// one 367).
 template <typename T, int D, int RT, bool MULTI, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && D == 128 && RT == 1 && WAVES == 4 ? 3 : 1) void paged_kernel(PagedArgs a, PagedPlan plan, float *part)
+__global__ __launch_bounds__(64 * WAVES, D == 128 && RT == 1 && WAVES == 4 ? (sizeof(T) == 2 ? 3 : 2) : 1)
+void paged_kernel(PagedArgs a, PagedPlan plan, float *part)
 {
     using M = Mat<T, D>;
     constexpr int VW = M::VW, ROWS = 16 * RT, RS = D + 4;
@@ -319,7 +323,19 @@ __global__ __launch_bounds__(64 * WAVES, sizeof(T) == 2 && D == 128 && RT == 1 &
                 }
                 // A value that is infinite or NaN takes the step out of MFMA: a row
                 // whose weight is 0 because it does not see the key would get NaN,
-                // and so would infinity times a weight's second part.
+                // and so would infinity times a weight's second part.  Without
+                // either (float32, one token: its rows see the same keys) what was
+                // read in place of a key that is not seen becomes 0, as its weight.
+                if constexpr (!M::PARTS && !MULTI) {
+                    if (!all) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (visible(base[i / 4] + 4 * h + i % 4, pos[0], a.window, a.sinks)) continue;
+#pragma unroll
+                            for (auto &x : v.x[i]) x = 0.f;
+                        }
+                    }
+                }
                 const bool odd = (M::PARTS || (MULTI && !all)) && __any(M::odd(v));
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {

@@ -1,0 +1,47 @@
+"""GPU tests of values that are infinite or not a number in the paged
+attention: what the rows that see them get, and that no other row notices."""
+import numpy as np
+import pytest
+
+from paper_2402_07901_amd import fastmax as fm
+
+import serve_util as su
+from gpu_util import say
+from paged_util import positions, put, seen
+from test_paged import Cache
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    fm.lib()
+    yield
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [16, 32, 64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
+def test_single_tokens_get_the_infinity_they_see(dtype, D, window, sinks):
+    """Lengths that end inside a tile of 16 keys, in an odd number of tiles, in
+    one tile and in several splits: lanes without a key of their own read
+    another one under weight 0, which must not make a NaN of its infinity."""
+    import torch
+    say(f"one token and an infinity D={D} {dtype} window={window}")
+    lens = [1, 8, 16, 17, 40, 72, 333, 777, 3000]
+    for back in (0, 1, 5, 19, 20, 50, 10 ** 6):        # tokens before the last; or the first
+        for value in (float("inf"), float("-inf"), float("nan")):
+            c = Cache(lens, [1] * len(lens), 4, 2, D, 32, dtype, seed=D)
+            want = np.zeros((len(lens), 4, D), bool)
+            for s, n in enumerate(lens):
+                t = max(0, n - 1 - back)
+                put(c, s, t, 1, value, 9)
+                want[s, 2:, 9] = seen(n - 1, t, window, sinks)
+            out = su.np64(c.run(starts=False, window=window, sinks=sinks))
+            assert np.array_equal(~np.isfinite(out), want), (back, value)
+            if value == value:
+                assert (out[want] == value).all(), (back, value)
