@@ -332,9 +332,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 64 ? 3 : 2) void ch
                     for (int i = 0; i < ROWS && r0 + i < rows; ++i) {
                         const int t = (r0 + i) / a.group;
                         if (!visible(n, pos0 + t, a.window, a.sinks)) continue;
-                        const bool nan = isnan(io<T>::ld(&v, 0));
-                        bool neg = io<T>::ld(&v, 0) < 0.f;
-                        if (!nan && a.c2 == 0.f) {   // first order: the weight has a sign
+                        bool nan = isnan(io<T>::ld(&v, 0)), neg = io<T>::ld(&v, 0) < 0.f;
+                        if (!nan && a.c2 == 0.f) {   // first order: the weight may be negative, or 0
                             const T *qp = (const T *)a.q + (seq.t0 + t) * a.q_token +
                                           (head * a.group + r0 + i - t * a.group) * a.q_head;
                             const int page = min((unsigned)table[n >> a.page_shift], (unsigned)a.pages - 1);
@@ -342,7 +341,9 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 64 ? 3 : 2) void ch
                             float dot = 0.f;
 #pragma unroll 1
                             for (int d = 0; d < D; ++d) dot = fmaf(io<T>::ld(qp, d), io<T>::ld(kp, d), dot);
-                            neg ^= fmaf(dot, a.c1, 1.0f) < 0.f;
+                            const float w = fmaf(dot, a.c1, 1.0f);
+                            nan = w == 0.f;
+                            neg ^= w < 0.f;
                         }
                         const int ch = P * c + e;
                         if (nan || !neg) atomicOr(&flags[0][i][ch / 32], 1u << (ch % 32));

@@ -45,3 +45,27 @@ def test_single_tokens_get_the_infinity_they_see(dtype, D, window, sinks):
             assert np.array_equal(~np.isfinite(out), want), (back, value)
             if value == value:
                 assert (out[want] == value).all(), (back, value)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("starts", [True, False])
+def test_a_weight_of_zero_makes_nan_of_an_infinity(dtype, D, starts):
+    """p = 1, scale 1 / D, q^ = -k^ of +-1 entries: the weight is exactly 0 and
+    0 times infinity is NaN; where q^ = k^ it is 2."""
+    import torch
+    n, t = 150, 100
+    news = n if starts else 1
+    c = Cache([n], [news], 4, 2, D, 32, dtype, seed=D)
+    u = torch.ones(D, device="cuda")
+    u[::2] = -1.0
+    c.k[int(c.table_h[0, t // 32]), 1, t % 32] = u.to(c.k.dtype)
+    put(c, 0, t, 1, float("inf"), 9)
+    c.q[:, 2], c.q[:, 3] = -u.to(c.q.dtype), u.to(c.q.dtype)
+    out = c.run(starts=starts, p=1, scale=1.0 / D, max_q=news)
+    see = seen(positions(c, 0), t)
+    bad = su.np64(~torch.isfinite(out)) > 0
+    assert bad[see, 2:, 9].all() and bad.sum() == 2 * see.sum()
+    out = su.np64(out)
+    assert np.isnan(out[see, 2, 9]).all()
+    assert (out[see, 3, 9] == np.inf).all()
