@@ -434,8 +434,9 @@ int fastmax_cache_append(const void *q, const void *k, const void *v,
  * A row that sees no key (lens[s] smaller than its new tokens) is 0.  What
  * lies in slots that no row of a sequence sees is not used, whatever it
  * holds; entries of the page table past lens[s] or behind the window are not
- * read.  If an entry that is read is not a page, or lens[s] is more than
- * table_cols pages hold, the rows that it concerns are NaN.
+ * read.  A row that sees a key whose entry is not a page is NaN, and so is
+ * every row with a key of a sequence whose lens[s] is more than table_cols
+ * pages hold.
  * table_cols * page_size <= 2^30, S <= 65535.
  */
 size_t fastmax_paged_workspace_bytes(int S, int T, int Hq, int Hkv, int D, int max_q, int max_len,

@@ -53,6 +53,21 @@ __device__ __forceinline__ bool visible(int n, int pos, int window, int sinks)
     return n <= pos && (n > pos - window || n < sinks);
 }
 
+// Whether a query at position pos sees a key of a page that is not there, among
+// the key tiles [begin, end): asked only once such a page was met.
+__device__ __forceinline__ bool sees_bad_page(const PagedArgs &a, const int32_t *table, const Span &sp, int begin,
+                                              int end, int pos)
+{
+    bool bad = false;
+#pragma unroll 1
+    for (int i = begin; i < end; ++i) {
+        const int n0 = sp.tile(i) * KT;
+        if ((unsigned)table[n0 >> a.page_shift] < (unsigned)a.pages) continue;
+        bad |= n0 <= pos && (min(n0 + KT - 1, pos) > pos - a.window || n0 < a.sinks);
+    }
+    return bad;
+}
+
 // A sequence's new tokens: rows [t0, t0 + count) of q, the last at len - 1.
 struct Seq {
     int t0, count, len;

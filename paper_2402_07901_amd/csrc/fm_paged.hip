@@ -378,9 +378,10 @@ void paged_kernel(PagedArgs a, PagedPlan plan, float *part)
         // the waves' sums, one row tile at a time
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            const float gs = rows4_sum(g[r]);
+            float gs = rows4_sum(g[r]);
+            if (bad && (seq.cut || sees_bad_page(a, table, sp, begin, end, pos[r]))) gs = __builtin_nanf("");
             __syncthreads();
-            if (h == 0) gred[wave][r16] = bad ? __builtin_nanf("") : gs;
+            if (h == 0) gred[wave][r16] = gs;
 #pragma unroll
             for (int d = 0; d < D / 4; ++d) red[wave][r16][h * (D / 4) + d] = acc[r][d % VW][d / VW];
             __syncthreads();

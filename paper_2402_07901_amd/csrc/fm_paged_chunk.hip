@@ -409,7 +409,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 2 && D == 64 ? 3 : 2) void ch
         met_odd = __syncthreads_or(met_odd);
 
         float gs = halves_sum(g);
-        if (bad) gs = __builtin_nanf("");
+        if (bad && (seq.cut || sees_bad_page(a, table, sp, begin, end, pos))) gs = __builtin_nanf("");
         const float inv = 1.0f / gs;
         const size_t o = (size_t)(seq.t0 + t) * a.Hq + q_head;
         if (row < rows) {
