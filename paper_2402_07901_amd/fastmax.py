@@ -622,7 +622,8 @@ def _cache_of(q, k_cache, v_cache, Hkv):
     _rows_of("k_cache", k_cache, (pages, Hkv, page, q.shape[-1]), dtype, dev, q)
     _rows_of("v_cache", v_cache, shape, dtype, dev, q)
     st = k_cache.stride()
-    if v_cache.stride() != st:
+    if v_cache.stride() != st and any(n > 1 and x != y
+                                      for n, x, y in zip(shape, st, v_cache.stride())):
         raise ValueError(f"k_cache and v_cache must have the same strides, got {st} and "
                          f"{v_cache.stride()}")
     return pages, page, _LL3(st[0], st[2], st[1])

@@ -189,3 +189,22 @@ def test_binding_checks():
                    (cache, torch.zeros(4, 16, 2, 64).transpose(1, 2))):
         with pytest.raises(ValueError):
             fm._cache_of(q, kc, vc, 2)
+
+
+def test_strides_of_single_pages_and_heads():
+    """Strides along an axis of size 1 reach nothing: the caches may differ there."""
+    import torch
+    q = torch.zeros(3, 4, 64)
+    whole = torch.zeros(5, 1, 16, 64)
+    turned = torch.zeros(5, 16, 1, 64).transpose(1, 2)
+    assert whole.stride() != turned.stride()
+    for kc, vc in ((whole, turned), (turned, whole)):
+        pages, page, st = fm._cache_of(q, kc, vc, 1)
+        assert (pages, page) == (5, 16) and tuple(st)[:2] == (1024, 64)
+    one, first = torch.zeros(1, 2, 16, 64), torch.zeros(7, 2, 16, 64)[::3][:1]
+    assert one.stride() != first.stride()
+    for kc, vc in ((one, first), (first, one)):
+        pages, page, st = fm._cache_of(q, kc, vc, 2)
+        assert (pages, page) == (1, 16) and tuple(st)[1:] == (64, 1024)
+    with pytest.raises(ValueError, match="same strides"):
+        fm._cache_of(q, torch.zeros(5, 2, 16, 64), torch.zeros(5, 16, 2, 64).transpose(1, 2), 2)
