@@ -512,7 +512,9 @@ def _owner(stream, device):
     others while it runs."""
     torch = _torch()
     if not hasattr(stream, "cuda_stream"):
-        stream = torch.cuda.ExternalStream(stream, device=device)
+        # handle 0 is the null stream; torch would make a stream of its own of it
+        stream = (torch.cuda.ExternalStream(stream, device=device) if stream
+                  else torch.cuda.default_stream(device))
     with torch.cuda.stream(stream):
         yield
 
