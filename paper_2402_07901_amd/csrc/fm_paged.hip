@@ -541,7 +541,15 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
     plan.chunk_kernel = D >= 32 && max_q > 1 && (rows > 64 || (rows > 32 && is_bf16 && D >= 64));
     plan.rows = plan.chunk_kernel ? CHUNK_ROWS : rows <= 16 ? 16 : rows <= 32 || (!is_bf16 && D == 128) ? 32 : 64;
     plan.waves = WAVES;
-    const long long tiles = (rows + plan.rows - 1) / plan.rows;
+    // max_q holds for the longest sequence and may be all of T, so most row tiles
+    // of a grid may be empty: past 2^18 workgroups it has no more of them, and
+    // the rows behind them are taken in rounds.  (An empty workgroup costs a ns:
+    // 1024 prompts of 128 tokens, 8 key heads, D = 32, max_q left out 594 us, 1367
+    // with up to 2^20, 8910 with 2^23; 359 with the max_q that they have.  One
+    // prompt of 8192 tokens among 1023 of up to 40, D = 64: 810, 1701, 2811 us,
+    // and 2530 with up to 2^16.)
+    const long long pairs = (long long)S * Hkv, most = (1 << 18) / pairs > 1 ? (1 << 18) / pairs : 1;
+    const long long all = (rows + plan.rows - 1) / plan.rows, tiles = all < most ? all : most;
     // the most key tiles that a row tile can see
     const long long tokens = (long long)plan.rows * Hkv / Hq + 2;
     const long long seen = (long long)window + tokens + 2 * KT + sinks;
@@ -554,7 +562,7 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
     // sequence of 131072 keys, 8 heads, D = 128: 112 us in 1024 workgroups,
     // 127 in 2048; 4 of 16384: 29 us in 512, 39 in 2048; 61 of up to 8192:
     // 155 us in up to 2440, 171 in 1464.
-    const long long base = tiles * Hkv * S;
+    const long long base = tiles * pairs;
     const auto toward = [&](long long target, long long least) {
         const long long by_target = (target + base - 1) / base, by_size = (key_tiles + least - 1) / least;
         return by_target < by_size ? by_target : by_size;
@@ -590,7 +598,7 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
     if (splits < 1) splits = 1;
     long long chunk = (key_tiles + splits - 1) / splits;
     chunk = (chunk + 2 * plan.waves - 1) / (2 * plan.waves) * (2 * plan.waves);
-    plan.tiles = (int)(tiles < INT32_MAX ? tiles : INT32_MAX);
+    plan.tiles = (int)tiles;
     plan.chunk = (int)chunk;
     plan.splits = (int)((key_tiles + chunk - 1) / chunk);
     return plan;
