@@ -528,8 +528,14 @@ def _new(q, shapes, stream, dtype=None):
         return [x if x is None else q.new_empty(x, dtype=dtype) for x in shapes]
 
 
-def _scratch(q, nbytes, stream):
-    return _new(q, [(nbytes,)], stream, _torch().uint8)[0] if nbytes else None
+def _workspace(q, given, nbytes, stream):
+    """(tensor, bytes) of a call's workspace: the caller's, checked, or
+    ``nbytes()`` of its own."""
+    if given is not None:
+        _whole("workspace", given, given.shape, given.dtype, q.get_device(), q)
+        return given, given.numel() * given.element_size()
+    n = nbytes()
+    return (_new(q, [(n,)], stream, _torch().uint8)[0], n) if n else (None, 0)
 
 
 def _run(what, fn, dev, stream, *args):
@@ -602,9 +608,8 @@ def fastmax_rope_bwd(q, k, gq, gk, gv, pos, cos, sin, wq=None, wk=None, eps=1e-6
     dwq = dwk = None
     if wq is not None:
         dwq, dwk = _new(q, ((D,), (D,)), stream, wq.dtype)
-    if workspace is None:
-        workspace = _scratch(q, rope_workspace_bytes(B, N, Hq, Hkv, D, wq is not None), stream)
-    ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    workspace, ws_n = _workspace(
+        q, workspace, lambda: rope_workspace_bytes(B, N, Hq, Hkv, D, wq is not None), stream)
     _run("fastmax_rope_bwd", lib().fastmax_rope_bwd, dev, stream,
          q.data_ptr(), k.data_ptr(), _LL6(*q.stride()[:3], *k.stride()[:3]),
          gq.data_ptr(), gk.data_ptr(), gv.data_ptr(),
@@ -693,10 +698,9 @@ def fastmax_paged_fwd(q, k_cache, v_cache, table, lens, q_start=None, max_q=None
         out, = _new(q, ((T, Hq, D),), stream)
     else:
         _whole("out", out, (T, Hq, D), dtype, dev, q)
-    if workspace is None:
-        workspace = _scratch(q, paged_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window,
-                                                      sinks, dt), stream)
-    ws_n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    workspace, ws_n = _workspace(
+        q, workspace,
+        lambda: paged_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window, sinks, dt), stream)
     _run("fastmax_paged_fwd", lib().fastmax_paged_fwd, dev, stream,
          q.data_ptr(), _LL3(0, *q.stride()[:2]), k_cache.data_ptr(), v_cache.data_ptr(), cache,
          table.data_ptr(), lens.data_ptr(), _ptr(q_start), out.data_ptr(), S, T, Hq, Hkv, D, pages,

@@ -31,3 +31,21 @@ def test_allocations_of_the_null_stream():
     torch.cuda.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def test_workspaces_in_the_wrong_place_are_refused():
+    import torch
+    r = Rows(1, 50, 6, 2, 64, "bf16")
+    ups = [torch.randn((1, 6, 50, 64), device="cuda").bfloat16() for _ in range(3)]
+    need = fm.rope_workspace_bytes(1, 50, 6, 2, 64, True)
+    kv = torch.zeros((2, 8, 2, 1024, 64), dtype=torch.bfloat16, device="cuda")
+    table = torch.arange(8, dtype=torch.int32, device="cuda")[None]
+    lens = torch.full((1,), 8192, dtype=torch.int32, device="cuda")
+    paged = fm.paged_workspace_bytes(1, 1, 6, 2, 64, 1, 8192, 0, 0, fm.BF16)
+    assert need > 0 and paged > 0
+    for bad in (torch.empty(max(need, paged), dtype=torch.uint8),
+                torch.empty(2 * max(need, paged), dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            fm.fastmax_rope_bwd(r.q, r.k, *ups, workspace=bad, **r.kw())
+        with pytest.raises(ValueError, match="workspace"):
+            fm.fastmax_paged_fwd(r.q[0, :1], *kv, table, lens, workspace=bad)

@@ -208,3 +208,17 @@ def test_strides_of_single_pages_and_heads():
         assert (pages, page) == (1, 16) and tuple(st)[1:] == (64, 1024)
     with pytest.raises(ValueError, match="same strides"):
         fm._cache_of(q, torch.zeros(5, 2, 16, 64), torch.zeros(5, 16, 2, 64).transpose(1, 2), 2)
+
+
+def test_workspaces_are_checked():
+    """A workspace with gaps, or in another place than the rows, is refused: the
+    library writes its bytes one after the other, on the GPU."""
+    import torch
+    q, given = torch.zeros(2, 4, 64), torch.zeros(100, dtype=torch.uint8)
+    assert fm._workspace(q, given, None, None) == (given, 100)
+    assert fm._workspace(q, given.view(torch.int32), None, None)[1] == 100
+    assert fm._workspace(q, None, lambda: 0, None) == (None, 0)
+    with pytest.raises(ValueError, match="workspace must be contiguous"):
+        fm._workspace(q, given[::2], None, None)
+    with pytest.raises(ValueError, match="workspace is on meta"):
+        fm._workspace(q, given.to("meta")[::2], None, None)
