@@ -69,3 +69,48 @@ def test_a_weight_of_zero_makes_nan_of_an_infinity(dtype, D, starts):
     out = su.np64(out)
     assert np.isnan(out[see, 2, 9]).all()
     assert (out[see, 3, 9] == np.inf).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("n,news,t", [(150, 150, 100), (150, 3, 148), (4000, 100, 3950),
+                                      (4000, 100, 17), (4000, 1, 3990)])
+def test_first_order_weights_have_a_sign(dtype, D, n, news, t):
+    """p = 1: an infinity comes out under its weight's sign, near the diagonal
+    and far behind it, in one launch and in splits."""
+    say(f"first order and an infinity D={D} {dtype} n={n} new={news} t={t}")
+    c = Cache([n], [news], 4, 2, D, 32, dtype, seed=D)
+    put(c, 0, t, 1, float("inf"), 9)
+    tau = 1.0 / np.sqrt(D)                             # scores of size 1
+    out = su.np64(c.run(starts=news > 1, p=1, scale=float(np.float32(tau)), max_q=news))
+    see = seen(positions(c, 0), t)
+    G = 1.0 + tau * np.einsum("thd,nd->thn", su.np64(c.q)[:, 2:], c.k_h[0][:, 1])
+    w = G[..., t]
+    G = np.where((np.arange(n) <= positions(c, 0)[:, None])[:, None], G, 0.0).sum(-1)
+    bad = ~np.isfinite(out)
+    assert bad[see, 2:, 9].all() and bad.sum() == 2 * see.sum()
+    # a score near -1 / tau leaves its weight's sign to rounding (D + 8 steps of
+    # 2^-24 of a sum of magnitudes up to D), and so does a sum near 0
+    sure = see[:, None] & (np.abs(w) > 1e-3) & (np.abs(G) > 1e-3 * n)
+    assert sure.any() and (see.sum() < 20 or ((w < 0) & sure).any())
+    assert np.array_equal(out[:, 2:, 9][sure], np.sign(w / G)[sure] * np.inf)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_infinities_in_splits_of_a_chunk(dtype):
+    """One sequence whose keys are cut into pieces that are joined: tokens near
+    the diagonal, in the last and in an earlier piece."""
+    import torch
+    n, news, D = 4000, 100, 64
+    assert fm.paged_workspace_bytes(1, news, 4, 2, D, news, n, 0, 0,
+                                    fm.F32 if dtype == "f32" else fm.BF16) > 0
+    for t in (3990, 3950, 3904, 1000):
+        for value in (float("inf"), float("-inf"), float("nan")):
+            c = Cache([n], [news], 4, 2, D, 32, dtype, seed=t)
+            put(c, 0, t, 0, value, 40)
+            out = c.run(max_q=news, max_len=n)
+            see = seen(positions(c, 0), t)
+            bad = su.np64(~torch.isfinite(out)) > 0
+            assert bad[see, :2, 40].all() and bad.sum() == 2 * see.sum(), (t, value)
+            if value == value:
+                assert (su.np64(out)[see, :2, 40] == value).all(), (t, value)

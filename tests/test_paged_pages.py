@@ -56,3 +56,63 @@ def test_rows_that_see_no_bad_page_are_whole(dtype, D, lens, news, Hq, Hkv, page
         assert np.isnan(got[see]).all(), entry
         check_rows(c, out, 0, ~see, entry, window=window, sinks=sinks)
         check_rows(c, out, 1, np.ones(news[1], bool), entry, window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 16), ("bf16", 64), ("f32", 64)])
+def test_chunk_of_a_sequence_longer_than_its_table(dtype, D):
+    import torch
+    c = Cache([640, 200], [300, 200], 4, 2, D, 32, dtype, cols=20)
+    c.lens[0] = 641
+    out = c.run(max_q=300, max_len=640)
+    assert torch.isnan(out[:300]).all()
+    check_rows(c, out, 1, np.ones(200, bool), "the other sequence")
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 16), ("bf16", 64), ("bf16", 128), ("f32", 32),
+                                     ("f32", 128)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (33, 0), (64, 16), (100, 33), (500, 1)])
+def test_evicted_pages_under_chunks(dtype, D, window, sinks):
+    """Pages that no new token of a sequence sees are gone: what they hold and
+    their entries are not used, for few rows and for many."""
+    say(f"evicted pages D={D} {dtype} window={window} sinks={sinks}")
+    lens, news, page = [20, 333, 801, 1000, 1500], [3, 40, 1, 90, 300], 32
+    c = Cache(lens, news, 6, 2, D, page, dtype, seed=window)
+    for s, (n, new) in enumerate(zip(lens, news)):
+        for i in range(-(-n // page)):
+            if i * page >= sinks and (i + 1) * page - 1 <= n - new - window:
+                gone = int(c.table_h[s, i])
+                c.k[gone], c.v[gone] = float("nan"), float("inf")
+                c.table[s, i] = -1 if i % 2 else 2 ** 31 - 1
+    out = c.run(max_q=300, window=window, sinks=sinks)
+    c.check(out, (window, sinks), window=window, sinks=sinks, starts=False)
+    few = c.run(max_q=1, window=window, sinks=sinks)
+    c.check(few, (window, sinks, "few"), window=window, sinks=sinks, starts=False)
+
+
+@pytest.mark.parametrize("pages,Hkv", [(6, 1), (1, 2), (1, 1)])
+def test_caches_that_differ_where_no_stride_counts(pages, Hkv):
+    """One key head, or one page: the caches' strides along it may differ."""
+    import torch
+    page, D, n = 64, 64, min(pages * 64, 300)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(pages)
+    kc = torch.zeros((pages, Hkv, page, D), dtype=torch.bfloat16, device="cuda")
+    vc = torch.zeros((3 * pages, Hkv, page, D), dtype=torch.bfloat16, device="cuda")
+    vc = vc[::3] if pages == 1 else vc[:pages].reshape(pages, page, Hkv, D).transpose(1, 2)
+    assert kc.stride() != vc.stride() and kc.shape == vc.shape
+    q, k, v = (torch.randn((n, h, D), generator=gen, device="cuda").bfloat16()
+               for h in (4, Hkv, Hkv))
+    table = torch.randperm(pages, device="cuda").to(torch.int32)[None]
+    at = torch.arange(n, device="cuda")
+    slots = table[0].long()[at // page] * page + at % page
+    qh = fm.fastmax_cache_append(q, k, v, kc, vc, slots, None, None, None)
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    out = fm.fastmax_paged_fwd(qh[-1:], kc, vc, table, lens)
+    rows = [x[table[0].long()].transpose(0, 1).reshape(Hkv, -1, D)[:, :n] for x in (kc, vc)]
+    assert torch.equal(rows[1], v.transpose(0, 1))
+    g = 4 // Hkv
+    for h in range(Hkv):
+        hs = slice(g * h, g * h + g)
+        ref, bound = su.attend(su.np64(qh[-1:, hs]), su.np64(rows[0][h]), su.np64(rows[1][h]),
+                               np.array([n - 1]), 2, 1.0, 0, 0)
+        su.check(out[:, hs], ref, su.OUT["bf16"] * np.abs(ref) + 1.01 * bound, h)

@@ -8,8 +8,9 @@ validation, workspace plans, dispatch).
   build in a child process with gcc's ASan runtime preloaded.
 * The library is rebuilt with the sanitizers on its host code only
   (hipcc -Xarch_host ...; GPU code unchanged) and the host ABI tests
-  (tests/test_abi_host.py: every error path of every entry point, the
-  workspace sizing) run against it with clang's ASan runtime preloaded.
+  (tests/test_abi_host.py, tests/test_serve_host.py: every error path of
+  every entry point, the workspace sizing) run against it with clang's ASan
+  runtime preloaded.
 * A planted out-of-bounds read in a call of the sanitized oracle must be
   reported, which shows the runtime is really active.
 """
@@ -96,6 +97,19 @@ def test_library_host_code_under_asan_ubsan():
         build.build(sanitize=True)
     r = _child([sys.executable, "-m", "pytest", "-q", "-x", "-p", "no:cacheprovider",
                 "tests/test_abi_host.py"],
+               {"LD_PRELOAD": _clang_asan(), "FASTMAX_LIB": build.LIB_ASAN})
+    out = r.stdout + r.stderr
+    assert r.returncode == 0, out[-4000:]
+    assert "Sanitizer" not in out and "runtime error" not in out, out[-4000:]
+    assert " passed" in out
+
+
+def test_serving_host_code_under_asan_ubsan():
+    from paper_2402_07901_amd import build
+    if not _newer_than_sources(build.LIB_ASAN, build.CSRC):
+        build.build(sanitize=True)
+    r = _child([sys.executable, "-m", "pytest", "-q", "-x", "-p", "no:cacheprovider",
+                "tests/test_serve_host.py"],
                {"LD_PRELOAD": _clang_asan(), "FASTMAX_LIB": build.LIB_ASAN})
     out = r.stdout + r.stderr
     assert r.returncode == 0, out[-4000:]
