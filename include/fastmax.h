@@ -425,13 +425,15 @@ int fastmax_cache_append(const void *q, const void *k, const void *v,
  *   table    : int32 [S, table_cols]; lens: int32 [S]
  *   q_start  : int32 [S + 1], sequence s has the rows q_start[s] ..
  *              q_start[s + 1] - 1 of q; NULL: T = S, one row each
- *   max_q    : most rows of one sequence, max_len: longest sequence.  They
- *              size the grid; larger true values cost time, not correctness.
+ *   max_q    : most rows of one sequence (1 .. T), max_len: longest sequence.
+ *              They size the grid and the workspace; larger true values cost
+ *              time, not correctness.
  *   out      : [T, Hq, D] contiguous
  *   workspace: fastmax_paged_workspace_bytes with the same sizes
  * Weights are float32, in bf16 as two bf16 parts; sums are float32 and must fit
  * it (sum w |v| < 3e38).
- * A row that sees no key (lens[s] smaller than its new tokens) is 0.  What
+ * Rows of q that no sequence has are not written.  A row that sees no key
+ * (lens[s] smaller than its new tokens) is 0.  What
  * lies in slots that no row of a sequence sees is not used, whatever it
  * holds; entries of the page table past lens[s] or behind the window are not
  * read.  A row that sees a key whose entry is not a page is NaN, and so is

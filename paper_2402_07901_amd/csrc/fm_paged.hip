@@ -22,7 +22,7 @@
 // the number of heads that share it.  bf16, 32 heads to 8, D = 128: one sequence
 // of 131072 keys 99 to 102 us (5.3 TB/s, join included), 61 of 4096 186 us
 // (5.5), 61 of uneven lengths up to 8192 149 to 153 us (4.9: the last
-// workgroups run alone); float32, 32 windows of 4096 keys, D = 64: 99 us (5.4).
+// workgroups run alone); float32, 32 windows of 4096 keys, D = 64: 99 to 101 us (5.3).
 // One sequence of 777 keys, 12 heads of 64: 8.3 us, one launch.  Chunks of prompts with many
 // rows go to fm_paged_chunk.hip.
 #include <hip/hip_runtime.h>
@@ -583,7 +583,13 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
         // 12 against 17 a call); of 1024 keys, 8 heads of 128 13 against 9, so
         // split; 32 of 512 keys 15 against 19; 64 of up to 512, 4 heads of 64
         // 7.7 against 11; but 100 of up to 512, 8 heads of 128 26 against 18
-        // (four waves).  Under 256 keys four waves do: 60 keys 4.8, eight 5.4.
+        // (four waves).  Rows of at most 128 bytes (registers for more waves)
+        // take eight waves up to 1023 workgroups, against four and splits: bf16,
+        // 125 of 2048 keys, 8 heads of 64 95 against 105 (uneven: 43 against 51), of
+        // 1024 50 against 53 (26 against 24); 75 to 120 of 2048, heads of 32 36 against
+        // 40 (22 against 31), of 16 30 against 37; float32 heads of 32, 1024 keys 37
+        // against 41 (23 against 33); at 300 keys 12.5 against 11.4, 9.2 against 7.8
+        // and 9.8 against 8.5.  Under 256 keys four waves do: 60 keys 4.8, eight 5.4.
         const long long least = is_bf16 ? 64 : 32, row = (is_bf16 ? 2 : 4) * D;
         const bool one = base < 256 ? key_tiles * KT * row <= 128 << 10
                                     : key_tiles <= 2 * least && (base <= 512 || row <= 128);

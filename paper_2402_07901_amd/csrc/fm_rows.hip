@@ -14,9 +14,9 @@
 // tokens of one head, so that the head-major side is one contiguous run per
 // wave and the token-major side runs of D.  A lane keeps its token through a
 // run of heads: cos and sin are read once for all of them.  bf16, norm and
-// rotation: 4 x 8192 tokens, 16 heads of 64, forward 82 to 87 us (4.7 to 4.9 TB/s;
+// rotation: 4 x 8192 tokens, 16 heads of 64, forward 83 to 87 us (4.65 to 4.9 TB/s;
 // cards differ), backward 110 to 116 us with the weights' gradients; 16384
-// tokens of 32 and 8 heads of 128 appended in 82 to 88 us.  One token: 3.9 us, a launch.
+// tokens of 32 and 8 heads of 128 appended in 82 to 89 us.  One token: 3.9 us, a launch.
 #include <hip/hip_runtime.h>
 
 #include "fm_internal.h"

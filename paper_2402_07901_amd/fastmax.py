@@ -674,7 +674,8 @@ def fastmax_paged_fwd(q, k_cache, v_cache, table, lens, q_start=None, max_q=None
     caches [pages, Hkv, page, D]; table int32 [S, cols] of pages; lens int32 [S]
     tokens per sequence, its new ones last; q_start int32 [S + 1] where each
     sequence's rows of q begin (None: one row each).  max_q and max_len: the most
-    rows and the most tokens of a sequence (None: T, or what the table holds).
+    rows and the most tokens of a sequence (None: T, or what the table holds,
+    which costs time where sequences have less).
     window > 0: the last ``window`` keys and the first ``sinks`` only.  Returns
     O [T, Hq, D]."""
     _on_gpu(q, 3, "[T, Hq, D]")
