@@ -451,6 +451,50 @@ int fastmax_paged_fwd(const void *q, const fastmax_strides_t *q_strides, const v
                       fastmax_dtype_t dt, void *workspace, size_t workspace_bytes,
                       hipStream_t stream);
 
+/*
+ * The cache in 8 bits.  A row (a token's key or value of one head) is D codes
+ * -127 .. 127 and a float32 scale, amax / 127 for the row's largest magnitude
+ * amax; it stands for code * scale, off by at most amax / 254.  Rows with
+ * amax < 2^-100 are zeros (scale 0); a row that is not finite is NaN (scale
+ * NaN, codes 0).
+ *   k_cache, v_cache : int8, shapes and strides as above (multiples of 16)
+ *   k_scale, v_scale : float32 [pages, Hkv, page_size] contiguous
+ *
+ * fastmax_cache_append_q8 is fastmax_cache_append into such a cache: k^ and v
+ * are rounded once, from float32, code = rint(x (127 / amax)); q_out and
+ * everything else as there.
+ *
+ * fastmax_cache_read_q8 gives rows back: k, v [T, Hkv, D] contiguous in dt, what
+ * the slots' rows stand for; a slot outside the cache gives zeros.  The same
+ * slot may be asked for more than once.
+ *
+ * fastmax_paged_fwd_q8 is fastmax_paged_fwd over such a cache, dt the type of q
+ * and out.  q is taken as whole numbers of 16 bits (float32: 24) under a scale
+ * of its row, off by at most 2^-16 (2^-23) of the row's largest magnitude.  A
+ * row of q that is not finite gives NaN, and so does a key or value row that
+ * is, in the rows that see it and in no others.  Workspace:
+ * fastmax_paged_q8_workspace_bytes with the same sizes.
+ */
+int fastmax_cache_append_q8(const void *q, const void *k, const void *v,
+                            const fastmax_strides_t *strides, void *q_out, int8_t *k_cache,
+                            int8_t *v_cache, float *k_scale, float *v_scale,
+                            const fastmax_strides_t *cache, const int64_t *slots, int T, int Hq,
+                            int Hkv, int D, int pages, int page_size, const fastmax_rope_t *rope,
+                            fastmax_dtype_t dt, hipStream_t stream);
+int fastmax_cache_read_q8(const int8_t *k_cache, const int8_t *v_cache, const float *k_scale,
+                          const float *v_scale, const fastmax_strides_t *cache,
+                          const int64_t *slots, void *k, void *v, int T, int Hkv, int D, int pages,
+                          int page_size, fastmax_dtype_t dt, hipStream_t stream);
+size_t fastmax_paged_q8_workspace_bytes(int S, int T, int Hq, int Hkv, int D, int max_q,
+                                        int max_len, int window, int sinks, fastmax_dtype_t dt);
+int fastmax_paged_fwd_q8(const void *q, const fastmax_strides_t *q_strides, const int8_t *k_cache,
+                         const int8_t *v_cache, const float *k_scale, const float *v_scale,
+                         const fastmax_strides_t *cache, const int32_t *table, const int32_t *lens,
+                         const int32_t *q_start, void *out, int S, int T, int Hq, int Hkv, int D,
+                         int pages, int page_size, int table_cols, int max_q, int max_len, int p,
+                         float qk_scale, int window, int sinks, fastmax_dtype_t dt, void *workspace,
+                         size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,6 +15,7 @@ int code_of(hipError_t e);
 namespace {
 
 constexpr int NO_WINDOW = 1 << 30;   // wider than any sequence
+constexpr int CODES = 2;             // 8-bit rows, beside the fastmax_dtype_t
 
 bool supported_d(int D) { return D == 16 || D == 32 || D == 64 || D == 128; }
 bool aligned(const void *p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
@@ -86,7 +87,7 @@ int check_strides(const fastmax_strides_t *s, int B, int N, int H, int D, int dt
     for (int i = 0; i < 3; ++i) {
         if (st[i] < 0 || st[i] > (1LL << 46)) return FASTMAX_EINVAL;
         if (rows_apart && n[i] > 1 && st[i] < D) return FASTMAX_EINVAL;
-        if (st[i] % (dt == FASTMAX_BF16 ? 8 : 4)) return FASTMAX_EALIGN;
+        if (st[i] % (dt == CODES ? 16 : dt == FASTMAX_BF16 ? 8 : 4)) return FASTMAX_EALIGN;
     }
     *out = {st[0], st[1], st[2]};
     return FASTMAX_OK;
@@ -136,6 +137,81 @@ int check_paged(int S, int T, int Hq, int Hkv, int D, int max_q, int max_len, in
     if (S < 1 || S > 65535 || max_q < 1 || max_q > T || max_len < 1 || max_len > (1 << 30)) return FASTMAX_EINVAL;
     if (window < 0 || sinks < 0 || (long long)T * Hq > INT_MAX / 2) return FASTMAX_EINVAL;
     return FASTMAX_OK;
+}
+
+// The append's arguments; cache_dt: what the cache holds.
+int check_append(fm::RowsArgs *a, const void *q, const void *k, const void *v, const fastmax_strides_t *strides,
+                 void *q_out, void *k_cache, void *v_cache, const fastmax_strides_t *cache, const int64_t *slots,
+                 int T, int Hq, int Hkv, int D, int pages, int page_size, const fastmax_rope_t *rope, int dt,
+                 int cache_dt, hipStream_t stream)
+{
+    int rc = check_sizes(T, Hq, Hkv, D, dt);
+    if (rc != FASTMAX_OK) return rc;
+    if ((rc = check_rope(rope, D, &a->rope)) != FASTMAX_OK) return rc;
+    if ((rc = check_rows(strides, 3, 1, T, Hq, Hkv, D, dt, false, &a->qs, &a->ks, &a->vs)) != FASTMAX_OK) return rc;
+    if ((rc = check_cache(cache, Hkv, D, pages, page_size, cache_dt, true, &a->cache, &a->page_shift)) != FASTMAX_OK)
+        return rc;
+    const void *ptrs[] = {q, k, v, q_out, k_cache, v_cache};
+    if ((rc = check_ptrs(ptrs, 6)) != FASTMAX_OK) return rc;
+    if (!slots) return FASTMAX_ENULL;
+    if (!aligned(slots, 8)) return FASTMAX_EALIGN;
+    if ((rc = fm::check_stream(stream)) != FASTMAX_OK) return rc;
+    a->q = q, a->k = k, a->v = v, a->oq = q_out, a->ok = k_cache, a->ov = v_cache;
+    a->B = 1, a->N = T, a->Hq = Hq, a->Hkv = Hkv;
+    a->slots = slots, a->pages = pages;
+    return FASTMAX_OK;
+}
+
+// The plan of a paged call whose sizes are checked.
+fm::PagedPlan plan_of(bool q8, int S, int Hq, int Hkv, int D, int max_q, int max_len, int window, int sinks, int dt)
+{
+    const int wide = window && window < NO_WINDOW ? window : NO_WINDOW;
+    const int bf16 = dt == FASTMAX_BF16;
+    if (q8) return fm::paged_q8_plan(S, Hq, Hkv, D, bf16, max_q, max_len, wide, sinks);
+    return fm::paged_plan(S, Hq, Hkv, D, bf16, max_q, max_len, wide, sinks, !bf16 && D == 128 ? 32 : 64);
+}
+
+// The paged attention's arguments; cache_dt: what the cache holds.
+int check_paged_call(fm::PagedArgs *a, fm::PagedPlan *plan, const void *q, const fastmax_strides_t *q_strides,
+                     const void *k_cache, const void *v_cache, const fastmax_strides_t *cache, const int32_t *table,
+                     const int32_t *lens, const int32_t *q_start, void *out, int S, int T, int Hq, int Hkv, int D,
+                     int pages, int page_size, int table_cols, int max_q, int max_len, int p, float qk_scale,
+                     int window, int sinks, int dt, int cache_dt, void *workspace, size_t workspace_bytes,
+                     hipStream_t stream)
+{
+    int rc = check_paged(S, T, Hq, Hkv, D, max_q, max_len, window, sinks, dt);
+    if (rc != FASTMAX_OK) return rc;
+    if (p != 1 && p != 2) return FASTMAX_EINVAL;
+    if (!(qk_scale > 0.0f && qk_scale <= 1.0f)) return FASTMAX_EINVAL;
+    if (!q_start && (T != S || max_q != 1)) return FASTMAX_EINVAL;
+    if ((rc = check_cache(cache, Hkv, D, pages, page_size, cache_dt, false, &a->cache, &a->page_shift)) != FASTMAX_OK)
+        return rc;
+    if (table_cols < 1 || (long long)table_cols * page_size > (1 << 30)) return FASTMAX_EINVAL;
+    fm::Strides qs;
+    if ((rc = check_strides(q_strides, 1, T, Hq, D, dt, false, &qs)) != FASTMAX_OK) return rc;
+    const void *ptrs[] = {q, k_cache, v_cache, out};
+    if ((rc = check_ptrs(ptrs, 4)) != FASTMAX_OK) return rc;
+    if (!table || !lens) return FASTMAX_ENULL;
+    if (!aligned(table, 4) || !aligned(lens, 4) || !aligned(q_start, 4)) return FASTMAX_EALIGN;
+    *plan = plan_of(cache_dt == CODES, S, Hq, Hkv, D, max_q, max_len, window, sinks, dt);
+    const size_t need = fm::paged_workspace(*plan, T, Hq, D);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return FASTMAX_EWORKSPACE;
+    if (workspace && !aligned(workspace, 16)) return FASTMAX_EALIGN;
+    if ((rc = fm::check_stream(stream)) != FASTMAX_OK) return rc;
+    a->q = q, a->k = k_cache, a->v = v_cache, a->out = out;
+    a->q_token = qs.token, a->q_head = qs.head;
+    a->table = table, a->lens = lens, a->q_start = q_start;
+    a->S = S, a->T = T, a->Hq = Hq, a->Hkv = Hkv, a->group = Hq / Hkv;
+    a->pages = pages, a->table_cols = table_cols;
+    a->window = window && window < NO_WINDOW ? window : NO_WINDOW, a->sinks = sinks;
+    a->c1 = qk_scale, a->c2 = p == 2 ? 0.5f * qk_scale * qk_scale : 0.0f;
+    return FASTMAX_OK;
+}
+
+size_t paged_bytes(bool q8, int S, int T, int Hq, int Hkv, int D, int max_q, int max_len, int window, int sinks, int dt)
+{
+    if (check_paged(S, T, Hq, Hkv, D, max_q, max_len, window, sinks, dt) != FASTMAX_OK) return 0;
+    return fm::paged_workspace(plan_of(q8, S, Hq, Hkv, D, max_q, max_len, window, sinks, dt), T, Hq, D);
 }
 
 }  // namespace
@@ -200,32 +276,60 @@ int fastmax_cache_append(const void *q, const void *k, const void *v, const fast
                          const fastmax_rope_t *rope, fastmax_dtype_t dt_arg, hipStream_t stream)
 {
     const int dt = dt_bits(&dt_arg);
-    int rc = check_sizes(T, Hq, Hkv, D, dt);
-    if (rc != FASTMAX_OK) return rc;
     fm::RowsArgs a = {};
-    if ((rc = check_rope(rope, D, &a.rope)) != FASTMAX_OK) return rc;
-    if ((rc = check_rows(strides, 3, 1, T, Hq, Hkv, D, dt, false, &a.qs, &a.ks, &a.vs)) != FASTMAX_OK) return rc;
-    if ((rc = check_cache(cache, Hkv, D, pages, page_size, dt, true, &a.cache, &a.page_shift)) != FASTMAX_OK)
+    const int rc = check_append(&a, q, k, v, strides, q_out, k_cache, v_cache, cache, slots, T, Hq, Hkv, D, pages,
+                                page_size, rope, dt, dt, stream);
+    return rc != FASTMAX_OK ? rc : fm::code_of(fm::cache_append(a, D, dt == FASTMAX_BF16, stream));
+}
+
+int fastmax_cache_append_q8(const void *q, const void *k, const void *v, const fastmax_strides_t *strides,
+                            void *q_out, int8_t *k_cache, int8_t *v_cache, float *k_scale, float *v_scale,
+                            const fastmax_strides_t *cache, const int64_t *slots, int T, int Hq, int Hkv, int D,
+                            int pages, int page_size, const fastmax_rope_t *rope, fastmax_dtype_t dt_arg,
+                            hipStream_t stream)
+{
+    const int dt = dt_bits(&dt_arg);
+    const void *scales[] = {k_scale, v_scale};
+    fm::RowsArgs a = {};
+    int rc = check_append(&a, q, k, v, strides, q_out, k_cache, v_cache, cache, slots, T, Hq, Hkv, D, pages,
+                          page_size, rope, dt, CODES, stream);
+    if (rc == FASTMAX_OK) rc = check_ptrs(scales, 2);
+    if (rc != FASTMAX_OK) return rc;
+    a.k_scale = k_scale, a.v_scale = v_scale;
+    return fm::code_of(fm::cache_append_q8(a, D, dt == FASTMAX_BF16, stream));
+}
+
+int fastmax_cache_read_q8(const int8_t *k_cache, const int8_t *v_cache, const float *k_scale, const float *v_scale,
+                          const fastmax_strides_t *cache, const int64_t *slots, void *k, void *v, int T, int Hkv,
+                          int D, int pages, int page_size, fastmax_dtype_t dt_arg, hipStream_t stream)
+{
+    const int dt = dt_bits(&dt_arg);
+    int rc = check_sizes(T, Hkv, Hkv, D, dt);
+    if (rc != FASTMAX_OK) return rc;
+    fm::ReadArgs a = {};
+    if ((rc = check_cache(cache, Hkv, D, pages, page_size, CODES, false, &a.cache, &a.page_shift)) != FASTMAX_OK)
         return rc;
-    const void *ptrs[] = {q, k, v, q_out, k_cache, v_cache};
+    const void *ptrs[] = {k_cache, v_cache, k_scale, v_scale, k, v};
     if ((rc = check_ptrs(ptrs, 6)) != FASTMAX_OK) return rc;
     if (!slots) return FASTMAX_ENULL;
     if (!aligned(slots, 8)) return FASTMAX_EALIGN;
     if ((rc = fm::check_stream(stream)) != FASTMAX_OK) return rc;
-    a.q = q, a.k = k, a.v = v, a.oq = q_out, a.ok = k_cache, a.ov = v_cache;
-    a.B = 1, a.N = T, a.Hq = Hq, a.Hkv = Hkv;
-    a.slots = slots, a.pages = pages;
-    return fm::code_of(fm::cache_append(a, D, dt == FASTMAX_BF16, stream));
+    a.k = k_cache, a.v = v_cache, a.k_scale = k_scale, a.v_scale = v_scale;
+    a.slots = slots, a.ok = k, a.ov = v;
+    a.T = T, a.Hkv = Hkv, a.pages = pages;
+    return fm::code_of(fm::cache_read_q8(a, D, dt == FASTMAX_BF16, stream));
 }
 
 size_t fastmax_paged_workspace_bytes(int S, int T, int Hq, int Hkv, int D, int max_q, int max_len, int window,
                                      int sinks, fastmax_dtype_t dt_arg)
 {
-    const int dt = dt_bits(&dt_arg);
-    if (check_paged(S, T, Hq, Hkv, D, max_q, max_len, window, sinks, dt) != FASTMAX_OK) return 0;
-    const fm::PagedPlan plan = fm::paged_plan(S, Hq, Hkv, D, dt == FASTMAX_BF16, max_q, max_len,
-                                              window ? window : NO_WINDOW, sinks);
-    return fm::paged_workspace(plan, T, Hq, D);
+    return paged_bytes(false, S, T, Hq, Hkv, D, max_q, max_len, window, sinks, dt_bits(&dt_arg));
+}
+
+size_t fastmax_paged_q8_workspace_bytes(int S, int T, int Hq, int Hkv, int D, int max_q, int max_len, int window,
+                                        int sinks, fastmax_dtype_t dt_arg)
+{
+    return paged_bytes(true, S, T, Hq, Hkv, D, max_q, max_len, window, sinks, dt_bits(&dt_arg));
 }
 
 int fastmax_paged_fwd(const void *q, const fastmax_strides_t *q_strides, const void *k_cache, const void *v_cache,
@@ -236,35 +340,33 @@ int fastmax_paged_fwd(const void *q, const fastmax_strides_t *q_strides, const v
                       hipStream_t stream)
 {
     const int dt = dt_bits(&dt_arg);
-    int rc = check_paged(S, T, Hq, Hkv, D, max_q, max_len, window, sinks, dt);
-    if (rc != FASTMAX_OK) return rc;
-    if (p != 1 && p != 2) return FASTMAX_EINVAL;
-    if (!(qk_scale > 0.0f && qk_scale <= 1.0f)) return FASTMAX_EINVAL;
-    if (!q_start && (T != S || max_q != 1)) return FASTMAX_EINVAL;
     fm::PagedArgs a = {};
-    if ((rc = check_cache(cache, Hkv, D, pages, page_size, dt, false, &a.cache, &a.page_shift)) != FASTMAX_OK)
-        return rc;
-    if (table_cols < 1 || (long long)table_cols * page_size > (1 << 30)) return FASTMAX_EINVAL;
-    fm::Strides qs;
-    if ((rc = check_strides(q_strides, 1, T, Hq, D, dt, false, &qs)) != FASTMAX_OK) return rc;
-    const void *ptrs[] = {q, k_cache, v_cache, out};
-    if ((rc = check_ptrs(ptrs, 4)) != FASTMAX_OK) return rc;
-    if (!table || !lens) return FASTMAX_ENULL;
-    if (!aligned(table, 4) || !aligned(lens, 4) || !aligned(q_start, 4)) return FASTMAX_EALIGN;
-    const int wide = window && window < NO_WINDOW ? window : NO_WINDOW;
-    const fm::PagedPlan plan = fm::paged_plan(S, Hq, Hkv, D, dt == FASTMAX_BF16, max_q, max_len, wide, sinks);
-    const size_t need = fm::paged_workspace(plan, T, Hq, D);
-    if (need > 0 && (!workspace || workspace_bytes < need)) return FASTMAX_EWORKSPACE;
-    if (workspace && !aligned(workspace, 16)) return FASTMAX_EALIGN;
-    if ((rc = fm::check_stream(stream)) != FASTMAX_OK) return rc;
-    a.q = q, a.k = k_cache, a.v = v_cache, a.out = out;
-    a.q_token = qs.token, a.q_head = qs.head;
-    a.table = table, a.lens = lens, a.q_start = q_start;
-    a.S = S, a.T = T, a.Hq = Hq, a.Hkv = Hkv, a.group = Hq / Hkv;
-    a.pages = pages, a.table_cols = table_cols;
-    a.window = wide, a.sinks = sinks;
-    a.c1 = qk_scale, a.c2 = p == 2 ? 0.5f * qk_scale * qk_scale : 0.0f;
-    return fm::code_of(fm::paged_fwd(a, plan, D, dt == FASTMAX_BF16, workspace, stream));
+    fm::PagedPlan plan;
+    const int rc = check_paged_call(&a, &plan, q, q_strides, k_cache, v_cache, cache, table, lens, q_start, out, S, T,
+                                    Hq, Hkv, D, pages, page_size, table_cols, max_q, max_len, p, qk_scale, window,
+                                    sinks, dt, dt, workspace, workspace_bytes, stream);
+    return rc != FASTMAX_OK ? rc : fm::code_of(fm::paged_fwd(a, plan, D, dt == FASTMAX_BF16, workspace, stream));
+}
+
+int fastmax_paged_fwd_q8(const void *q, const fastmax_strides_t *q_strides, const int8_t *k_cache,
+                         const int8_t *v_cache, const float *k_scale, const float *v_scale,
+                         const fastmax_strides_t *cache, const int32_t *table, const int32_t *lens,
+                         const int32_t *q_start, void *out, int S, int T, int Hq, int Hkv, int D, int pages,
+                         int page_size, int table_cols, int max_q, int max_len, int p, float qk_scale, int window,
+                         int sinks, fastmax_dtype_t dt_arg, void *workspace, size_t workspace_bytes,
+                         hipStream_t stream)
+{
+    const int dt = dt_bits(&dt_arg);
+    const void *scales[] = {k_scale, v_scale};
+    fm::PagedArgs a = {};
+    fm::PagedPlan plan;
+    int rc = check_paged_call(&a, &plan, q, q_strides, k_cache, v_cache, cache, table, lens, q_start, out, S, T, Hq,
+                              Hkv, D, pages, page_size, table_cols, max_q, max_len, p, qk_scale, window, sinks, dt,
+                              CODES, workspace, workspace_bytes, stream);
+    if (rc == FASTMAX_OK) rc = check_ptrs(scales, 2);
+    if (rc != FASTMAX_OK) return rc;
+    a.k_scale = k_scale, a.v_scale = v_scale;
+    return fm::code_of(fm::paged_q8_fwd(a, plan, D, dt == FASTMAX_BF16, workspace, stream));
 }
 
 }  // extern "C"

@@ -484,6 +484,19 @@ __global__ __launch_bounds__(THREADS) void join_kernel(PagedArgs a, PagedPlan pl
     }
 }
 
+template <typename T, int D>
+hipError_t join(const PagedArgs &a, const PagedPlan &plan, const float *part, hipStream_t st)
+{
+    // a workgroup to a row where there are more splits than a wave has in flight
+    const int per = plan.splits > 16 ? 1 : WAVES;
+    const long long rows = (long long)plan.rows * plan.tiles / a.group * a.Hq;
+    const long long most = (long long)a.T * a.Hq;   // of one sequence
+    const dim3 grid((unsigned)(((rows < most ? rows : most) + per - 1) / per), (unsigned)a.S);
+    if (per == 1) join_kernel<T, D, WAVES><<<grid, THREADS, 0, st>>>(a, plan, part);
+    else join_kernel<T, D, 1><<<grid, THREADS, 0, st>>>(a, plan, part);
+    return hipGetLastError();
+}
+
 template <typename T, int D, int RT, int W = WAVES>
 hipError_t launch_rt(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
 {
@@ -505,14 +518,7 @@ hipError_t launch(const PagedArgs &a, const PagedPlan &plan, float *part, hipStr
     else if constexpr (sizeof(T) * D <= 256) e = launch_rt<T, D, 4>(a, plan, part, st);
     else e = hipErrorInvalidValue;   // no plan has such rows
     if (e != hipSuccess || plan.splits == 1) return e;
-    // a workgroup to a row where there are more splits than a wave has in flight
-    const int per = plan.splits > 16 ? 1 : WAVES;
-    const long long rows = (long long)plan.rows * plan.tiles / a.group * a.Hq;
-    const long long most = (long long)a.T * a.Hq;   // of one sequence
-    const dim3 grid((unsigned)(((rows < most ? rows : most) + per - 1) / per), (unsigned)a.S);
-    if (per == 1) join_kernel<T, D, WAVES><<<grid, THREADS, 0, st>>>(a, plan, part);
-    else join_kernel<T, D, 1><<<grid, THREADS, 0, st>>>(a, plan, part);
-    return hipGetLastError();
+    return join<T, D>(a, plan, part, st);
 }
 
 template <typename T> hipError_t launch_d(const PagedArgs &a, const PagedPlan &plan, int D, float *part, hipStream_t st)
@@ -528,7 +534,7 @@ template <typename T> hipError_t launch_d(const PagedArgs &a, const PagedPlan &p
 }  // namespace
 
 PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int max_len, int window,
-                     int sinks)
+                     int sinks, int most_rows)
 {
     PagedPlan plan;
     const long long rows = (long long)max_q * (Hq / Hkv);
@@ -539,7 +545,7 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
     // D = 128 154 against 129, D = 64 84 against 61; 128 rows D = 128 49 against
     // 50 and more beyond.  Single tokens stay here whatever their heads.
     plan.chunk_kernel = D >= 32 && max_q > 1 && (rows > 64 || (rows > 32 && is_bf16 && D >= 64));
-    plan.rows = plan.chunk_kernel ? CHUNK_ROWS : rows <= 16 ? 16 : rows <= 32 || (!is_bf16 && D == 128) ? 32 : 64;
+    plan.rows = plan.chunk_kernel ? CHUNK_ROWS : rows <= 16 ? 16 : rows <= 32 || most_rows == 32 ? 32 : 64;
     plan.waves = WAVES;
     // max_q holds for the longest sequence and may be all of T, so most row tiles
     // of a grid may be empty: past 2^18 workgroups it has no more of them, and
@@ -613,6 +619,21 @@ PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int 
 size_t paged_workspace(const PagedPlan &plan, int T, int Hq, int D)
 {
     return plan.splits == 1 ? 0 : (size_t)T * Hq * plan.splits * (D + 1) * sizeof(float);
+}
+
+template <typename T> static hipError_t join_d(const PagedArgs &a, const PagedPlan &plan, int D, const float *part, hipStream_t st)
+{
+    switch (D) {
+    case 16: return join<T, 16>(a, plan, part, st);
+    case 32: return join<T, 32>(a, plan, part, st);
+    case 64: return join<T, 64>(a, plan, part, st);
+    default: return join<T, 128>(a, plan, part, st);
+    }
+}
+
+hipError_t paged_join(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, const float *part, hipStream_t st)
+{
+    return is_bf16 ? join_d<bf16_t>(a, plan, D, part, st) : join_d<float>(a, plan, D, part, st);
 }
 
 hipError_t paged_fwd(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, void *ws, hipStream_t st)

@@ -1,0 +1,713 @@
+// Fastmax attention of new tokens over a paged cache of 8-bit rows: key n is
+// ks_n c_n, value n is vs_n e_n with codes c_n, e_n of -127 .. 127 and a float32
+// scale each (fm_paged.hip has the formulas and what a row sees).
+//
+// Scores take the codes as they are: q^ of a row becomes one 16-bit (float32: 24-bit)
+// whole number per channel under a scale of its row, cut in signed bytes, and
+// int8 MFMA gives exact sums,
+//     q^ = qs (256 a + b)  ->  s = qs ks (256 a.c + b.c),
+// two products of int8 at the price of one in bf16; q^ is off by at most 2^-16
+// (2^-23) of the row's largest magnitude.  Values: weights times vs in two bf16
+// parts (float32: three) against the codes, which bf16 holds exactly.  A code is
+// always a number, so what unseen slots hold needs no care beyond their scales,
+// which a select keeps out.
+//
+// Single tokens: HBM bounds it, D + 4 bytes a row.  A wave walks over key tiles of
+// 16, two at a time, straight from the cache into registers, as fm_paged.hip.
+#include <hip/hip_runtime.h>
+
+#include "fm_internal.h"
+#include "fm_paged.h"
+#include "fm_rows.h"
+#include "fm_serve.h"
+
+namespace fm {
+namespace {
+
+using namespace paged;
+
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef int i4 __attribute__((ext_vector_type(4)));
+typedef int i16v __attribute__((ext_vector_type(16)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+constexpr int WAVES = 4, THREADS = 64 * WAVES;
+
+// Bytes of a whole number of q^, and bf16 parts of a weight.
+template <typename T> constexpr int PARTS = sizeof(T) == 2 ? 2 : 3;
+
+// Largest over the four rows of 16 lanes, in every lane.
+__device__ __forceinline__ uint32_t rows4_max(uint32_t x)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(a[0], a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max(b[0], b[1]);
+}
+__device__ __forceinline__ uint32_t halves_max(uint32_t x)
+{
+    const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max(b[0], b[1]);
+}
+__device__ __forceinline__ float halves_sum(float x)
+{
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+template <int N> __device__ __forceinline__ uint32_t abs_max(const float *x)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    return top;
+}
+
+// A row's whole numbers: the factor from its values, and the scale back.  The
+// largest magnitude (float32 bits) becomes M, whose bytes are at most 127 (24
+// bits: with room for the product's rounding).  A row that is not finite has no
+// numbers (NaN); below 2^-100 it is 0.
+template <int NP> __device__ __forceinline__ float2 whole_scale(uint32_t top)
+{
+    constexpr float M = NP == 2 ? 32639.0f : 8355584.0f;
+    const float amax = __uint_as_float(top);
+    if (top >= 0x7f800000u) return make_float2(0.f, __builtin_nanf(""));
+    if (amax < Q8_LEAST) return make_float2(0.f, 0.f);
+    return make_float2(M / amax, amax / M);
+}
+
+// Four values as whole numbers, byte p of each in word p (the highest first).
+template <int NP> __device__ __forceinline__ void whole4(const float *x, float f, uint32_t *w)
+{
+#pragma unroll
+    for (int p = 0; p < NP; ++p) w[p] = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float y = x[i] * f;
+        int n = y == y ? __float2int_rn(y) : 0;
+#pragma unroll
+        for (int p = NP - 1; p >= 0; --p) {
+            const int b = (int)(int8_t)n;
+            w[p] |= (uint32_t)(b & 255) << (8 * i);
+            n = (n - b) >> 8;
+        }
+    }
+}
+
+// Byte j of two words as two bf16 (whole numbers up to 127 have few bits).
+__device__ __forceinline__ uint32_t codes2(uint32_t a, uint32_t b, int j)
+{
+    const float x = (float)(int8_t)(a >> (8 * j)), y = (float)(int8_t)(b >> (8 * j));
+    return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+}
+
+// Two weights as NP pairs of bf16 parts, each the rest of the ones before it.
+template <int NP> __device__ __forceinline__ void parts2(float x, float y, uint32_t *p)
+{
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        p[i] = rows::pack2(x, y);
+        x -= __uint_as_float(p[i] << 16);
+        y -= __uint_as_float(p[i] & 0xffff0000u);
+    }
+}
+
+template <int N, typename T> __device__ __forceinline__ void ld_row(const T *p, float *x)
+{
+#pragma unroll
+    for (int i = 0; i < N; i += 8) rows::ld8(p + i, x + i);
+}
+
+// --- few rows -------------------------------------------------------------------
+
+// 16x16x64 int8 (D >= 64: a lane of row h holds channels 64 c + 16 h .. + 15) or
+// 16x16x32 (channels 8 h .. 8 h + 7; D = 16: rows 0 and 1 only).
+template <typename T, int D> struct Few {
+    static constexpr int NP = PARTS<T>;
+    static constexpr int QC = D >= 64 ? D / 64 : 1, QB = D >= 64 ? 16 : 8;   // pieces, bytes of one
+    static constexpr int VW = D / 16;
+    struct Q { u4 x[NP][QC]; float scale; };
+    struct K { u4 x[QC]; };
+    struct V { uint32_t x[8][VW > 4 ? 2 : 1]; };
+
+    static __device__ __forceinline__ void ld_q(const T *p, int h, Q &q)
+    {
+        float x[QC][QB];
+        uint32_t top = 0;
+        const bool in = D >= 32 || h < 2;
+#pragma unroll
+        for (int c = 0; c < QC; ++c) {
+            ld_row<QB>(p + (in ? 64 * c + QB * h : 0), x[c]);
+            top = max(top, abs_max<QB>(x[c]));
+        }
+        const float2 f = whole_scale<NP>(rows4_max(top));
+        q.scale = f.y;
+#pragma unroll
+        for (int c = 0; c < QC; ++c) {
+#pragma unroll
+            for (int i = 0; i < QB / 4; ++i) {
+                uint32_t w[NP];
+                whole4<NP>(x[c] + 4 * i, f.x, w);
+#pragma unroll
+                for (int n = 0; n < NP; ++n) q.x[n][c][i] = in ? w[n] : 0u;
+            }
+        }
+    }
+    static __device__ __forceinline__ void ld_k(const int8_t *p, int h, K &k)
+    {
+        if constexpr (D >= 64) {
+#pragma unroll
+            for (int c = 0; c < QC; ++c) k.x[c] = *(const u4 *)(p + 64 * c + 16 * h);
+        } else {
+            // D = 16: the queries' bytes are 0 where h > 1
+            const uint2 u = *(const uint2 *)(p + (D == 16 ? h & 1 : h) * 8);
+            k.x[0] = u4{u.x, u.y, 0, 0};
+        }
+    }
+    static __device__ __forceinline__ i4 mma(const K &k, const u4 *q, i4 s)
+    {
+#pragma unroll
+        for (int c = 0; c < QC; ++c) {
+            if constexpr (D >= 64) {
+                s = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i4, k.x[c]), __builtin_bit_cast(i4, q[c]),
+                                                          s, 0, 0, 0);
+            } else {
+                const uint2 a = make_uint2(k.x[c][0], k.x[c][1]), b = make_uint2(q[c][0], q[c][1]);
+                s = __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, a), __builtin_bit_cast(long, b), s,
+                                                          0, 0, 0);
+            }
+        }
+        return s;
+    }
+    // Sums of products of the whole numbers: |256 a.c + b.c| < 2^30.
+    static __device__ __forceinline__ f4 scores(const K &k, const Q &q)
+    {
+        const i4 z = {0, 0, 0, 0};
+        const i4 s = mma(k, q.x[1], mma(k, q.x[0], z) << 8);
+        f4 r;
+        if constexpr (NP == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = (float)s[i];
+        } else {
+            const i4 l = mma(k, q.x[2], z);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = fmaf((float)s[i], 256.0f, (float)l[i]);
+        }
+        return r;
+    }
+    // key i of the lane's eight: tile i / 4, key 4 h + i % 4
+    static __device__ __forceinline__ void ld_v(const int8_t *p, int r16, uint32_t *x)
+    {
+        p += r16 * VW;
+        if constexpr (VW == 8) {
+            const uint2 u = *(const uint2 *)p;
+            x[0] = u.x; x[1] = u.y;
+        } else if constexpr (VW == 4) {
+            x[0] = *(const uint32_t *)p;
+        } else if constexpr (VW == 2) {
+            x[0] = *(const uint16_t *)p;
+        } else {
+            x[0] = *(const uint8_t *)p;
+        }
+    }
+    // acc[j] += V^T W^T for channel r16 VW + j
+    static __device__ __forceinline__ void add(f4 *acc, const V &v, const f4 *w)
+    {
+        u4 b[NP];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t p[NP];
+            parts2<NP>(w[i / 2][2 * (i % 2)], w[i / 2][2 * (i % 2) + 1], p);
+#pragma unroll
+            for (int n = 0; n < NP; ++n) b[n][i] = p[n];
+        }
+#pragma unroll
+        for (int j = 0; j < VW; ++j) {
+            u4 x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = codes2(v.x[2 * i][j / 4], v.x[2 * i + 1][j / 4], j % 4);
+#pragma unroll
+            for (int n = NP - 1; n >= 0; --n)
+                acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, x), __builtin_bit_cast(b8, b[n]),
+                                                                 acc[j], 0, 0, 0);
+        }
+    }
+};
+
+template <typename T, int D, int RT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void few_kernel(PagedArgs a, PagedPlan plan, float *part)
+{
+    using M = Few<T, D>;
+    constexpr int VW = M::VW, ROWS = 16 * RT, RS = D + 4;
+    __shared__ float red[WAVES][16][RS];
+    __shared__ float gred[WAVES][16];
+
+    // Splits last: later ones are empty in shorter sequences, and workgroups are
+    // dealt out to the XCDs in turn.
+    int id = blockIdx.x;
+    const int head = id % a.Hkv;
+    id /= a.Hkv;
+    const int s = id % a.S;
+    id /= a.S;
+    const int tile0 = id % plan.tiles, split = id / plan.tiles;
+    const int wave = scalar(threadIdx.x / 64), lane = threadIdx.x % 64, h = lane / 16, r16 = lane % 16;
+    const Seq seq = seq_of(a, s);
+    const int rows = seq.count * a.group, page_mask = (1 << a.page_shift) - 1;
+    const int8_t *kc = (const int8_t *)a.k + head * a.cache.head, *vc = (const int8_t *)a.v + head * a.cache.head;
+    const int32_t *table = a.table + (size_t)s * a.table_cols;
+    const int token = (int)a.cache.token;
+
+    // max_q sets the grid; a sequence with more new tokens goes round again
+    for (int r0 = tile0 * ROWS; r0 < rows; r0 += plan.tiles * ROWS) {
+        const Span sp = scalar(span_of_rows(a, seq, r0, ROWS));
+        const int begin = split * plan.chunk;
+        const int end = split == plan.splits - 1 ? sp.tiles : min(sp.tiles, begin + plan.chunk);
+        if (begin >= sp.tiles && split > 0) continue;   // the join knows
+
+        typename M::Q q[RT];
+        int pos[RT];
+        float c1[RT], c2[RT], g[RT];
+        f4 acc[RT][VW];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int row = min(r0 + 16 * r + r16, rows - 1);
+            const int t = row / a.group;
+            pos[r] = seq.len - seq.count + t;
+            M::ld_q((const T *)a.q + (seq.t0 + t) * a.q_token + (head * a.group + row - t * a.group) * a.q_head, h, q[r]);
+            c1[r] = a.c1 * q[r].scale;
+            c2[r] = a.c2 * q[r].scale * q[r].scale;
+            g[r] = 0.f;
+#pragma unroll
+            for (int j = 0; j < VW; ++j) acc[r][j] = f4{0.f, 0.f, 0.f, 0.f};
+        }
+        const int first = scalar(seq.len - seq.count + r0 / a.group), last = sp.end - 1;
+        // Key tiles [whole, whole_end) exist in full and every row sees all their
+        // keys; elsewhere weights are masked.
+        const int shift = sp.low - sp.sink_tiles;   // from a tile's number here to its own
+        const int whole = a.window < sp.end ? max(sp.sink_tiles, (last - a.window) / KT + 1 - shift) : 0;
+        const int whole_end = min(end, (first + 1) / KT - shift);
+        bool bad = seq.cut;
+
+        // The wave's steps of two key tiles, 32 steps at a time, their pages a
+        // tile to a lane, so that no step waits for the page table.
+        for (int b0 = begin + 2 * wave; b0 < end; b0 += 64 * WAVES) {
+            const int mine = sp.tile(min(b0 + lane / 2 * (2 * WAVES) + lane % 2, end - 1)) * KT;
+            int page = table[mine >> a.page_shift];
+            if ((unsigned)page >= (unsigned)a.pages) {
+                bad = true;
+                page = 0;
+            }
+            for (int n = 0; n < 32; ++n) {
+                const int i0 = b0 + n * (2 * WAVES);
+                if (i0 >= end) break;
+                typename M::K k[2];
+                typename M::V v;
+                f4 ks[2], vs[2];
+                const bool all = i0 >= whole && i0 + 2 <= whole_end;
+                int base[2];   // of the key tiles; past every position if there is none
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const long long pg = __builtin_amdgcn_readlane(page, 2 * n + i);
+                    const int n0 = sp.tile(min(i0 + i, end - 1)) * KT, place = n0 & page_mask;
+                    const long long from = pg * a.cache.batch + place * a.cache.token;
+                    const long long at = ((pg * a.Hkv + head) << a.page_shift) + place;
+                    base[i] = i0 + i < end ? n0 : INT32_MAX - KT;
+                    M::ld_k(kc + from + r16 * token, h, k[i]);
+                    ks[i] = *(const f4 *)(a.k_scale + at + 4 * h);
+                    vs[i] = *(const f4 *)(a.v_scale + at + 4 * h);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) M::ld_v(vc + from + (4 * h + j) * token, r16, v.x[4 * i + j]);
+                }
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    f4 w[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const f4 x = M::scores(k[i], q[r]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float y = x[j] * ks[i][j];
+                            float f = fmaf(fmaf(y, c2[r], c1[r]), y, 1.0f), fv = f * vs[i][j];
+                            if (!all && !visible(base[i] + 4 * h + j, pos[r], a.window, a.sinks)) f = fv = 0.f;
+                            g[r] += f;
+                            w[i][j] = fv;
+                        }
+                    }
+                    M::add(acc[r], v, w);
+                }
+            }
+        }
+        bad = __any(bad);
+
+        // the waves' sums, one row tile at a time
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float gs = rows4_sum(g[r]);
+            if (bad && (seq.cut || sees_bad_page(a, table, sp, begin, end, pos[r]))) gs = __builtin_nanf("");
+            __syncthreads();
+            if (h == 0) gred[wave][r16] = gs;
+#pragma unroll
+            for (int d = 0; d < D / 4; ++d) red[wave][r16][h * (D / 4) + d] = acc[r][d % VW][d / VW];
+            __syncthreads();
+            const int rr = threadIdx.x / 16, c = threadIdx.x % 16 * VW, row = r0 + 16 * r + rr;
+            if (rr < 16 && row < rows) {
+                float f[VW], gg = 0.f;
+#pragma unroll
+                for (int j = 0; j < VW; ++j) f[j] = 0.f;
+#pragma unroll
+                for (int v = 0; v < WAVES; ++v) {
+                    gg += gred[v][rr];
+#pragma unroll
+                    for (int j = 0; j < VW; ++j) f[j] += red[v][rr][c + j];
+                }
+                const int t = row / a.group;
+                const size_t o = (size_t)(seq.t0 + t) * a.Hq + head * a.group + row - t * a.group;
+                if (plan.splits == 1) {
+                    const bool none = seq.len - seq.count + t < 0;   // sees no key
+                    T *out = (T *)a.out + o * D + c;
+#pragma unroll
+                    for (int j = 0; j < VW; ++j) io<T>::st(out, j, none ? 0.f : f[j] / gg);
+                } else {
+                    float *p = part + (o * plan.splits + split) * D + c;
+#pragma unroll
+                    for (int j = 0; j < VW; ++j) p[j] = f[j];
+                    if (c == 0) part[(size_t)a.T * a.Hq * plan.splits * D + o * plan.splits + split] = gg;
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int D, int RT, int W = WAVES>
+hipError_t launch_few(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
+{
+    const long long blocks = (long long)plan.splits * plan.tiles * a.Hkv * a.S;
+    if (!grid_fits(blocks, 64 * W)) return hipErrorInvalidConfiguration;
+    few_kernel<T, D, RT, W><<<(unsigned)blocks, 64 * W, 0, st>>>(a, plan, part);
+    return hipGetLastError();
+}
+
+// --- many rows ------------------------------------------------------------------
+
+// LDS rows have no padding: piece c of row r (16 bytes) lies at c ^ swizzle(r),
+// which puts 8 consecutive rows' piece c, and pieces c, c + 1 of 4 consecutive
+// rows, on distinct banks.
+template <int C> __device__ __forceinline__ int swizzle(int r)
+{
+    if constexpr (C >= 8) return (r & 3) << 1 | (r >> 2 & 1);
+    else if constexpr (C == 4) return (r >> 1 & 1) << 1 | (r >> 2 & 1);   // two rows to a line of banks
+    else return r >> 2 & 1;
+}
+
+__device__ __forceinline__ f16v mma(u4 a, u4 b, f16v c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+}
+
+// MFMA bounds it: 128 rows to a workgroup, 32 to a wave, 64 keys at a time
+// through two LDS buffers, products of 32x32 as fm_paged_chunk.hip (its layouts:
+// lane = 32 hh + c32; accumulator register i: column c32, row 8 (i/4) + 4 hh + i%4).
+// The cache's bytes go through registers, where a workgroup turns the values'
+// codes into bf16 once for its four waves; the keys' stay bytes.
+template <typename T, int D>
+__global__ __launch_bounds__(THREADS, 2) void many_kernel(PagedArgs a, PagedPlan plan, int pieces, float *part)
+{
+    constexpr int NP = PARTS<T>, ROWS = CHUNK_ROWS, WR = ROWS / 4, KB = 64;
+    constexpr int KP = D / 16, VP = D / 8, DT = D / 32;       // 16-byte pieces of a key row, a value row; channel tiles
+    constexpr int LN = KB * KP > THREADS ? KB * KP / THREADS : 1, LR = THREADS / KP;   // loads of a thread, rows of one
+    __shared__ u4 keys[2][KB * KP], values[2][KB * VP];
+    __shared__ f4 kscale[2][KB / 4], vscale[2][KB / 4];
+
+    // Row tiles of one (sequence, key head, split) read the same keys, so every
+    // `pieces`th of them go to the same XCD.  Late row tiles see the most keys and
+    // start first.
+    const int in_piece = (plan.tiles + pieces - 1) / pieces;
+    const int turn = blockIdx.x / 8 / in_piece, piece = turn * 8 + (blockIdx.x + turn) % 8;
+    const int row_tile = plan.tiles - 1 - (piece % pieces + pieces * (blockIdx.x / 8 % in_piece));
+    const int split = piece / pieces % plan.splits, pair = piece / pieces / plan.splits;
+    if (pair >= a.S * a.Hkv || row_tile < 0) return;
+    const int head = pair % a.Hkv, s = pair / a.Hkv;
+
+    const int wave = scalar(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32, c32 = lane % 32;
+    const Seq seq = seq_of(a, s);
+    const int rows = seq.count * a.group, page_mask = (1 << a.page_shift) - 1;
+    const int8_t *kc = (const int8_t *)a.k + head * a.cache.head, *vc = (const int8_t *)a.v + head * a.cache.head;
+    const int32_t *table = a.table + (size_t)s * a.table_cols;
+    const int my_row = threadIdx.x / KP, my_piece = threadIdx.x % KP;   // of a load
+
+    for (int r0 = row_tile * ROWS; r0 < rows; r0 += plan.tiles * ROWS) {
+        const Span sp = scalar(span_of_rows(a, seq, r0, ROWS));
+        const int begin = split * plan.chunk;
+        const int end = split == plan.splits - 1 ? sp.tiles : min(sp.tiles, begin + plan.chunk);
+        if (begin >= sp.tiles && split > 0) continue;   // the join knows
+        const int pos0 = seq.len - seq.count;           // position of row 0
+        const int first = scalar(pos0 + r0 / a.group), last = sp.end - 1;
+
+        const int row = r0 + wave * WR + c32;           // the lane's own
+        const int t = min(row, rows - 1) / a.group, pos = pos0 + t;
+        const int q_head = head * a.group + min(row, rows - 1) - t * a.group;
+        u4 q[NP][DT];
+        float c1, c2;
+        {
+            const T *p = (const T *)a.q + (seq.t0 + t) * a.q_token + q_head * a.q_head + 16 * hh;
+            float x[DT][16];
+            uint32_t top = 0;
+#pragma unroll
+            for (int c = 0; c < DT; ++c) {
+                ld_row<16>(p + 32 * c, x[c]);
+                top = max(top, abs_max<16>(x[c]));
+            }
+            const float2 f = whole_scale<NP>(halves_max(top));
+            c1 = a.c1 * f.y;
+            c2 = a.c2 * f.y * f.y;
+#pragma unroll
+            for (int c = 0; c < DT; ++c) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t w[NP];
+                    whole4<NP>(x[c] + 4 * i, f.x, w);
+#pragma unroll
+                    for (int n = 0; n < NP; ++n) q[n][c][i] = w[n];
+                }
+            }
+        }
+        f16v acc[DT];
+        float g = 0.f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[d] = f16v{};
+
+        bool bad = seq.cut;
+        const int shift = sp.low - sp.sink_tiles;   // from a tile's number here to its own
+        const int whole = a.window < sp.end ? max(sp.sink_tiles, (last - a.window) / KT + 1 - shift) : 0;
+        const int whole_end = min(end, (first + 1) / KT - shift);
+
+        // A step's bytes in registers: this thread's pieces of keys and values, and
+        // a scale (threads 0 .. 63: of a key, 64 .. 127: of a value).
+        u4 kr[LN], vr[LN];
+        float sr = 0.f;
+        const bool loads = KB * KP >= THREADS || threadIdx.x < KB * KP;
+        const auto place_of = [&](int i0, int r) { return sp.tile(min(i0 + r / KT, end - 1)) * KT + r % KT; };
+        int page[LN], spage = 0;   // of the next loads' rows, a step ahead
+        const auto pages_of = [&](int i0) {
+#pragma unroll
+            for (int i = 0; i < LN; ++i)
+                page[i] = table[place_of(i0, (my_row + LR * i) & (KB - 1)) >> a.page_shift];
+            spage = table[place_of(i0, threadIdx.x & (KB - 1)) >> a.page_shift];
+        };
+        const auto checked = [&](int p) {
+            if ((unsigned)p < (unsigned)a.pages) return p;
+            bad = true;
+            return 0;
+        };
+        const auto load = [&](int i0) {
+#pragma unroll
+            for (int i = 0; i < LN; ++i) {
+                const int n = place_of(i0, (my_row + LR * i) & (KB - 1));
+                const long long at = checked(page[i]) * a.cache.batch + (n & page_mask) * a.cache.token + 16 * my_piece;
+                if (loads) {
+                    kr[i] = *(const u4 *)(kc + at);
+                    vr[i] = *(const u4 *)(vc + at);
+                }
+            }
+            const int n = place_of(i0, threadIdx.x & (KB - 1));
+            const long long at = (((long long)checked(spage) * a.Hkv + head) << a.page_shift) + (n & page_mask);
+            if (threadIdx.x < 2 * KB) sr = (threadIdx.x < KB ? a.k_scale : a.v_scale)[at];
+        };
+        const auto store = [&](int b) {
+#pragma unroll
+            for (int i = 0; i < LN; ++i) {
+                const int r = my_row + LR * i;
+                if (!loads) continue;
+                keys[b][r * KP + (my_piece ^ swizzle<KP>(r))] = kr[i];
+                u4 x[2];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint32_t w = vr[i][j / 2];
+                    const float lo = (float)(int8_t)(w >> (16 * (j % 2))), hi = (float)(int8_t)(w >> (16 * (j % 2) + 8));
+                    x[j / 4][j % 4] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) values[b][r * VP + ((2 * my_piece + j) ^ swizzle<VP>(r))] = x[j];
+            }
+            if (threadIdx.x < 2 * KB) ((float *)(threadIdx.x < KB ? kscale : vscale)[b])[threadIdx.x & (KB - 1)] = sr;
+        };
+
+        constexpr int STEP = KB / KT;
+        const auto compute = [&](int b, int i0) {
+            const bool all = i0 >= whole && i0 + STEP <= whole_end;
+#pragma unroll
+            for (int kb = 0; kb < KB / 32; ++kb) {
+                u4 k[DT], va[2][DT];
+#pragma unroll
+                for (int i = 0; i < DT; ++i) k[i] = keys[b][(32 * kb + c32) * KP + ((2 * i + hh) ^ swizzle<KP>(c32))];
+                i16v n = i16v{}, l = i16v{};
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+                    n = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i4, k[i]), __builtin_bit_cast(i4, q[0][i]), n, 0, 0, 0);
+                n = n << 8;
+#pragma unroll
+                for (int i = 0; i < DT; ++i)
+                    n = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i4, k[i]), __builtin_bit_cast(i4, q[1][i]), n, 0, 0, 0);
+                if constexpr (NP == 3) {
+#pragma unroll
+                    for (int i = 0; i < DT; ++i)
+                        l = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i4, k[i]), __builtin_bit_cast(i4, q[2][i]), l, 0, 0, 0);
+                }
+                // the value operands: keys {4 hh .. + 3, 8 + 4 hh .. + 3} of 16, channel c32 of 32
+                const s4 *v = (const s4 *)values[b];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        typedef s4 __attribute__((address_space(3))) *lp;
+                        const int j = lane >> 2 & 3, r = 32 * kb + 16 * m + 4 * hh + j;
+                        const int c = 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+                        const int at = 2 * (r * VP + (c ^ swizzle<VP>(4 * hh + j))) + (lane & 1);
+                        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(v + at));
+                        const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(v + at + 2 * 8 * VP));
+                        const uint2 x = __builtin_bit_cast(uint2, lo), y = __builtin_bit_cast(uint2, hi);
+                        va[m][d] = u4{x.x, x.y, y.x, y.y};
+                    }
+                }
+                float w[16];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f4 ks = kscale[b][8 * kb + 2 * i + hh], vs = vscale[b][8 * kb + 2 * i + hh];
+                    // key n0 + e of a tile is seen if e <= lim and (e > lim - window or it
+                    // is a first token)
+                    const int it = i0 + 2 * kb + i / 2, n0 = sp.tile(min(it, end - 1)) * KT + 4 * hh;
+                    const int lim = it < end ? max(pos, -1) - n0 : -1, low = lim - a.window, sinks = a.sinks - n0;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float x = (float)n[4 * i + j];
+                        if constexpr (NP == 3) x = fmaf(x, 256.0f, (float)l[4 * i + j]);
+                        x *= ks[j];
+                        float f = fmaf(fmaf(x, c2, c1), x, 1.0f), fv = f * vs[j];
+                        const int e = 8 * (i % 2) + j;
+                        if (!all && (e > lim || (e <= low && e >= sinks))) f = fv = 0.f;
+                        g += f;
+                        w[4 * i + j] = fv;
+                    }
+                }
+                u4 wp[NP][2];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t p[NP];
+                    parts2<NP>(w[2 * i], w[2 * i + 1], p);
+#pragma unroll
+                    for (int x = 0; x < NP; ++x) wp[x][i / 4][i % 4] = p[x];
+                }
+#pragma unroll
+                for (int x = NP - 1; x >= 0; --x) {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) acc[d] = mma(va[m][d], wp[x][m], acc[d]);
+                    }
+                }
+            }
+        };
+
+        if (begin < end) {
+            pages_of(begin);
+            load(begin);
+            pages_of(begin + STEP);
+            store(0);
+            load(begin + STEP);
+            pages_of(begin + 2 * STEP);
+        }
+        __syncthreads();
+        for (int i0 = begin, b = 0; i0 < end; i0 += STEP, b ^= 1) {
+            compute(b, i0);
+            // the other buffer: every wave is past the step that read it
+            store(b ^ 1);
+            load(i0 + 2 * STEP);
+            pages_of(i0 + 3 * STEP);
+            __syncthreads();
+        }
+        bad = __syncthreads_or(bad);
+
+        float gs = halves_sum(g);
+        if (bad && (seq.cut || sees_bad_page(a, table, sp, begin, end, pos))) gs = __builtin_nanf("");
+        const float inv = 1.0f / gs;
+        const size_t o = (size_t)(seq.t0 + t) * a.Hq + q_head;
+        if (row < rows) {
+            if (plan.splits > 1 && hh == 0) part[(size_t)a.T * a.Hq * plan.splits * D + o * plan.splits + split] = gs;
+#pragma unroll
+            for (int n = 0; n < 4 * DT; ++n) {
+                float f[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[j] = acc[n / 4][n % 4 * 4 + j];
+                const int ch = 32 * (n / 4) + 8 * (n % 4) + 4 * hh;
+                if (plan.splits > 1) {
+                    *(float4 *)(part + (o * plan.splits + split) * D + ch) = make_float4(f[0], f[1], f[2], f[3]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[j] = pos < 0 ? 0.f : f[j] * inv;   // pos < 0: sees no key
+                    T *out = (T *)a.out + o * D + ch;
+                    if constexpr (sizeof(T) == 2) *(uint2 *)out = make_uint2(rows::pack2(f[0], f[1]), rows::pack2(f[2], f[3]));
+                    else *(float4 *)out = make_float4(f[0], f[1], f[2], f[3]);
+                }
+            }
+        }
+    }
+}
+
+template <typename T, int D> hipError_t launch_many(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
+{
+    // Row tiles that share their keys stay on one XCD unless that leaves XCDs idle
+    // or uneven (the measurements of fm_paged_chunk.hip).
+    const long long units = (long long)a.S * a.Hkv * plan.splits;
+    const auto more = [&](long long n) { return 7 * ((n + 7) / 8) > n || (a.S > 1 && n < 64); };
+    int pieces = 1;
+    while (pieces < 8 && 2 * pieces <= plan.tiles && more(units * pieces)) pieces *= 2;
+    const long long blocks = (units * pieces + 7) / 8 * 8 * ((plan.tiles + pieces - 1) / pieces);
+    if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
+    many_kernel<T, D><<<(unsigned)blocks, THREADS, 0, st>>>(a, plan, pieces, part);
+    return hipGetLastError();
+}
+
+template <typename T, int D> hipError_t launch(const PagedArgs &a, const PagedPlan &plan, float *part, hipStream_t st)
+{
+    if (plan.chunk_kernel) {
+        if constexpr (D >= 32) return launch_many<T, D>(a, plan, part, st);
+    } else if (plan.waves == 8) {
+        return launch_few<T, D, 1, 8>(a, plan, part, st);
+    } else if (plan.rows == 16) {
+        return launch_few<T, D, 1>(a, plan, part, st);
+    } else if (plan.rows == 32) {
+        return launch_few<T, D, 2>(a, plan, part, st);
+    } else if constexpr (D <= 64) {
+        return launch_few<T, D, 4>(a, plan, part, st);
+    }
+    return hipErrorInvalidValue;   // no plan has such rows
+}
+
+template <typename T> hipError_t launch_d(const PagedArgs &a, const PagedPlan &plan, int D, float *part, hipStream_t st)
+{
+    switch (D) {
+    case 16: return launch<T, 16>(a, plan, part, st);
+    case 32: return launch<T, 32>(a, plan, part, st);
+    case 64: return launch<T, 64>(a, plan, part, st);
+    default: return launch<T, 128>(a, plan, part, st);
+    }
+}
+
+}  // namespace
+
+PagedPlan paged_q8_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int max_len, int window, int sinks)
+{
+    (void)is_bf16;
+    return paged_plan(S, Hq, Hkv, D, 1, max_q, max_len, window, sinks, D == 128 ? 32 : 64);
+}
+
+hipError_t paged_q8_fwd(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, void *ws, hipStream_t st)
+{
+    const hipError_t e = is_bf16 ? launch_d<bf16_t>(a, plan, D, (float *)ws, st) : launch_d<float>(a, plan, D, (float *)ws, st);
+    return e != hipSuccess || plan.splits == 1 ? e : paged_join(a, plan, D, is_bf16, (const float *)ws, st);
+}
+
+}  // namespace fm

@@ -67,6 +67,15 @@ template <int L> __device__ __forceinline__ float row_sum(float x)
     return x;
 }
 
+// The largest of the lanes' values, likewise.
+template <int L> __device__ __forceinline__ uint32_t row_max(uint32_t x)
+{
+    if constexpr (L >= 2) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, true));
+    if constexpr (L >= 4) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, true));
+    if constexpr (L >= 8) x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xF, 0xF, true));
+    return x;
+}
+
 // A lane's place in its row: where its two runs of 8 channels start, and
 // whether they are rotated.
 struct Place {

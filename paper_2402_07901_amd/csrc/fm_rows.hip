@@ -61,10 +61,45 @@ int heads_per_run(long long blocks, int Hq, int Hkv)
     return per;
 }
 
-template <typename T, int D, bool APPEND>
+// The 8-bit cache row of a lane's 16 channels: codes of its two runs and, from
+// the row's first lane, the scale.  amax is the largest magnitude as float32
+// bits, in which a NaN lies above infinity and both above every number.  Both
+// divisions are IEEE's, once a row; codes round to nearest even.
+template <int L>
+__device__ __forceinline__ void st_q8(int8_t *row, float *scale, const Place &at, int c, const float *y)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(y[i]) & 0x7fffffffu);
+    top = row_max<L>(top);
+    const float amax = __uint_as_float(top);
+    const bool odd = top >= 0x7f800000u;
+    const float f = odd || amax < Q8_LEAST ? 0.f : 127.0f / amax;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int code = __float2int_rn(y[4 * i + j] * f);
+            w[i] |= (uint32_t)(code & 255) << (8 * j);
+        }
+        w[i] = odd ? 0u : w[i];
+    }
+    *(uint2 *)(row + at.a) = make_uint2(w[0], w[1]);
+    *(uint2 *)(row + at.b) = make_uint2(w[2], w[3]);
+    if (c == 0) *scale = odd ? __builtin_nanf("") : amax < Q8_LEAST ? 0.f : amax / 127.0f;
+}
+
+// What becomes of the rows: heads of the attention, or a cache in the rows' type
+// or in 8 bits.
+enum Into { HEADS, CACHE, CACHE_Q8 };
+
+template <typename T, int D, Into INTO>
 __global__ __launch_bounds__(THREADS) void rows_kernel(RowsArgs a, int per)
 {
     constexpr int L = D / 16, U = 4;
+    constexpr bool APPEND = INTO != HEADS;
     const long long tokens = (long long)a.B * a.N;
     const long long lane = (long long)blockIdx.x * THREADS + threadIdx.x;
     const long long t = lane / L;
@@ -78,6 +113,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(RowsArgs a, int per)
     const T *src = (const T *)(run.kind == 0 ? a.q : run.kind == 1 ? a.k : a.v) + b * st.batch + n * st.token;
     T *dst = (T *)(run.kind == 0 ? a.oq : run.kind == 1 ? a.ok : a.ov);
     long long head, row;       // elements between heads, and where the token is in a head
+    long long scale = 0;       // 8 bits: where the row's scale is in head 0
     int copies = 1;
     if constexpr (!APPEND) {
         head = (long long)a.N * D;
@@ -91,6 +127,7 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(RowsArgs a, int per)
         if (slot < 0 || slot >= (long long)a.pages << a.page_shift) return;
         head = a.cache.head;
         row = (slot >> a.page_shift) * a.cache.batch + (slot & ((1 << a.page_shift) - 1)) * a.cache.token;
+        scale = ((slot >> a.page_shift) * a.Hkv << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
     }
 
     const bool plain = run.kind == 2;
@@ -144,12 +181,53 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(RowsArgs a, int per)
                     for (int i = 0; i < 16; ++i) y[i] *= r;
                 }
             }
+            if constexpr (INTO == CACHE_Q8) {
+                if (run.kind) {
+                    st_q8<L>((int8_t *)dst + row + (h + u) * head,
+                             (run.kind == 1 ? a.k_scale : a.v_scale) + scale + ((long long)(h + u) << a.page_shift), at, c, y);
+                    continue;
+                }
+            }
             T *o = dst + row + (long long)(h + u) * copies * head;
             for (int j = 0; j < copies; ++j, o += head) {
                 st8(o + at.a, y);
                 st8(o + at.b, y + 8);
             }
         }
+    }
+}
+
+// Rows of the 8-bit cache by their slots: code times scale, rounded once; a slot
+// outside the cache gives a row of zeros.
+template <typename T, int D>
+__global__ __launch_bounds__(THREADS) void read_q8_kernel(ReadArgs a)
+{
+    constexpr int L = D / 8;
+    const long long lane = (long long)blockIdx.x * THREADS + threadIdx.x, row = lane / L;
+    const int c = (int)(lane % L);
+    const long long t = row / a.Hkv;
+    if (t >= a.T) return;
+    const int h = (int)(row - t * a.Hkv);
+    const long long slot = a.slots[t];
+    const bool in = slot >= 0 && slot < (long long)a.pages << a.page_shift;
+    uint2 w[2] = {};
+    float f[2] = {0.f, 0.f};
+    if (in) {
+        const long long page = slot >> a.page_shift, place = slot & ((1 << a.page_shift) - 1);
+        const long long at = page * a.cache.batch + place * a.cache.token + h * a.cache.head + 8 * c;
+        const long long sat = ((page * a.Hkv + h) << a.page_shift) + place;
+        w[0] = *(const uint2 *)(a.k + at);
+        w[1] = *(const uint2 *)(a.v + at);
+        f[0] = a.k_scale[sat];
+        f[1] = a.v_scale[sat];
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t u[2] = {w[i].x, w[i].y};
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = (float)(int8_t)(u[j / 4] >> (8 * (j % 4))) * f[i];
+        st8((T *)(i ? a.ov : a.ok) + row * D + 8 * c, x);
     }
 }
 
@@ -308,7 +386,7 @@ bool rows_fit(long long blocks, long long y)
     return grid_fits(blocks, THREADS) && y <= 65535;
 }
 
-template <bool APPEND> hipError_t rows_launch(const RowsArgs &a, int D, int is_bf16, hipStream_t st)
+template <Into INTO> hipError_t rows_launch(const RowsArgs &a, int D, int is_bf16, hipStream_t st)
 {
     const long long blocks = token_blocks((long long)a.B * a.N, D);
     const int per = heads_per_run(blocks, a.Hq, a.Hkv);
@@ -317,8 +395,8 @@ template <bool APPEND> hipError_t rows_launch(const RowsArgs &a, int D, int is_b
     const dim3 grid((unsigned)blocks, (unsigned)y);
 #define FM_ROWS(DD)                                                                               \
     case DD:                                                                                      \
-        if (is_bf16) rows_kernel<bf16_t, DD, APPEND><<<grid, THREADS, 0, st>>>(a, per);           \
-        else rows_kernel<float, DD, APPEND><<<grid, THREADS, 0, st>>>(a, per);                    \
+        if (is_bf16) rows_kernel<bf16_t, DD, INTO><<<grid, THREADS, 0, st>>>(a, per);           \
+        else rows_kernel<float, DD, INTO><<<grid, THREADS, 0, st>>>(a, per);                    \
         break
     switch (D) {
         FM_ROWS(16);
@@ -334,12 +412,37 @@ template <bool APPEND> hipError_t rows_launch(const RowsArgs &a, int D, int is_b
 
 hipError_t rope_fwd(const RowsArgs &a, int D, int is_bf16, hipStream_t st)
 {
-    return rows_launch<false>(a, D, is_bf16, st);
+    return rows_launch<HEADS>(a, D, is_bf16, st);
 }
 
 hipError_t cache_append(const RowsArgs &a, int D, int is_bf16, hipStream_t st)
 {
-    return rows_launch<true>(a, D, is_bf16, st);
+    return rows_launch<CACHE>(a, D, is_bf16, st);
+}
+
+hipError_t cache_append_q8(const RowsArgs &a, int D, int is_bf16, hipStream_t st)
+{
+    return rows_launch<CACHE_Q8>(a, D, is_bf16, st);
+}
+
+hipError_t cache_read_q8(const ReadArgs &a, int D, int is_bf16, hipStream_t st)
+{
+    // a lane reads 8 codes of a key row and of the value row beside it
+    const long long lanes = (long long)a.T * a.Hkv * (D / 8), blocks = (lanes + THREADS - 1) / THREADS;
+    if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
+#define FM_READ(DD)                                                                               \
+    case DD:                                                                                      \
+        if (is_bf16) read_q8_kernel<bf16_t, DD><<<(unsigned)blocks, THREADS, 0, st>>>(a);         \
+        else read_q8_kernel<float, DD><<<(unsigned)blocks, THREADS, 0, st>>>(a);                  \
+        break
+    switch (D) {
+        FM_READ(16);
+        FM_READ(32);
+        FM_READ(64);
+        FM_READ(128);
+    }
+#undef FM_READ
+    return hipGetLastError();
 }
 
 size_t rope_bwd_workspace(long long tokens, int Hq, int Hkv, int D, int norm)

@@ -33,9 +33,24 @@ struct RowsArgs {
     Strides cache;                 // batch: page, token: slot in the page, head
     const int64_t *slots;
     int pages, page_shift;
+    float *k_scale, *v_scale;      // 8-bit caches: [pages, Hkv, page]
 };
+// A row of an 8-bit cache is its largest magnitude / 127 (its scale) times codes
+// -127 .. 127.  Rows below this are stored as zeros: 127 / amax stays finite.
+constexpr float Q8_LEAST = 0x1p-100f;
 hipError_t rope_fwd(const RowsArgs &a, int D, int is_bf16, hipStream_t st);
 hipError_t cache_append(const RowsArgs &a, int D, int is_bf16, hipStream_t st);
+hipError_t cache_append_q8(const RowsArgs &a, int D, int is_bf16, hipStream_t st);
+
+struct ReadArgs {
+    const int8_t *k, *v;
+    const float *k_scale, *v_scale;
+    Strides cache;
+    const int64_t *slots;
+    void *ok, *ov;                 // [T, Hkv, D]
+    int T, Hkv, pages, page_shift;
+};
+hipError_t cache_read_q8(const ReadArgs &a, int D, int is_bf16, hipStream_t st);
 
 struct RowsBwdArgs {
     const void *q, *k;             // the forward's rows (norm only)
@@ -59,6 +74,7 @@ struct PagedArgs {
     int S, T, Hq, Hkv, group, pages, table_cols, page_shift;
     int window, sinks;             // window 2^30: none
     float c1, c2;                  // weight 1 + s (c1 + c2 s) of the raw product s; c2 is 0 for first order
+    const float *k_scale, *v_scale;   // 8-bit caches: [pages, Hkv, page]
 };
 // How a call is cut: rows of a (sequence, key head) in tiles, keys in splits.
 struct PagedPlan {
@@ -69,11 +85,17 @@ struct PagedPlan {
     int chunk;                     // key tiles of 16 per split
     int splits;
 };
+// most_rows: of a row tile of the few-row kernels (16, 32 or 64).
 PagedPlan paged_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int max_len, int window,
-                     int sinks);
+                     int sinks, int most_rows);
 size_t paged_workspace(const PagedPlan &plan, int T, int Hq, int D);
 hipError_t paged_fwd(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, void *ws,
                      hipStream_t st);
+// Adds the splits' sums of a call (part: its workspace).
+hipError_t paged_join(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, const float *part, hipStream_t st);
+// The same attention over a cache of 8-bit rows (fm_paged_q8.hip).
+PagedPlan paged_q8_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int max_len, int window, int sinks);
+hipError_t paged_q8_fwd(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, void *ws, hipStream_t st);
 constexpr int CHUNK_ROWS = 128;    // rows of a workgroup of the chunk kernel
 hipError_t paged_chunk(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, float *part,
                        hipStream_t st);

@@ -105,6 +105,16 @@ def lib():
         L.fastmax_paged_fwd.argtypes = [vp, st, vp, vp, st, vp, vp, vp, vp, i, i, i, i, i, i, i, i,
                                         i, i, i, f, i, i, i, vp, sz, vp]
         L.fastmax_paged_fwd.restype = i
+        L.fastmax_cache_append_q8.argtypes = [vp, vp, vp, st, vp, vp, vp, vp, vp, st, vp, i, i, i,
+                                              i, i, i, rope, i, vp]
+        L.fastmax_cache_append_q8.restype = i
+        L.fastmax_cache_read_q8.argtypes = [vp, vp, vp, vp, st, vp, vp, vp, i, i, i, i, i, i, vp]
+        L.fastmax_cache_read_q8.restype = i
+        L.fastmax_paged_q8_workspace_bytes.argtypes = [i, i, i, i, i, i, i, i, i, i]
+        L.fastmax_paged_q8_workspace_bytes.restype = sz
+        L.fastmax_paged_fwd_q8.argtypes = [vp, st, vp, vp, vp, vp, st, vp, vp, vp, vp, i, i, i, i, i,
+                                           i, i, i, i, i, i, f, i, i, i, vp, sz, vp]
+        L.fastmax_paged_fwd_q8.restype = i
         L.fastmax_strerror.argtypes = [i]
         L.fastmax_strerror.restype = ctypes.c_char_p
         L.fastmax_version.restype = ctypes.c_char_p
@@ -619,13 +629,14 @@ def fastmax_rope_bwd(q, k, gq, gk, gv, pos, cos, sin, wq=None, wk=None, eps=1e-6
     return (*out, dwq, dwk)
 
 
-def _cache_of(q, k_cache, v_cache, Hkv):
-    """(pages, page size, strides) of the caches [pages, Hkv, page, D]."""
+def _cache_of(q, k_cache, v_cache, Hkv, dtype=None):
+    """(pages, page size, strides) of the caches [pages, Hkv, page, D]; their
+    type is q's unless given."""
     shape = k_cache.shape
     if len(shape) != 4:
         raise ValueError(f"k_cache must be [pages, Hkv, page, D], got shape {tuple(shape)}")
     pages, _, page, _ = shape
-    dtype, dev = q.dtype, q.get_device()
+    dtype, dev = dtype or q.dtype, q.get_device()
     _rows_of("k_cache", k_cache, (pages, Hkv, page, q.shape[-1]), dtype, dev, q)
     _rows_of("v_cache", v_cache, shape, dtype, dev, q)
     st = k_cache.stride()
@@ -707,4 +718,112 @@ def fastmax_paged_fwd(q, k_cache, v_cache, table, lens, q_start=None, max_q=None
          table.data_ptr(), lens.data_ptr(), _ptr(q_start), out.data_ptr(), S, T, Hq, Hkv, D, pages,
          page, cols, max_q, max_len, p, 1.0 if scale is None else scale, window, sinks, dt,
          _ptr(workspace), ws_n)
+    return out
+
+
+# --- the cache in 8 bits ------------------------------------------------------
+def _cache_q8_of(q, k_cache, v_cache, k_scale, v_scale, Hkv):
+    """_cache_of 8-bit caches, with their scales float32 [pages, Hkv, page]."""
+    torch = _torch()
+    pages, page, cache = _cache_of(q, k_cache, v_cache, Hkv, torch.int8)
+    _whole("k_scale", k_scale, (pages, Hkv, page), torch.float32, q.get_device(), q)
+    _whole("v_scale", v_scale, (pages, Hkv, page), torch.float32, q.get_device(), q)
+    return pages, page, cache
+
+
+def fastmax_cache_append_q8(q, k, v, k_cache, v_cache, k_scale, v_scale, slots, pos, cos, sin,
+                            wq=None, wk=None, eps=1e-6, sections=None, interleaved=False,
+                            q_out=None, stream=None):
+    """fastmax_cache_append into a cache of 8-bit rows: k_cache and v_cache int8
+    [pages, Hkv, page, D], k_scale and v_scale float32 [pages, Hkv, page]; a row
+    stands for code * scale.  Returns q^ [T, Hq, D]."""
+    _on_gpu(q, 3, "[T, Hq, D]")
+    T, Hq, D = q.shape
+    dtype, dev, dt = q.dtype, q.get_device(), _dtype_code(q)
+    Hkv = k.shape[1] if k.dim() == 3 else 0
+    _rows_of("k", k, (T, Hkv, D), dtype, dev, q)
+    _rows_of("v", v, (T, Hkv, D), dtype, dev, q)
+    pages, page, cache = _cache_q8_of(q, k_cache, v_cache, k_scale, v_scale, Hkv)
+    _whole("slots", slots, (T,), _torch().int64, dev, q)
+    rope = _rope_of(q, (T,), pos, cos, sin, wq, wk, eps, sections, interleaved)
+    if q_out is None:
+        q_out, = _new(q, ((T, Hq, D),), stream)
+    else:
+        _whole("q_out", q_out, (T, Hq, D), dtype, dev, q)
+    _run("fastmax_cache_append_q8", lib().fastmax_cache_append_q8, dev, stream,
+         q.data_ptr(), k.data_ptr(), v.data_ptr(),
+         _LL9(0, *q.stride()[:2], 0, *k.stride()[:2], 0, *v.stride()[:2]),
+         q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(),
+         v_scale.data_ptr(), cache, slots.data_ptr(), T, Hq, Hkv, D, pages, page, rope, dt)
+    return q_out
+
+
+def fastmax_cache_read_q8(k_cache, v_cache, k_scale, v_scale, slots, dtype=None, out=None,
+                          stream=None):
+    """Rows of an 8-bit cache by their slots (int64 [T], page * page size +
+    place; one outside the cache: zeros).  Returns k^ and v [T, Hkv, D] of
+    ``dtype`` (float32 or bfloat16, the default; ``out``: the same two, the
+    caller's)."""
+    torch = _torch()
+    _on_gpu(k_cache, 4, "[pages, Hkv, page, D]")
+    _, Hkv, _, D = k_cache.shape
+    dev = k_cache.get_device()
+    pages, page, cache = _cache_q8_of(k_cache, k_cache, v_cache, k_scale, v_scale, Hkv)
+    if slots.dim() != 1:
+        raise ValueError(f"slots must be [T], got shape {tuple(slots.shape)}")
+    T = slots.shape[0]
+    _whole("slots", slots, (T,), torch.int64, dev, k_cache)
+    if out is None:
+        dtype = dtype or torch.bfloat16
+        out = _new(k_cache, ((T, Hkv, D),) * 2, stream, dtype)
+    else:
+        dtype = dtype or out[0].dtype
+        for name, t in zip(("out[0]", "out[1]"), out):
+            _whole(name, t, (T, Hkv, D), dtype, dev, k_cache)
+    _run("fastmax_cache_read_q8", lib().fastmax_cache_read_q8, dev, stream,
+         k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), cache,
+         slots.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), T, Hkv, D, pages, page,
+         _dtype_code(out[0]))
+    return tuple(out)
+
+
+def paged_q8_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window, sinks, dt) -> int:
+    return int(lib().fastmax_paged_q8_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window,
+                                                      sinks, dt))
+
+
+def fastmax_paged_fwd_q8(q, k_cache, v_cache, k_scale, v_scale, table, lens, q_start=None,
+                         max_q=None, max_len=None, p=2, scale=None, window=0, sinks=0, out=None,
+                         workspace=None, stream=None):
+    """fastmax_paged_fwd over a cache of 8-bit rows (fastmax_cache_append_q8); q
+    [T, Hq, D] and O in float32 or bfloat16."""
+    _on_gpu(q, 3, "[T, Hq, D]")
+    T, Hq, D = q.shape
+    dtype, dev, dt = q.dtype, q.get_device(), _dtype_code(q)
+    Hkv = k_cache.shape[1] if k_cache.dim() == 4 else 0
+    pages, page, cache = _cache_q8_of(q, k_cache, v_cache, k_scale, v_scale, Hkv)
+    if table.dim() != 2:
+        raise ValueError(f"table must be [S, cols], got shape {tuple(table.shape)}")
+    S, cols = table.shape
+    int32 = _torch().int32
+    _whole("table", table, (S, cols), int32, dev, q)
+    _whole("lens", lens, (S,), int32, dev, q)
+    if q_start is not None:
+        _whole("q_start", q_start, (S + 1,), int32, dev, q)
+    if max_q is None:
+        max_q = 1 if q_start is None else T
+    if max_len is None:
+        max_len = cols * page
+    if out is None:
+        out, = _new(q, ((T, Hq, D),), stream)
+    else:
+        _whole("out", out, (T, Hq, D), dtype, dev, q)
+    workspace, ws_n = _workspace(
+        q, workspace,
+        lambda: paged_q8_workspace_bytes(S, T, Hq, Hkv, D, max_q, max_len, window, sinks, dt), stream)
+    _run("fastmax_paged_fwd_q8", lib().fastmax_paged_fwd_q8, dev, stream,
+         q.data_ptr(), _LL3(0, *q.stride()[:2]), k_cache.data_ptr(), v_cache.data_ptr(),
+         k_scale.data_ptr(), v_scale.data_ptr(), cache, table.data_ptr(), lens.data_ptr(),
+         _ptr(q_start), out.data_ptr(), S, T, Hq, Hkv, D, pages, page, cols, max_q, max_len, p,
+         1.0 if scale is None else scale, window, sinks, dt, _ptr(workspace), ws_n)
     return out
