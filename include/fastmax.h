@@ -495,6 +495,52 @@ int fastmax_paged_fwd_q8(const void *q, const fastmax_strides_t *q_strides, cons
                          float qk_scale, int window, int sinks, fastmax_dtype_t dt, void *workspace,
                          size_t workspace_bytes, hipStream_t stream);
 
+/*
+ * Whole sequences of different lengths, packed one after the other (prompts, or
+ * a training batch without padding), query heads sharing key heads as above.
+ * Sequence s has the tokens starts[s] .. starts[s + 1] - 1 of T and attends to
+ * itself: the row of token i and query head h gets
+ *     O = sum_n w_in v_n / G,  G = sum_n w_in,  w_in = f_p(qk_scale q^_i . k^_n)
+ * over the sequence's tokens n (n <= i when causal) of key head h / (Hq / Hkv).
+ *   q, k, v   : [T, Hq | Hkv, D] with strides[0 | 1 | 2] (batch unread; NULL:
+ *               contiguous), standardised by the call as fastmax_fwd does
+ *   starts    : int32 [S + 1] on the device, ascending; empty sequences may be
+ *               among them.  Values outside 0 .. T count as the nearest bound;
+ *               sequences that overlap give undefined rows.
+ *   out       : [T, Hq, D] contiguous; g: float32 [T, Hq], NULL to skip
+ *   workspace : fastmax_packed_workspace_bytes (backward = 0)
+ * T * Hq <= 2^30, S <= 2^20.  Every pair is computed: the cost grows with the
+ * square of a sequence's length (fastmax_fwd on the sequences one by one takes
+ * the factorised kernels where these are faster).
+ * Rows of no sequence are not written (their inputs may be read).  What one
+ * sequence holds does not touch another, and what a row does not see does not
+ * touch it, not finite values among it; a value that is not finite makes its
+ * channel of the rows that see it not finite.  bf16: v's rows (backward: dout's
+ * too) enter fp16 products under a power of two each, outputs and gradients
+ * keep bf16's accuracy beside rows up to 2^12 larger; float32: float32 products.
+ *
+ * Backward: gradients of sum(dout * O), from the forward's out and g.
+ *   dout       : [T, Hq, D] contiguous
+ *   dq, dk, dv : with dstrides[0 | 1 | 2] (NULL: contiguous; no two rows may share
+ *                memory); dk and dv are sums over the query heads that share them
+ *   workspace  : fastmax_packed_workspace_bytes (backward = 1)
+ * A row of q, k, v, out or dout that is not finite makes the gradient rows that
+ * it enters not finite.  Sums run in a fixed order: equal calls give equal bits.
+ */
+size_t fastmax_packed_workspace_bytes(int S, int T, int Hq, int Hkv, int D, fastmax_dtype_t dt,
+                                      int backward);
+int fastmax_packed_fwd(const void *q, const void *k, const void *v,
+                       const fastmax_strides_t *strides, const int32_t *starts, void *out, float *g,
+                       int S, int T, int Hq, int Hkv, int D, int p, int causal, float qk_scale,
+                       fastmax_dtype_t dt, void *workspace, size_t workspace_bytes,
+                       hipStream_t stream);
+int fastmax_packed_bwd(const void *q, const void *k, const void *v,
+                       const fastmax_strides_t *strides, const int32_t *starts, const void *out,
+                       const void *dout, const float *g, void *dq, void *dk, void *dv,
+                       const fastmax_strides_t *dstrides, int S, int T, int Hq, int Hkv, int D,
+                       int p, int causal, float qk_scale, fastmax_dtype_t dt, void *workspace,
+                       size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

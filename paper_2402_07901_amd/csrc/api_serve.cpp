@@ -214,6 +214,33 @@ size_t paged_bytes(bool q8, int S, int T, int Hq, int Hkv, int D, int max_q, int
     return fm::paged_workspace(plan_of(q8, S, Hq, Hkv, D, max_q, max_len, window, sinks, dt), T, Hq, D);
 }
 
+// The packed attention's arguments (backward: with dout, dq, dk, dv).
+int check_packed(fm::PackedArgs *a, const void *q, const void *k, const void *v, const fastmax_strides_t *strides,
+                 const int32_t *starts, const void *out, const float *g, int S, int T, int Hq, int Hkv, int D, int p,
+                 int causal, float qk_scale, int dt)
+{
+    int rc = check_sizes(T, Hq, Hkv, D, dt);
+    if (rc != FASTMAX_OK) return rc;
+    if (S < 1 || S > (1 << 20) || (long long)T * Hq > INT_MAX / 2) return FASTMAX_EINVAL;
+    if ((p != 1 && p != 2) || (causal != 0 && causal != 1)) return FASTMAX_EINVAL;
+    if (!(qk_scale > 0.0f && qk_scale <= 1.0f)) return FASTMAX_EINVAL;
+    if ((rc = check_rows(strides, 3, 1, T, Hq, Hkv, D, dt, false, &a->qs, &a->ks, &a->vs)) != FASTMAX_OK) return rc;
+    const void *ptrs[] = {q, k, v, out};
+    if ((rc = check_ptrs(ptrs, 4)) != FASTMAX_OK) return rc;
+    if (!starts) return FASTMAX_ENULL;
+    if (!aligned(starts, 4) || !aligned(g, 16)) return FASTMAX_EALIGN;
+    a->q = q, a->k = k, a->v = v, a->starts = starts, a->out = (void *)out, a->g = (float *)g;
+    a->S = S, a->T = T, a->Hq = Hq, a->Hkv = Hkv, a->group = Hq / Hkv, a->p = p, a->causal = causal;
+    a->tau = qk_scale;
+    return FASTMAX_OK;
+}
+
+int check_workspace(const void *workspace, size_t bytes, size_t need)
+{
+    if (need > 0 && (!workspace || bytes < need)) return FASTMAX_EWORKSPACE;
+    return aligned(workspace, 16) ? FASTMAX_OK : FASTMAX_EALIGN;
+}
+
 }  // namespace
 
 extern "C" {
@@ -367,6 +394,48 @@ int fastmax_paged_fwd_q8(const void *q, const fastmax_strides_t *q_strides, cons
     if (rc != FASTMAX_OK) return rc;
     a.k_scale = k_scale, a.v_scale = v_scale;
     return fm::code_of(fm::paged_q8_fwd(a, plan, D, dt == FASTMAX_BF16, workspace, stream));
+}
+
+size_t fastmax_packed_workspace_bytes(int S, int T, int Hq, int Hkv, int D, fastmax_dtype_t dt_arg, int backward)
+{
+    const int dt = dt_bits(&dt_arg);
+    if (check_sizes(T, Hq, Hkv, D, dt) != FASTMAX_OK || S < 1 || S > (1 << 20) || (long long)T * Hq > INT_MAX / 2) return 0;
+    return fm::packed_workspace(T, Hq, Hkv, D, dt == FASTMAX_BF16, backward);
+}
+
+int fastmax_packed_fwd(const void *q, const void *k, const void *v, const fastmax_strides_t *strides,
+                       const int32_t *starts, void *out, float *g, int S, int T, int Hq, int Hkv, int D, int p,
+                       int causal, float qk_scale, fastmax_dtype_t dt_arg, void *workspace, size_t workspace_bytes,
+                       hipStream_t stream)
+{
+    const int dt = dt_bits(&dt_arg), bf16 = dt == FASTMAX_BF16;
+    fm::PackedArgs a = {};
+    int rc = check_packed(&a, q, k, v, strides, starts, out, g, S, T, Hq, Hkv, D, p, causal, qk_scale, dt);
+    if (rc != FASTMAX_OK) return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, fm::packed_workspace(T, Hq, Hkv, D, bf16, 0))) != FASTMAX_OK)
+        return rc;
+    if ((rc = fm::check_stream(stream)) != FASTMAX_OK) return rc;
+    return fm::code_of(fm::packed_fwd(a, D, bf16, workspace, stream));
+}
+
+int fastmax_packed_bwd(const void *q, const void *k, const void *v, const fastmax_strides_t *strides,
+                       const int32_t *starts, const void *out, const void *dout, const float *g, void *dq, void *dk,
+                       void *dv, const fastmax_strides_t *dstrides, int S, int T, int Hq, int Hkv, int D, int p,
+                       int causal, float qk_scale, fastmax_dtype_t dt_arg, void *workspace, size_t workspace_bytes,
+                       hipStream_t stream)
+{
+    const int dt = dt_bits(&dt_arg), bf16 = dt == FASTMAX_BF16;
+    fm::PackedArgs a = {};
+    int rc = check_packed(&a, q, k, v, strides, starts, out, g, S, T, Hq, Hkv, D, p, causal, qk_scale, dt);
+    if (rc != FASTMAX_OK) return rc;
+    if ((rc = check_rows(dstrides, 3, 1, T, Hq, Hkv, D, dt, true, &a.dqs, &a.dks, &a.dvs)) != FASTMAX_OK) return rc;
+    const void *ptrs[] = {g, dout, dq, dk, dv};
+    if ((rc = check_ptrs(ptrs, 5)) != FASTMAX_OK) return rc;
+    if ((rc = check_workspace(workspace, workspace_bytes, fm::packed_workspace(T, Hq, Hkv, D, bf16, 1))) != FASTMAX_OK)
+        return rc;
+    if ((rc = fm::check_stream(stream)) != FASTMAX_OK) return rc;
+    a.dout = dout, a.dq = dq, a.dk = dk, a.dv = dv;
+    return fm::code_of(fm::packed_bwd(a, D, bf16, workspace, stream));
 }
 
 }  // extern "C"

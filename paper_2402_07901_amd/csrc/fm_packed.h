@@ -1,0 +1,388 @@
+// Shared pieces of the packed attention (fm_packed_fwd.hip, fm_packed_bwd.hip):
+// sequences one after the other in [T, H, D] rows, query heads sharing key heads.
+//
+// Rows are the (token, query head) pairs of a key head, token by token; a
+// sequence's rows of one key head form the "row" side, its keys the "key" side.
+// A wave holds 32 rows or keys of one side as its columns, in registers, and
+// walks over the other side 32 at a time, 64 (float32, D = 128: 32) to an LDS
+// tile for a workgroup's four waves:
+//   S = X own^T          32x32 scores: X the tile, own the columns
+//   acc += X^T w         w made of S, element for element where S left it
+// (lane = 32 hh + c32; accumulator register i: column c32, row 8 (i/4) + 4 hh + i%4.)
+//
+// bf16 calls work on fp16: q^ and k^ (|x| <= sqrt D) have three bits more than
+// bf16; a row of v (dO) is an exact fp16 row times a power of two of its own,
+// which leaves all but what is 2^-17 of the row's largest.  The powers go into
+// the weights, relative to the largest among the tiles so far: a wave that meets
+// a larger one scales its sums down.  32x32x16 MFMA: one 16-byte LDS read per
+// lane and 16 channels for scores, the transposing read for X^T.
+// float32 calls: float32 MFMA (32x32x2), operands in full, no powers.
+//
+// Tiles come straight from the planes that the prep kernel writes (k^, v; backward
+// also q^ and dO, [key head][row][D]) into LDS, double buffered.  LDS rows have
+// no padding: piece c of row r (16 bytes) lies at c ^ swizzle(r), which puts 8
+// consecutive rows' piece c, and pieces c, c + 1 of 4 consecutive rows, on
+// distinct banks.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fm_common.h"
+#include "fm_internal.h"
+#include "fm_pairs_rows.h"
+#include "fm_serve.h"
+
+namespace fm {
+namespace packed {
+
+using pr::f16v;
+using pr::h8;
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+constexpr int THREADS = 256, COLS = 128;   // columns of a workgroup
+constexpr int WAIT_LOADS = 0x0f70;         // vmcnt(0), the other counters at their most
+constexpr int NO_POWER = -1000;            // of a row of zeros
+
+template <typename T> struct plane_of { typedef float type; };
+template <> struct plane_of<bf16_t> { typedef _Float16 type; };
+
+__device__ __forceinline__ int scalar(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+template <int C> __device__ __forceinline__ int swizzle(int r)
+{
+    if constexpr (C >= 8) return (r & 3) << 1 | (r >> 2 & 1);
+    else if constexpr (C == 4) return (r >> 1 & 1) << 1 | (r >> 2 & 1);   // two rows to a line of banks
+    else return r >> 2 & 1;
+}
+
+// 16 bytes of every lane from global memory to LDS at `to` + 16 lane.
+__device__ __forceinline__ void to_lds(const void *from, void *to)
+{
+    typedef const uint32_t __attribute__((address_space(1))) *gp;
+    typedef uint32_t __attribute__((address_space(3))) *lp;
+    __builtin_amdgcn_global_load_lds((gp)from, (lp)to, 16, 0, 0);
+}
+
+// Largest over a wave's lanes.
+__device__ __forceinline__ int wave_max(int x)
+{
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x140, 0xF, 0xF, true));
+    const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+    x = max((int)a[0], (int)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
+    return scalar(max((int)b[0], (int)b[1]));
+}
+
+// What a wave does with rows 32 kb .. 32 kb + 31 of a tile t.
+template <typename E, int D> struct Ops;
+
+template <int D> struct Ops<_Float16, D> {
+    typedef _Float16 E;
+    static constexpr int C = D / 8, KS = D / 16, DT = D < 32 ? 1 : D / 32, TILE = 64;
+    static constexpr bool POWERS = true;
+    struct Own { u4 x[KS]; };
+    struct Turned { u4 x[2][DT]; };
+
+    static __device__ __forceinline__ void own(Own &o, const E *row, int hh)
+    {
+#pragma unroll
+        for (int k = 0; k < KS; ++k) o.x[k] = *(const u4 *)(row + 16 * k + 8 * hh);
+    }
+    static __device__ __forceinline__ f16v scores(const u4 *t, int kb, int hh, int c32, const Own &o)
+    {
+        u4 x[KS];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) x[i] = t[(32 * kb + c32) * C + ((2 * i + hh) ^ swizzle<C>(c32))];
+        f16v s = f16v{};
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+            s = pr::mma(__builtin_bit_cast(h8, x[i]), __builtin_bit_cast(h8, o.x[i]), s);
+        return s;
+    }
+    // X^T: rows {4 hh .. + 3, 8 + 4 hh .. + 3} of 16, channel c32 of 32 (D = 16: the
+    // upper 16 repeat the lower)
+    static __device__ __forceinline__ void turn(Turned &a, const u4 *t, int kb, int lane)
+    {
+        const s4 *v = (const s4 *)t;
+        const int j = lane >> 2 & 3, hh = lane >> 5;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                typedef s4 __attribute__((address_space(3))) *lp;
+                const int r = 32 * kb + 16 * m + 4 * hh + j;
+                const int c = 4 * d + (D < 32 ? 0 : 2 * (lane >> 4 & 1)) + (lane >> 1 & 1);
+                const int at = 2 * (r * C + (c ^ swizzle<C>(4 * hh + j))) + (lane & 1);
+                const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(v + at));
+                const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(v + at + 2 * 8 * C));
+                const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
+                a.x[m][d] = u4{l.x, l.y, h.x, h.y};
+            }
+        }
+    }
+    // Whether an element of the operand is infinite or NaN.
+    static __device__ __forceinline__ bool odd(const Turned &a)
+    {
+        typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+        us2 most = {0, 0};
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t x = a.x[m][d][i];   // (a bit cast of the vector's element itself reads its first)
+                    most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, x) << 1);
+                }
+        return most[0] >= 0xf800 || most[1] >= 0xf800;
+    }
+    static __device__ __forceinline__ void add(f16v *acc, const Turned &a, const float *w)
+    {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            h8 b;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const pr::h2 p = pr::cvt2(w[8 * m + i], w[8 * m + i + 1]);
+                b[i] = p[0];
+                b[i + 1] = p[1];
+            }
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] = pr::mma(__builtin_bit_cast(h8, a.x[m][d]), b, acc[d]);
+        }
+    }
+    // the channel of register i of accumulator d, the first of 4 neighbours if i % 4 == 0
+    static __device__ __forceinline__ int channel(int d, int i, int hh) { return 32 * d + 8 * (i / 4) + 4 * hh + i % 4; }
+    static __device__ __forceinline__ float at(const u4 *t, int r, int ch)
+    {
+        return (float)((const E *)(t + r * C + ((ch / 8) ^ swizzle<C>(r))))[ch % 8];
+    }
+};
+
+template <int D> struct Ops<float, D> {
+    typedef float E;
+    static constexpr int C = D / 4, DT = D < 32 ? 1 : D / 32, TILE = D == 128 ? 32 : 64;
+    static constexpr bool POWERS = false;
+    struct Own { f4 x[D / 8]; };
+    struct Turned { float x[16][DT]; };
+
+    // the lanes of half hh hold channels hh D/2 .. (hh + 1) D/2
+    static __device__ __forceinline__ void own(Own &o, const E *row, int hh)
+    {
+#pragma unroll
+        for (int j = 0; j < C / 2; ++j) o.x[j] = *(const f4 *)(row + hh * (D / 2) + 4 * j);
+    }
+    static __device__ __forceinline__ f16v scores(const u4 *t, int kb, int hh, int c32, const Own &o)
+    {
+        f16v s = f16v{};
+#pragma unroll
+        for (int j = 0; j < C / 2; ++j) {
+            const f4 x = __builtin_bit_cast(f4, t[(32 * kb + c32) * C + ((hh * (C / 2) + j) ^ swizzle<C>(c32))]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], o.x[j][i], s, 0, 0, 0);
+        }
+        return s;
+    }
+    // rows 8 (i/4) + 4 hh + i%4, DT neighbouring channels from c32 DT on (D = 16: the
+    // upper lanes repeat the lower)
+    static __device__ __forceinline__ void turn(Turned &a, const u4 *t, int kb, int lane)
+    {
+        const int hh = lane >> 5, ch = (lane & (D < 32 ? 15 : 31)) * DT;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = 32 * kb + 8 * (i / 4) + 4 * hh + i % 4;
+            const float *v = (const float *)(t + r * C + ((ch / 4) ^ swizzle<C>(r))) + ch % 4;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) a.x[i][d] = v[d];
+        }
+    }
+    static __device__ __forceinline__ bool odd(const Turned &a)
+    {
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) most = max(most, __float_as_uint(a.x[i][d]) << 1);
+        return most >= 0xff000000u;
+    }
+    static __device__ __forceinline__ void add(f16v *acc, const Turned &a, const float *w)
+    {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[i][d], w[i], acc[d], 0, 0, 0);
+    }
+    static __device__ __forceinline__ int channel(int d, int i, int hh) { return (8 * (i / 4) + 4 * hh + i % 4) * DT + d; }
+    static __device__ __forceinline__ float at(const u4 *t, int r, int ch)
+    {
+        return ((const float *)(t + r * C + ((ch / 4) ^ swizzle<C>(r))))[ch % 4];
+    }
+};
+
+// acc += X^T w over a block of which some columns do not see every row.  An
+// infinity or a NaN in the block would make NaN of weight 0, so such a block is
+// added row by row, to the columns that see the row (bit i of seen: register i).
+template <typename E, int D>
+__device__ __forceinline__ void add_masked(f16v *acc, const u4 *t, int kb, int lane, const typename Ops<E, D>::Turned &a,
+                                           const float *w, uint32_t seen)
+{
+    using O = Ops<E, D>;
+    if (!__any(O::odd(a))) {
+        O::add(acc, a, w);
+        return;
+    }
+    const int hh = lane >> 5;
+#pragma unroll 1
+    for (int r = 0; r < 32; ++r) {
+        const int reg = r / 8 * 4 + r % 4, from = (lane & 31) + 32 * (r / 4 % 2);
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x = i == reg ? w[i] : x;
+        x = __shfl(x, from);
+        const bool see = __shfl((int)(seen >> reg & 1u), from);
+        if (!see) continue;
+#pragma unroll
+        for (int d = 0; d < O::DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int ch = O::channel(d, i, hh);
+                if (D >= 32 || ch < D) acc[d][i] = fmaf(x, O::at(t, 32 * kb + r, ch), acc[d][i]);
+            }
+    }
+}
+
+// A sequence's tokens [t0, t0 + len) and the workgroup's first column in it.
+struct Place {
+    int t0, len, first;
+};
+
+// Which columns workgroup `idx` of a key head takes, of sequences whose tokens
+// have `per` columns each: sequence s has the numbers from
+// floor(starts[s] per / COLS) + s on, which are enough for it and no other's.
+// Whole waves look for it 64 sequences at a time.  len 0: nothing to do.
+__device__ __forceinline__ Place place_of(const int32_t *starts, int S, int T, int per, int idx)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, step = 1;
+    while (64LL * step < S) step *= 64;
+    for (;; step /= 64) {
+        const long long s = lo + (long long)lane * step;
+        bool below = false;
+        if (s < S) below = (long long)min(max(starts[s], 0), T) * per / COLS + s <= idx;
+        const int n = __popcll(__ballot(below));
+        if (n == 0) return Place{0, 0, 0};
+        lo += (n - 1) * step;
+        if (step == 1) break;
+    }
+    lo = scalar(lo);
+    Place p;
+    p.t0 = min(max(starts[lo], 0), T);
+    p.len = min(max(starts[lo + 1], p.t0), T) - p.t0;
+    p.first = (int)((idx - lo - (long long)p.t0 * per / COLS) * COLS);
+    if (p.first >= (long long)p.len * per) p.len = 0;
+    return Place{scalar(p.t0), scalar(p.len), scalar(p.first)};
+}
+
+// Loads tile rows r0 .. r0 + TILE - 1 of two planes (rows past `last` repeat it)
+// into LDS: the loads of a wave are every fourth.
+template <typename E, int D>
+__device__ __forceinline__ void load_tiles(const E *x, const E *y, int r0, int last, u4 *xt, u4 *yt, int wave, int lane)
+{
+    using O = Ops<E, D>;
+    constexpr int C = O::C, LR = 64 / C, N = O::TILE / LR;   // rows of a load, loads of a tile
+#pragma unroll
+    for (int i = 0; i < (2 * N + 3) / 4; ++i) {
+        const int n = wave + 4 * i;
+        if (2 * N % 4 && n >= 2 * N) break;
+        const int l0 = n % N * LR, r = l0 + lane / C;
+        const size_t off = (size_t)min(r0 + r, last) * D + 16 / sizeof(E) * (lane % C ^ swizzle<C>(r));
+        to_lds((n < N ? x : y) + off, (n < N ? xt : yt) + l0 * C);
+    }
+}
+
+// Walks over the tiles of rows [begin, end) of two planes: compute(xt, yt, r0) sees
+// tile r0 while the next one is on its way.  Four LDS arrays, restrict: a load
+// into one buffer need not be waited for before the other is read.
+template <typename E, int D, typename F>
+__device__ __forceinline__ void walk(const E *x, const E *y, int begin, int end, int last, u4 *__restrict__ x0,
+                                     u4 *__restrict__ x1, u4 *__restrict__ y0, u4 *__restrict__ y1, int wave, int lane,
+                                     F compute)
+{
+    constexpr int TILE = Ops<E, D>::TILE;
+    if (begin < end) load_tiles<E, D>(x, y, begin, last, x0, y0, wave, lane);
+    __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
+    __syncthreads();
+    if (begin + TILE < end) load_tiles<E, D>(x, y, begin + TILE, last, x1, y1, wave, lane);
+    const auto step = [&](int r0, u4 *xt, u4 *yt) {
+        compute(xt, yt, r0);
+        // the next tile is there, and this one's buffer is free
+        __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
+        __syncthreads();
+        if (r0 + 2 * TILE < end) load_tiles<E, D>(x, y, r0 + 2 * TILE, last, xt, yt, wave, lane);
+    };
+    for (int r0 = begin; r0 < end; r0 += 2 * TILE) {
+        step(r0, x0, y0);
+        if (r0 + TILE < end) step(r0 + TILE, x1, y1);
+    }
+}
+
+// Four neighbouring values (n of them where fewer) of a row.
+template <int N> __device__ __forceinline__ void put(float *p, const float *f)
+{
+    if constexpr (N == 4) *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
+    else if constexpr (N == 2) *(float2 *)p = make_float2(f[0], f[1]);
+    else *p = *f;
+}
+template <int N> __device__ __forceinline__ void put(bf16_t *p, const float *f)
+{
+    static_assert(N == 4, "a register quad");
+    *(uint2 *)p = make_uint2(mx::pack_bf16x2(f[0], f[1]), mx::pack_bf16x2(f[2], f[3]));
+}
+// Stores a column's channels as a row.
+template <typename T, int D>
+__device__ __forceinline__ void store_row(T *row, const f16v *acc, int hh)
+{
+    using O = Ops<typename plane_of<T>::type, D>;
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int N = F32 ? O::DT : 4;
+#pragma unroll
+    for (int n = 0; n < 16 * O::DT / N; ++n) {
+        // bf16: a register quad of one accumulator; float32: a register of every one
+        const int d0 = F32 ? 0 : n / 4, i0 = F32 ? n : n % 4 * 4, ch = O::channel(d0, i0, hh);
+        if (D < 32 && ch >= D) continue;
+        float f[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) f[j] = F32 ? acc[j][i0] : acc[d0][i0 + j];
+        put<N>(row + ch, f);
+    }
+}
+
+// What the prep kernel leaves (workspace), per key (key head, token) and, for the
+// backward, per row (key head, token, head in its group).
+struct RowInfo {
+    float m;        // 1 / G times 2^a is m 2^e, a the power of dO; float32: 1 / G
+    int e;
+    float delta;    // dO.O 2^-a
+    int ed;         // least power above it
+};
+template <typename E> struct Planes {
+    E *kh, *vh, *qh, *oh;
+    int *b;              // powers of v
+    float *rk, *rq;      // 1 / std of k and q
+    RowInfo *info;
+};
+size_t planes_bytes(int T, int Hq, int Hkv, int D, int is_bf16, int backward);
+template <typename E> Planes<E> planes_at(void *ws, int T, int Hq, int Hkv, int D, int backward);
+template <typename T, typename E>
+hipError_t prep(const PackedArgs &a, const Planes<E> &p, int D, int backward, hipStream_t st);
+
+inline long long workgroups(int S, int T, int per) { return (long long)T * per / COLS + S; }
+
+}  // namespace packed
+}  // namespace fm

@@ -1,0 +1,317 @@
+// Packed attention, backward (see fm_packed.h), from O and G as the other
+// backwards (Sec. 2.5): with u = 1 / G, delta_i = dO_i.O_i, t = f_p'(tau s),
+//   T_in  = t u_i (dO_i.v_n - delta_i)                (Sec. 2.3, Eq. "bound")
+//   dq^_i = tau sum_n T_in k^_n,  dk^_n = tau sum_i T_in q^_i,
+//   dv_n  = sum_i w_in u_i dO_i,
+// sums over i with every query head of the group, then the standardisation
+// backward, dx = (dx^ - mean dx^ - x^ mean(dx^ x^)) / std (Eqs. 6-7).
+//
+// The prep kernel writes q^, k^, v, dO as planes and a few words per row; one launch
+// holds two kinds of workgroups: of 128 rows over the keys (dq), and of 128 keys
+// over the rows (dk and dv, which share their scores).  No atomics: every output
+// row has one owner, equal calls give equal bits.
+//
+// Powers of two (bf16 calls).  With dO_i = 2^a_i o_i, v_n = 2^b_n x_n and
+// delta_i = 2^a_i d_i:
+//   rows:  T 2^-(a_i + E) / u_i = t (2^(b_n - E) o_i.x_n - 2^-E d_i), E >= every b_n so far
+//          and the wave's d_i, so that t (.) stays below (1 + D)^2 < 2^15;
+//   keys:  u_i 2^a_i = m_i 2^e_i, M >= every e_i so far, F >= the wave's b_n and every d_i
+//          so far:  T 2^-(M + F) = t (X_i 2^(b_n - F) o_i.x_n - Y_i),  X_i = m_i 2^(e_i - M),
+//          Y_i = X_i d_i 2^-F,  and w X_i for dv.
+// A wave that meets a larger one scales its sums down.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fm_internal.h"
+#include "fm_packed.h"
+
+namespace fm {
+namespace packed {
+
+// The standardisation backward of a wave's columns in place: x^ from the plane's
+// row, r = 1 / std.
+template <typename E, int D>
+__device__ __forceinline__ void standardise_back(const E *row, float r, f16v *acc, int hh)
+{
+    using O = Ops<E, D>;
+    float x[O::DT][16], m1 = 0.f, m2 = 0.f;
+#pragma unroll
+    for (int d = 0; d < O::DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int ch = O::channel(d, i, hh);
+            const bool in = D >= 32 || ch < D;
+            x[d][i] = in ? (float)row[in ? ch : 0] : 0.f;
+            if (!in) acc[d][i] = 0.f;
+            m1 += acc[d][i];
+            m2 = fmaf(acc[d][i], x[d][i], m2);
+        }
+    m1 = pr::half_sum(m1) * (1.0f / D);
+    m2 = pr::half_sum(m2) * (1.0f / D);
+#pragma unroll
+    for (int d = 0; d < O::DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] = (acc[d][i] - m1 - x[d][i] * m2) * r;
+}
+
+// acc times f 2^e, in steps that stay normal numbers.
+template <int DT>
+__device__ __forceinline__ void scale_up(f16v *acc, float f, int e)
+{
+    const int e0 = e / 2, e1 = e - e0;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] = __builtin_ldexpf(__builtin_ldexpf(acc[d][i], e0) * f, e1);
+}
+template <int DT>
+__device__ __forceinline__ void scale_down(f16v *acc, int e)
+{
+    const float f = __builtin_ldexpf(1.0f, max(e, -300));
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] *= f;
+}
+
+template <typename T, int D, int P>
+__device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typename plane_of<T>::type> &p, int head,
+                                           const Place &pl, u4 *x0, u4 *x1, u4 *y0, u4 *y1, f4 *factors)
+{
+    typedef typename plane_of<T>::type E;
+    using O = Ops<E, D>;
+    constexpr int DT = O::DT, TILE = O::TILE;
+    const int wave = scalar(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32, c32 = lane % 32;
+    const int rows = pl.len * a.group, wfirst = pl.first + 32 * wave;
+    const int row = min(wfirst + c32, rows - 1), t = row / a.group;
+    const size_t base = ((size_t)head * a.T + pl.t0) * a.group, keys = (size_t)head * a.T + pl.t0;
+
+    typename O::Own q, o;
+    O::own(q, p.qh + (base + row) * D, hh);
+    O::own(o, p.oh + (base + row) * D, hh);
+    const RowInfo info = p.info[base + row];
+    f16v acc[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = f16v{};
+    int power = O::POWERS ? wave_max(info.ed) : 0;   // E
+    float delta = O::POWERS ? __builtin_ldexpf(info.delta, -power) : info.delta;
+
+    const int end = a.causal ? (min(pl.first + COLS, rows) - 1) / a.group + 1 : pl.len;
+    const int whole = a.causal ? scalar(min(wfirst, rows - 1) / a.group) + 1 : pl.len;
+    const int none = a.causal ? scalar(min(wfirst + 31, rows - 1) / a.group) + 1 : pl.len;
+    const int lim = a.causal ? t : pl.len - 1;
+    const float tau = a.tau;
+    int next = 0;
+    if constexpr (O::POWERS) next = p.b[keys + min(lane, pl.len - 1)];
+
+    walk<E, D>(p.kh + keys * D, p.vh + keys * D, 0, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
+               [&](const u4 *kt, const u4 *vt, int n0) {
+        if constexpr (O::POWERS) {
+            const int b = next;
+            next = p.b[keys + min(n0 + TILE + lane, pl.len - 1)];
+            const int most = wave_max(b);
+            if (most > power) {
+                scale_down<DT>(acc, power - most);
+                power = most;
+                delta = __builtin_ldexpf(info.delta, -power);
+            }
+            ((float *)factors)[lane] = __builtin_ldexpf(1.0f, b - power);
+        }
+#pragma unroll
+        for (int kb = 0; kb < TILE / 32; ++kb) {
+            const int n1 = n0 + 32 * kb;
+            if (n1 >= none) break;
+            f16v s = O::scores(kt, kb, hh, c32, q);
+            const f16v dp = O::scores(vt, kb, hh, c32, o);
+            typename O::Turned k;
+            O::turn(k, kt, kb, lane);
+            float w[16];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f4 f;
+                if constexpr (O::POWERS) f = factors[8 * kb + 2 * j + hh];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float d = O::POWERS ? fmaf(dp[4 * j + i], f[i], -delta) : dp[4 * j + i] - delta;
+                    w[4 * j + i] = P == 2 ? fmaf(s[4 * j + i], tau, 1.0f) * d : d;
+                }
+            }
+            if (n1 + 32 <= whole) {
+                O::add(acc, k, w);
+                continue;
+            }
+            uint32_t seen = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const bool see = n1 + 8 * (i / 4) + 4 * hh + i % 4 <= lim;
+                w[i] = see ? w[i] : 0.f;
+                seen |= (uint32_t)see << i;
+            }
+            add_masked<E, D>(acc, kt, kb, lane, k, w, seen);
+        }
+    });
+
+    if (O::POWERS) scale_up<DT>(acc, tau * info.m, info.e + (power > NO_POWER ? power : 0));
+    else scale_up<DT>(acc, tau * info.m, 0);
+    standardise_back<E, D>(p.qh + (base + row) * D, p.rq[base + row], acc, hh);
+    if (wfirst + c32 >= rows) return;
+    store_row<T, D>((T *)a.dq + (pl.t0 + t) * a.dqs.token + (head * a.group + row - t * a.group) * a.dqs.head, acc, hh);
+}
+
+template <typename T, int D, int P>
+__device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typename plane_of<T>::type> &p, int head,
+                                           const Place &pl, u4 *x0, u4 *x1, u4 *y0, u4 *y1, f4 *factors)
+{
+    typedef typename plane_of<T>::type E;
+    using O = Ops<E, D>;
+    constexpr int DT = O::DT, TILE = O::TILE;
+    const int wave = scalar(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32, c32 = lane % 32;
+    const int rows = pl.len * a.group, wfirst = pl.first + 32 * wave;
+    const int n = min(wfirst + c32, pl.len - 1);
+    const size_t base = ((size_t)head * a.T + pl.t0) * a.group, keys = (size_t)head * a.T + pl.t0;
+
+    typename O::Own k, v;
+    O::own(k, p.kh + (keys + n) * D, hh);
+    O::own(v, p.vh + (keys + n) * D, hh);
+    f16v dk[DT], dv[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d) dk[d] = dv[d] = f16v{};
+    int b = 0, mine = 0, M = NO_POWER, F = 0;   // the column's power, the wave's largest
+    float f = 1.0f;                             // 2^(b - F)
+    if constexpr (O::POWERS) {
+        b = p.b[keys + n];
+        mine = F = wave_max(b);
+        f = __builtin_ldexpf(1.0f, b - F);
+    }
+    (void)mine;
+
+    // rows of tokens from the wave's (the workgroup's) first key on see it; all of
+    // the wave's keys are seen by rows of its last key's token and later
+    const int begin = a.causal ? pl.first * a.group / TILE * TILE : 0;
+    const int some = a.causal ? min(wfirst, pl.len - 1) * a.group : 0;
+    const int whole = a.causal ? min(wfirst + 31, pl.len - 1) * a.group : 0;
+    const int least = a.causal ? n * a.group : 0;
+    const float c1 = a.tau;
+    RowInfo next = p.info[base + min(begin + lane % TILE, rows - 1)];
+
+    walk<E, D>(p.qh + base * D, p.oh + base * D, begin, rows, rows - 1, x0, x1, y0, y1, wave, lane,
+               [&](const u4 *qt, const u4 *ot, int r0) {
+        const RowInfo info = next;
+        next = p.info[base + min(r0 + TILE + lane % TILE, rows - 1)];
+        float X = info.m, Y = info.m * info.delta;
+        if constexpr (O::POWERS) {
+            const int e = wave_max(info.e), d = wave_max(info.ed);
+            if (e > M || d > F) {
+                const int m = max(M, e), g = max(F, d);
+                scale_down<DT>(dv, M - m);
+                scale_down<DT>(dk, M - m + F - g);
+                M = m;
+                F = g;
+                f = __builtin_ldexpf(1.0f, b - F);
+            }
+            X = __builtin_ldexpf(info.m, info.e - M);
+            Y = X * __builtin_ldexpf(info.delta, -F);
+        }
+        if (O::TILE == 64 || lane < 32) {
+            ((float *)factors)[lane] = X;
+            ((float *)(factors + 16))[lane] = Y;
+        }
+#pragma unroll
+        for (int kb = 0; kb < TILE / 32; ++kb) {
+            const int r1 = r0 + 32 * kb;
+            if (r1 + 31 < some || r1 >= rows) continue;
+            const f16v s = O::scores(qt, kb, hh, c32, k), dp = O::scores(ot, kb, hh, c32, v);
+            float w[16], x[16];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f4 fx = factors[8 * kb + 2 * j + hh], fy = factors[16 + 8 * kb + 2 * j + hh];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float st = fmaf(s[4 * j + i], c1, 1.0f);   // f_1, and f_2'
+                    const float d = fmaf(O::POWERS ? dp[4 * j + i] * f : dp[4 * j + i], fx[i], -fy[i]);
+                    x[4 * j + i] = P == 2 ? st * d : d;
+                    w[4 * j + i] = P == 2 ? fmaf(0.5f * st, st, 0.5f) * fx[i] : st * fx[i];
+                }
+            }
+            typename O::Turned xt;
+            if (r1 >= whole && r1 + 32 <= rows) {
+                O::turn(xt, qt, kb, lane);
+                O::add(dk, xt, x);
+                O::turn(xt, ot, kb, lane);
+                O::add(dv, xt, w);
+                continue;
+            }
+            uint32_t seen = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int r = r1 + 8 * (i / 4) + 4 * hh + i % 4;
+                const bool see = r >= least && r < rows;
+                w[i] = see ? w[i] : 0.f;
+                x[i] = see ? x[i] : 0.f;
+                seen |= (uint32_t)see << i;
+            }
+            O::turn(xt, qt, kb, lane);
+            add_masked<E, D>(dk, qt, kb, lane, xt, x, seen);
+            O::turn(xt, ot, kb, lane);
+            add_masked<E, D>(dv, ot, kb, lane, xt, w, seen);
+        }
+    });
+
+    scale_up<DT>(dk, a.tau, O::POWERS && M > NO_POWER ? M + (F > NO_POWER ? F : 0) : 0);
+    scale_up<DT>(dv, 1.0f, O::POWERS && M > NO_POWER ? M : 0);
+    standardise_back<E, D>(p.kh + (keys + n) * D, p.rk[keys + n], dk, hh);
+    if (wfirst + c32 >= pl.len) return;
+    const size_t tok = pl.t0 + n;
+    store_row<T, D>((T *)a.dk + tok * a.dks.token + head * a.dks.head, dk, hh);
+    store_row<T, D>((T *)a.dv + tok * a.dvs.token + head * a.dvs.head, dv, hh);
+}
+
+// Blocks [0, key_blocks) take keys (the first of a sequence meet the most rows),
+// the others rows.
+template <typename T, int D, int P>
+__global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void bwd_kernel(
+    PackedArgs a, Planes<typename plane_of<T>::type> p, unsigned key_blocks, int row_groups)
+{
+    using O = Ops<typename plane_of<T>::type, D>;
+    __shared__ u4 x0[O::TILE * O::C], x1[O::TILE * O::C], y0[O::TILE * O::C], y1[O::TILE * O::C];
+    __shared__ f4 factors[THREADS / 64][32];
+    f4 *const mine = factors[scalar(threadIdx.x / 64)];
+    const bool keys = blockIdx.x < key_blocks;
+    const int id = keys ? blockIdx.x : blockIdx.x - key_blocks, head = id % a.Hkv;
+    const Place pl = keys ? place_of(a.starts, a.S, a.T, 1, id / a.Hkv)
+                          : place_of(a.starts, a.S, a.T, a.group, row_groups - 1 - id / a.Hkv);
+    if (pl.len == 0) return;
+    if (keys) keys_block<T, D, P>(a, p, head, pl, x0, x1, y0, y1, mine);
+    else rows_block<T, D, P>(a, p, head, pl, x0, x1, y0, y1, mine);
+}
+
+template <typename T, int D> static hipError_t launch_bwd(const PackedArgs &a, void *ws, hipStream_t st)
+{
+    typedef typename plane_of<T>::type E;
+    const long long kg = workgroups(a.S, a.T, 1), rg = workgroups(a.S, a.T, a.group);
+    if (!grid_fits((kg + rg) * a.Hkv, THREADS)) return hipErrorInvalidConfiguration;
+    const Planes<E> p = planes_at<E>(ws, a.T, a.Hq, a.Hkv, D, 1);
+    const hipError_t e = prep<T, E>(a, p, D, 1, st);
+    if (e != hipSuccess) return e;
+    const unsigned kb = (unsigned)(kg * a.Hkv), blocks = (unsigned)((kg + rg) * a.Hkv);
+    if (a.p == 2) bwd_kernel<T, D, 2><<<blocks, THREADS, 0, st>>>(a, p, kb, (int)rg);
+    else bwd_kernel<T, D, 1><<<blocks, THREADS, 0, st>>>(a, p, kb, (int)rg);
+    return hipGetLastError();
+}
+
+template <typename T> static hipError_t launch_bwd_d(const PackedArgs &a, int D, void *ws, hipStream_t st)
+{
+    switch (D) {
+    case 16: return launch_bwd<T, 16>(a, ws, st);
+    case 32: return launch_bwd<T, 32>(a, ws, st);
+    case 64: return launch_bwd<T, 64>(a, ws, st);
+    default: return launch_bwd<T, 128>(a, ws, st);
+    }
+}
+
+}  // namespace packed
+
+hipError_t packed_bwd(const PackedArgs &a, int D, int is_bf16, void *ws, hipStream_t st)
+{
+    return is_bf16 ? packed::launch_bwd_d<bf16_t>(a, D, ws, st) : packed::launch_bwd_d<float>(a, D, ws, st);
+}
+
+}  // namespace fm

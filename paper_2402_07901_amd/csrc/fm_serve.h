@@ -100,4 +100,21 @@ constexpr int CHUNK_ROWS = 128;    // rows of a workgroup of the chunk kernel
 hipError_t paged_chunk(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, float *part,
                        hipStream_t st);
 
+// Packed sequences: sequence s has the tokens starts[s] .. starts[s + 1] - 1.
+struct PackedArgs {
+    const void *q, *k, *v;         // token rows
+    Strides qs, ks, vs;            // batch unread
+    const int32_t *starts;         // [S + 1]
+    void *out;                     // [T, Hq, D]; backward: the forward's
+    float *g;                      // [T, Hq] or null; backward: the forward's
+    const void *dout;              // [T, Hq, D]
+    void *dq, *dk, *dv;
+    Strides dqs, dks, dvs;
+    int S, T, Hq, Hkv, group, p, causal;
+    float tau;
+};
+size_t packed_workspace(int T, int Hq, int Hkv, int D, int is_bf16, int backward);
+hipError_t packed_fwd(const PackedArgs &a, int D, int is_bf16, void *ws, hipStream_t st);
+hipError_t packed_bwd(const PackedArgs &a, int D, int is_bf16, void *ws, hipStream_t st);
+
 }  // namespace fm

@@ -115,6 +115,14 @@ def lib():
         L.fastmax_paged_fwd_q8.argtypes = [vp, st, vp, vp, vp, vp, st, vp, vp, vp, vp, i, i, i, i, i,
                                            i, i, i, i, i, i, f, i, i, i, vp, sz, vp]
         L.fastmax_paged_fwd_q8.restype = i
+        L.fastmax_packed_workspace_bytes.argtypes = [i, i, i, i, i, i, i]
+        L.fastmax_packed_workspace_bytes.restype = sz
+        L.fastmax_packed_fwd.argtypes = [vp, vp, vp, st, vp, vp, vp, i, i, i, i, i, i, i, f, i, vp,
+                                         sz, vp]
+        L.fastmax_packed_fwd.restype = i
+        L.fastmax_packed_bwd.argtypes = [vp, vp, vp, st, vp, vp, vp, vp, vp, vp, vp, st, i, i, i, i,
+                                         i, i, i, f, i, vp, sz, vp]
+        L.fastmax_packed_bwd.restype = i
         L.fastmax_strerror.argtypes = [i]
         L.fastmax_strerror.restype = ctypes.c_char_p
         L.fastmax_version.restype = ctypes.c_char_p
@@ -827,3 +835,75 @@ def fastmax_paged_fwd_q8(q, k_cache, v_cache, k_scale, v_scale, table, lens, q_s
          _ptr(q_start), out.data_ptr(), S, T, Hq, Hkv, D, pages, page, cols, max_q, max_len, p,
          1.0 if scale is None else scale, window, sinks, dt, _ptr(workspace), ws_n)
     return out
+
+
+# --- packed sequences ---------------------------------------------------------
+def packed_workspace_bytes(S, T, Hq, Hkv, D, dt, backward=False) -> int:
+    return int(lib().fastmax_packed_workspace_bytes(S, T, Hq, Hkv, D, dt, int(bool(backward))))
+
+
+def _packed_of(q, k, v, starts):
+    """(S, T, Hq, Hkv, D, dtype code, strides) of packed rows, checked."""
+    _on_gpu(q, 3, "[T, Hq, D]")
+    T, Hq, D = q.shape
+    dtype, dev, dt = q.dtype, q.get_device(), _dtype_code(q)
+    Hkv = k.shape[1] if k.dim() == 3 else 0
+    _rows_of("k", k, (T, Hkv, D), dtype, dev, q)
+    _rows_of("v", v, (T, Hkv, D), dtype, dev, q)
+    if starts.dim() != 1 or starts.shape[0] < 2:
+        raise ValueError(f"starts must be [S + 1], got shape {tuple(starts.shape)}")
+    _whole("starts", starts, starts.shape, _torch().int32, dev, q)
+    return (starts.shape[0] - 1, T, Hq, Hkv, D, dt,
+            _LL9(0, *q.stride()[:2], 0, *k.stride()[:2], 0, *v.stride()[:2]))
+
+
+def fastmax_packed_fwd(q, k, v, starts, p=2, causal=False, out=None, g=None, want_g=True,
+                       workspace=None, stream=None, scale=None):
+    """Fastmax attention of packed sequences: q [T, Hq, D], k and v [T, Hkv, D]
+    (strided views; D contiguous), starts int32 [S + 1]: sequence s has the tokens
+    starts[s] .. starts[s + 1] - 1 and attends to itself.  Returns (O [T, Hq, D],
+    G float32 [T, Hq]); rows of no sequence stay as they are."""
+    S, T, Hq, Hkv, D, dt, st = _packed_of(q, k, v, starts)
+    torch, dev = _torch(), q.get_device()
+    if out is None:
+        out, = _new(q, ((T, Hq, D),), stream)
+    else:
+        _whole("out", out, (T, Hq, D), q.dtype, dev, q)
+    if g is not None:
+        _whole("g", g, (T, Hq), torch.float32, dev, q)
+    elif want_g:
+        g, = _new(q, ((T, Hq),), stream, torch.float32)
+    workspace, ws_n = _workspace(q, workspace,
+                                 lambda: packed_workspace_bytes(S, T, Hq, Hkv, D, dt), stream)
+    _run("fastmax_packed_fwd", lib().fastmax_packed_fwd, dev, stream,
+         q.data_ptr(), k.data_ptr(), v.data_ptr(), st, starts.data_ptr(), out.data_ptr(), _ptr(g),
+         S, T, Hq, Hkv, D, p, 1 if causal else 0, 1.0 if scale is None else scale, dt,
+         _ptr(workspace), ws_n)
+    return out, g
+
+
+def fastmax_packed_bwd(q, k, v, starts, out, dout, g, p=2, causal=False, grads=None, workspace=None,
+                       stream=None, scale=None):
+    """Backward of fastmax_packed_fwd from its outputs: (dq [T, Hq, D], dk and dv
+    [T, Hkv, D]) of sum(dout * O); ``grads``: the same three, the caller's, strided
+    as they like.  Rows of no sequence stay as they are."""
+    S, T, Hq, Hkv, D, dt, st = _packed_of(q, k, v, starts)
+    torch, dtype, dev = _torch(), q.dtype, q.get_device()
+    _whole("out", out, (T, Hq, D), dtype, dev, q)
+    _whole("dout", dout, (T, Hq, D), dtype, dev, q)
+    _whole("g", g, (T, Hq), torch.float32, dev, q)
+    shapes = ((T, Hq, D), (T, Hkv, D), (T, Hkv, D))
+    if grads is None:
+        grads = _new(q, shapes, stream)
+    else:
+        for i, (t, shape) in enumerate(zip(grads, shapes)):
+            _rows_of(f"grads[{i}]", t, shape, dtype, dev, q)
+    workspace, ws_n = _workspace(
+        q, workspace, lambda: packed_workspace_bytes(S, T, Hq, Hkv, D, dt, True), stream)
+    _run("fastmax_packed_bwd", lib().fastmax_packed_bwd, dev, stream,
+         q.data_ptr(), k.data_ptr(), v.data_ptr(), st, starts.data_ptr(), out.data_ptr(),
+         dout.data_ptr(), g.data_ptr(), grads[0].data_ptr(), grads[1].data_ptr(),
+         grads[2].data_ptr(), _LL9(*(n for t in grads for n in (0, *t.stride()[:2]))),
+         S, T, Hq, Hkv, D, p, 1 if causal else 0, 1.0 if scale is None else scale, dt,
+         _ptr(workspace), ws_n)
+    return tuple(grads)
