@@ -400,7 +400,7 @@ size_t fastmax_packed_workspace_bytes(int S, int T, int Hq, int Hkv, int D, fast
 {
     const int dt = dt_bits(&dt_arg);
     if (check_sizes(T, Hq, Hkv, D, dt) != FASTMAX_OK || S < 1 || S > (1 << 20) || (long long)T * Hq > INT_MAX / 2) return 0;
-    return fm::packed_workspace(T, Hq, Hkv, D, dt == FASTMAX_BF16, backward);
+    return fm::packed_workspace(S, T, Hq, Hkv, D, dt == FASTMAX_BF16, backward);
 }
 
 int fastmax_packed_fwd(const void *q, const void *k, const void *v, const fastmax_strides_t *strides,
@@ -412,7 +412,7 @@ int fastmax_packed_fwd(const void *q, const void *k, const void *v, const fastma
     fm::PackedArgs a = {};
     int rc = check_packed(&a, q, k, v, strides, starts, out, g, S, T, Hq, Hkv, D, p, causal, qk_scale, dt);
     if (rc != FASTMAX_OK) return rc;
-    if ((rc = check_workspace(workspace, workspace_bytes, fm::packed_workspace(T, Hq, Hkv, D, bf16, 0))) != FASTMAX_OK)
+    if ((rc = check_workspace(workspace, workspace_bytes, fm::packed_workspace(S, T, Hq, Hkv, D, bf16, 0))) != FASTMAX_OK)
         return rc;
     if ((rc = fm::check_stream(stream)) != FASTMAX_OK) return rc;
     return fm::code_of(fm::packed_fwd(a, D, bf16, workspace, stream));
@@ -431,7 +431,7 @@ int fastmax_packed_bwd(const void *q, const void *k, const void *v, const fastma
     if ((rc = check_rows(dstrides, 3, 1, T, Hq, Hkv, D, dt, true, &a.dqs, &a.dks, &a.dvs)) != FASTMAX_OK) return rc;
     const void *ptrs[] = {g, dout, dq, dk, dv};
     if ((rc = check_ptrs(ptrs, 5)) != FASTMAX_OK) return rc;
-    if ((rc = check_workspace(workspace, workspace_bytes, fm::packed_workspace(T, Hq, Hkv, D, bf16, 1))) != FASTMAX_OK)
+    if ((rc = check_workspace(workspace, workspace_bytes, fm::packed_workspace(S, T, Hq, Hkv, D, bf16, 1))) != FASTMAX_OK)
         return rc;
     if ((rc = fm::check_stream(stream)) != FASTMAX_OK) return rc;
     a.dout = dout, a.dq = dq, a.dk = dk, a.dv = dv;

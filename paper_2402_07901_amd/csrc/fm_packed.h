@@ -21,8 +21,14 @@
 // Tiles come straight from the planes that the prep kernel writes (k^, v; backward
 // also q^ and dO, [key head][row][D]) into LDS, double buffered.  LDS rows have
 // no padding: piece c of row r (16 bytes) lies at c ^ swizzle(r), which puts 8
-// consecutive rows' piece c, and pieces c, c + 1 of 4 consecutive rows, on
-// distinct banks.
+// consecutive rows' piece c, and pieces c, c + 1 of 4 consecutive rows, on distinct
+// banks.  (Over 16 rows instead, a quarter fewer conflicts: the same time in the
+// forward, 5 to 10 % longer in the backward, whose addresses take more registers.)
+//
+// What is not finite.  A tile that is contracted (X^T w) holds zeros in the place of
+// infinities and NaN, so that weight 0 of a row that does not see one leaves it out;
+// the rows that do get it at the end, from the marks that the prep kernel leaves
+// (forward: v; backward: dO), or through G and delta, which are not finite then.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -37,6 +43,7 @@ namespace fm {
 namespace packed {
 
 using pr::f16v;
+using pr::h4;
 using pr::h8;
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef short s4 __attribute__((ext_vector_type(4)));
@@ -126,43 +133,29 @@ template <int D> struct Ops<_Float16, D> {
             }
         }
     }
-    // Whether an element of the operand is infinite or NaN.
-    static __device__ __forceinline__ bool odd(const Turned &a)
-    {
-        typedef unsigned short us2 __attribute__((ext_vector_type(2)));
-        us2 most = {0, 0};
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t x = a.x[m][d][i];   // (a bit cast of the vector's element itself reads its first)
-                    most = __builtin_elementwise_max(most, __builtin_bit_cast(us2, x) << 1);
-                }
-        return most[0] >= 0xf800 || most[1] >= 0xf800;
-    }
-    static __device__ __forceinline__ void add(f16v *acc, const Turned &a, const float *w)
+    static __device__ __forceinline__ void add(f16v *acc, const Turned &a, const pr::h2 *w)
     {
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
             h8 b;
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const pr::h2 p = pr::cvt2(w[8 * m + i], w[8 * m + i + 1]);
-                b[i] = p[0];
-                b[i + 1] = p[1];
+            for (int i = 0; i < 4; ++i) {
+                b[2 * i] = w[4 * m + i][0];
+                b[2 * i + 1] = w[4 * m + i][1];
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[d] = pr::mma(__builtin_bit_cast(h8, a.x[m][d]), b, acc[d]);
         }
     }
+    static __device__ __forceinline__ void add(f16v *acc, const Turned &a, const float *w)
+    {
+        pr::h2 h[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = pr::cvt2(w[2 * i], w[2 * i + 1]);
+        add(acc, a, h);
+    }
     // the channel of register i of accumulator d, the first of 4 neighbours if i % 4 == 0
     static __device__ __forceinline__ int channel(int d, int i, int hh) { return 32 * d + 8 * (i / 4) + 4 * hh + i % 4; }
-    static __device__ __forceinline__ float at(const u4 *t, int r, int ch)
-    {
-        return (float)((const E *)(t + r * C + ((ch / 8) ^ swizzle<C>(r))))[ch % 8];
-    }
 };
 
 template <int D> struct Ops<float, D> {
@@ -202,15 +195,6 @@ template <int D> struct Ops<float, D> {
             for (int d = 0; d < DT; ++d) a.x[i][d] = v[d];
         }
     }
-    static __device__ __forceinline__ bool odd(const Turned &a)
-    {
-        uint32_t most = 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-#pragma unroll
-            for (int d = 0; d < DT; ++d) most = max(most, __float_as_uint(a.x[i][d]) << 1);
-        return most >= 0xff000000u;
-    }
     static __device__ __forceinline__ void add(f16v *acc, const Turned &a, const float *w)
     {
 #pragma unroll
@@ -219,117 +203,120 @@ template <int D> struct Ops<float, D> {
             for (int d = 0; d < DT; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[i][d], w[i], acc[d], 0, 0, 0);
     }
     static __device__ __forceinline__ int channel(int d, int i, int hh) { return (8 * (i / 4) + 4 * hh + i % 4) * DT + d; }
-    static __device__ __forceinline__ float at(const u4 *t, int r, int ch)
-    {
-        return ((const float *)(t + r * C + ((ch / 4) ^ swizzle<C>(r))))[ch % 4];
-    }
 };
 
-// acc += X^T w over a block of which some columns do not see every row.  An
-// infinity or a NaN in the block would make NaN of weight 0, so such a block is
-// added row by row, to the columns that see the row (bit i of seen: register i).
-template <typename E, int D>
-__device__ __forceinline__ void add_masked(f16v *acc, const u4 *t, int kb, int lane, const typename Ops<E, D>::Turned &a,
-                                           const float *w, uint32_t seen)
+// The infinities and NaN of marked rows to the columns that see them.  marked(r): is
+// row r; begin a multiple of 64; from(r): its channels; sees(r): the lane's column.
+template <typename T, int D, typename M, typename F, typename S>
+__device__ __forceinline__ void add_odd(f16v *acc, int begin, int end, int lane, M marked, F from, S sees)
 {
-    using O = Ops<E, D>;
-    if (!__any(O::odd(a))) {
-        O::add(acc, a, w);
-        return;
-    }
-    const int hh = lane >> 5;
+    using O = Ops<typename plane_of<T>::type, D>;
 #pragma unroll 1
-    for (int r = 0; r < 32; ++r) {
-        const int reg = r / 8 * 4 + r % 4, from = (lane & 31) + 32 * (r / 4 % 2);
-        float x = 0.f;
+    for (int r0 = begin; r0 < end; r0 += 64) {
+        uint64_t odd = __ballot(r0 + lane < end && marked(r0 + lane));
+#pragma unroll 1
+        while (odd) {
+            const int r = r0 + __builtin_ctzll(odd);
+            odd &= odd - 1;
+            const T *row = from(r);
+            const bool see = sees(r);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x = i == reg ? w[i] : x;
-        x = __shfl(x, from);
-        const bool see = __shfl((int)(seen >> reg & 1u), from);
-        if (!see) continue;
+            for (int d = 0; d < O::DT; ++d)
 #pragma unroll
-        for (int d = 0; d < O::DT; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int ch = O::channel(d, i, hh);
-                if (D >= 32 || ch < D) acc[d][i] = fmaf(x, O::at(t, 32 * kb + r, ch), acc[d][i]);
-            }
+                for (int i = 0; i < 16; ++i) {
+                    const int ch = O::channel(d, i, lane >> 5);
+                    if (D < 32 && ch >= D) continue;
+                    const float x = io<T>::ld(row, ch);
+                    if (see && !(fabsf(x) <= 3.4028235e38f)) acc[d][i] += x;
+                }
+        }
     }
 }
 
-// A sequence's tokens [t0, t0 + len) and the workgroup's first column in it.
+// What a workgroup takes: tokens [t0, t0 + len) of a sequence, its first column
+// (a row or a key), and whether the columns are keys.  len 0: nothing to do.
 struct Place {
-    int t0, len, first;
+    int t0, len, first, keys;
 };
+__device__ __forceinline__ Place scalar(Place p) { return Place{scalar(p.t0), scalar(p.len), scalar(p.first), scalar(p.keys)}; }
 
-// Which columns workgroup `idx` of a key head takes, of sequences whose tokens
-// have `per` columns each: sequence s has the numbers from
-// floor(starts[s] per / COLS) + s on, which are enough for it and no other's.
-// Whole waves look for it 64 sequences at a time.  len 0: nothing to do.
+// The columns of sequences whose tokens have `per` of them each: sequence s has the
+// places floor(starts[s] per / COLS) + s and on, enough for it and no other's.
+inline long long places(int S, int T, int per) { return (long long)T * per / COLS + S; }
+
 __device__ __forceinline__ Place place_of(const int32_t *starts, int S, int T, int per, int idx)
 {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, step = 1;
-    while (64LL * step < S) step *= 64;
-    for (;; step /= 64) {
-        const long long s = lo + (long long)lane * step;
-        bool below = false;
-        if (s < S) below = (long long)min(max(starts[s], 0), T) * per / COLS + s <= idx;
-        const int n = __popcll(__ballot(below));
-        if (n == 0) return Place{0, 0, 0};
-        lo += (n - 1) * step;
-        if (step == 1) break;
+    const auto at = [&](int s) { return (long long)min(max(starts[s], 0), T) * per / COLS + s; };
+    int lo = 0, hi = S - 1;   // the last sequence that begins at idx or before
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (at(mid) <= idx) lo = mid;
+        else hi = mid - 1;
     }
-    lo = scalar(lo);
-    Place p;
-    p.t0 = min(max(starts[lo], 0), T);
-    p.len = min(max(starts[lo + 1], p.t0), T) - p.t0;
-    p.first = (int)((idx - lo - (long long)p.t0 * per / COLS) * COLS);
-    if (p.first >= (long long)p.len * per) p.len = 0;
-    return Place{scalar(p.t0), scalar(p.len), scalar(p.first)};
+    const long long first = (idx - at(lo)) * COLS;
+    Place p = {min(max(starts[lo], 0), T), 0, 0, 0};
+    const int len = min(max(starts[lo + 1], p.t0), T) - p.t0;
+    if (first >= 0 && first < (long long)len * per) {
+        p.len = len;
+        p.first = (int)first;
+    }
+    return p;
 }
 
 // Loads tile rows r0 .. r0 + TILE - 1 of two planes (rows past `last` repeat it)
-// into LDS: the loads of a wave are every fourth.
+// into LDS: the loads of a wave are every fourth.  A lane's place in a whole tile
+// does not change: scalar base, 32-bit offset.
 template <typename E, int D>
 __device__ __forceinline__ void load_tiles(const E *x, const E *y, int r0, int last, u4 *xt, u4 *yt, int wave, int lane)
 {
     using O = Ops<E, D>;
     constexpr int C = O::C, LR = 64 / C, N = O::TILE / LR;   // rows of a load, loads of a tile
+    const bool in = r0 + O::TILE - 1 <= last;
+    const char *const xb = (const char *)(x + (size_t)r0 * D), *const yb = (const char *)(y + (size_t)r0 * D);
 #pragma unroll
     for (int i = 0; i < (2 * N + 3) / 4; ++i) {
         const int n = wave + 4 * i;
         if (2 * N % 4 && n >= 2 * N) break;
         const int l0 = n % N * LR, r = l0 + lane / C;
-        const size_t off = (size_t)min(r0 + r, last) * D + 16 / sizeof(E) * (lane % C ^ swizzle<C>(r));
-        to_lds((n < N ? x : y) + off, (n < N ? xt : yt) + l0 * C);
+        const int at = in ? r : min(r, last - r0);   // last >= r0
+        const uint32_t off = (uint32_t)(at * D * (int)sizeof(E) + 16 * (lane % C ^ swizzle<C>(r)));
+        to_lds((n < N ? xb : yb) + off, (n < N ? xt : yt) + l0 * C);
     }
 }
 
-// Walks over the tiles of rows [begin, end) of two planes: compute(xt, yt, r0) sees
-// tile r0 while the next one is on its way.  Four LDS arrays, restrict: a load
+// Walks over the tiles of rows [begin, end) of two planes: tile r0 is worked on while
+// the next one is on its way.  The tiles of [begin2, end2), whole pairs of them, go to
+// `fast`, the ones before and after to `masked`.  Four LDS arrays, restrict: a load
 // into one buffer need not be waited for before the other is read.
-template <typename E, int D, typename F>
-__device__ __forceinline__ void walk(const E *x, const E *y, int begin, int end, int last, u4 *__restrict__ x0,
-                                     u4 *__restrict__ x1, u4 *__restrict__ y0, u4 *__restrict__ y1, int wave, int lane,
-                                     F compute)
+template <typename E, int D, typename F, typename M>
+__device__ __forceinline__ void walk(const E *x, const E *y, int begin, int begin2, int end2, int end, int last,
+                                     u4 *__restrict__ x0, u4 *__restrict__ x1, u4 *__restrict__ y0, u4 *__restrict__ y1,
+                                     int wave, int lane, F fast, M masked)
 {
     constexpr int TILE = Ops<E, D>::TILE;
     if (begin < end) load_tiles<E, D>(x, y, begin, last, x0, y0, wave, lane);
     __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
     __syncthreads();
     if (begin + TILE < end) load_tiles<E, D>(x, y, begin + TILE, last, x1, y1, wave, lane);
-    const auto step = [&](int r0, u4 *xt, u4 *yt) {
-        compute(xt, yt, r0);
-        // the next tile is there, and this one's buffer is free
+    // the next tile is there, and this one's buffer is free
+    const auto turn = [&](int r0, u4 *xt, u4 *yt) {
         __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
         __syncthreads();
         if (r0 + 2 * TILE < end) load_tiles<E, D>(x, y, r0 + 2 * TILE, last, xt, yt, wave, lane);
     };
-    for (int r0 = begin; r0 < end; r0 += 2 * TILE) {
-        step(r0, x0, y0);
-        if (r0 + TILE < end) step(r0 + TILE, x1, y1);
-    }
+    const auto pairs = [&](int r0, int to, auto &compute) {
+        for (; r0 < to; r0 += 2 * TILE) {
+            compute(x0, y0, r0);
+            turn(r0, x0, y0);
+            if (r0 + TILE < end) {
+                compute(x1, y1, r0 + TILE);
+                turn(r0 + TILE, x1, y1);
+            }
+        }
+    };
+    pairs(begin, begin2, masked);
+    pairs(begin2, end2, fast);
+    pairs(end2, end, masked);
 }
 
 // Four neighbouring values (n of them where fewer) of a row.
@@ -363,26 +350,25 @@ __device__ __forceinline__ void store_row(T *row, const f16v *acc, int hh)
     }
 }
 
-// What the prep kernel leaves (workspace), per key (key head, token) and, for the
-// backward, per row (key head, token, head in its group).
+// What the prep kernel leaves (workspace): the places, and per key (key head, token)
+// and, for the backward, per row (key head, token, head in its group):
 struct RowInfo {
     float m;        // 1 / G times 2^a is m 2^e, a the power of dO; float32: 1 / G
     int e;
     float delta;    // dO.O 2^-a
-    int ed;         // least power above it
+    int ed;         // twice the least power above it, + 1 if dO has what is not finite
 };
 template <typename E> struct Planes {
     E *kh, *vh, *qh, *oh;
-    int *b;              // powers of v
+    int *b;              // twice the power of v, + 1 if v has what is not finite
     float *rk, *rq;      // 1 / std of k and q
     RowInfo *info;
+    Place *places;
+    int n_places, sorted;
 };
-size_t planes_bytes(int T, int Hq, int Hkv, int D, int is_bf16, int backward);
-template <typename E> Planes<E> planes_at(void *ws, int T, int Hq, int Hkv, int D, int backward);
+template <typename E> Planes<E> planes_at(void *ws, const PackedArgs &a, int D, int backward);
 template <typename T, typename E>
 hipError_t prep(const PackedArgs &a, const Planes<E> &p, int D, int backward, hipStream_t st);
-
-inline long long workgroups(int S, int T, int per) { return (long long)T * per / COLS + S; }
 
 }  // namespace packed
 }  // namespace fm

@@ -22,6 +22,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fm_internal.h"
 #include "fm_packed.h"
 
@@ -91,21 +93,37 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
     f16v acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f16v{};
-    int power = O::POWERS ? wave_max(info.ed) : 0;   // E
+    int power = O::POWERS ? wave_max(info.ed >> 1) : 0;   // E
     float delta = O::POWERS ? __builtin_ldexpf(info.delta, -power) : info.delta;
 
     const int end = a.causal ? (min(pl.first + COLS, rows) - 1) / a.group + 1 : pl.len;
-    const int whole = a.causal ? scalar(min(wfirst, rows - 1) / a.group) + 1 : pl.len;
+    const int whole = (a.causal ? pl.first / a.group + 1 : pl.len) / (2 * TILE) * (2 * TILE);
     const int none = a.causal ? scalar(min(wfirst + 31, rows - 1) / a.group) + 1 : pl.len;
     const int lim = a.causal ? t : pl.len - 1;
     const float tau = a.tau;
-    int next = 0;
-    if constexpr (O::POWERS) next = p.b[keys + min(lane, pl.len - 1)];
+    int next = p.b[keys + min(lane, pl.len - 1)];
 
-    walk<E, D>(p.kh + keys * D, p.vh + keys * D, 0, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
-               [&](const u4 *kt, const u4 *vt, int n0) {
+    const auto block = [&](const f16v &s, const f16v &dp, const u4 *kt, int n1, int kb, auto masked) {
+        typename O::Turned k;
+        O::turn(k, kt, kb, lane);
+        float w[16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f4 f;
+            if constexpr (O::POWERS) f = factors[8 * kb + 2 * j + hh];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float d = O::POWERS ? fmaf(dp[4 * j + i], f[i], -delta) : dp[4 * j + i] - delta;
+                float x = P == 2 ? fmaf(s[4 * j + i], tau, 1.0f) * d : d;
+                if constexpr (decltype(masked)::value) x = n1 + 8 * j + 4 * hh + i <= lim ? x : 0.f;
+                w[4 * j + i] = x;
+            }
+        }
+        O::add(acc, k, w);
+    };
+    const auto powers = [&](int n0) {
         if constexpr (O::POWERS) {
-            const int b = next;
+            const int b = next >> 1;
             next = p.b[keys + min(n0 + TILE + lane, pl.len - 1)];
             const int most = wave_max(b);
             if (most > power) {
@@ -115,38 +133,25 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
             }
             ((float *)factors)[lane] = __builtin_ldexpf(1.0f, b - power);
         }
+    };
+    walk<E, D>(p.kh + keys * D, p.vh + keys * D, 0, 0, whole, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
+               [&](const u4 *kt, const u4 *vt, int n0) {
+        powers(n0);
+        f16v s[TILE / 32], dp[TILE / 32];
 #pragma unroll
         for (int kb = 0; kb < TILE / 32; ++kb) {
-            const int n1 = n0 + 32 * kb;
-            if (n1 >= none) break;
-            f16v s = O::scores(kt, kb, hh, c32, q);
-            const f16v dp = O::scores(vt, kb, hh, c32, o);
-            typename O::Turned k;
-            O::turn(k, kt, kb, lane);
-            float w[16];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                f4 f;
-                if constexpr (O::POWERS) f = factors[8 * kb + 2 * j + hh];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float d = O::POWERS ? fmaf(dp[4 * j + i], f[i], -delta) : dp[4 * j + i] - delta;
-                    w[4 * j + i] = P == 2 ? fmaf(s[4 * j + i], tau, 1.0f) * d : d;
-                }
-            }
-            if (n1 + 32 <= whole) {
-                O::add(acc, k, w);
-                continue;
-            }
-            uint32_t seen = 0;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const bool see = n1 + 8 * (i / 4) + 4 * hh + i % 4 <= lim;
-                w[i] = see ? w[i] : 0.f;
-                seen |= (uint32_t)see << i;
-            }
-            add_masked<E, D>(acc, kt, kb, lane, k, w, seen);
+            s[kb] = O::scores(kt, kb, hh, c32, q);
+            dp[kb] = O::scores(vt, kb, hh, c32, o);
         }
+#pragma unroll
+        for (int kb = 0; kb < TILE / 32; ++kb) block(s[kb], dp[kb], kt, n0 + 32 * kb, kb, std::false_type{});
+    },
+               [&](const u4 *kt, const u4 *vt, int n0) {
+        powers(n0);
+#pragma unroll
+        for (int kb = 0; kb < TILE / 32; ++kb)
+            if (n0 + 32 * kb < none)
+                block(O::scores(kt, kb, hh, c32, q), O::scores(vt, kb, hh, c32, o), kt, n0 + 32 * kb, kb, std::true_type{});
     });
 
     if (O::POWERS) scale_up<DT>(acc, tau * info.m, info.e + (power > NO_POWER ? power : 0));
@@ -174,31 +179,59 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
     f16v dk[DT], dv[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) dk[d] = dv[d] = f16v{};
-    int b = 0, mine = 0, M = NO_POWER, F = 0;   // the column's power, the wave's largest
-    float f = 1.0f;                             // 2^(b - F)
+    int b = 0, M = NO_POWER, F = 0;   // the column's power; the largest so far
+    float f = 1.0f;                   // 2^(b - F)
     if constexpr (O::POWERS) {
-        b = p.b[keys + n];
-        mine = F = wave_max(b);
+        b = p.b[keys + n] >> 1;
+        F = wave_max(b);
         f = __builtin_ldexpf(1.0f, b - F);
     }
-    (void)mine;
 
-    // rows of tokens from the wave's (the workgroup's) first key on see it; all of
-    // the wave's keys are seen by rows of its last key's token and later
+    // rows of tokens from the workgroup's (the wave's) first key on see it; all keys
+    // are seen by rows of the last key's token and later
     const int begin = a.causal ? pl.first * a.group / TILE * TILE : 0;
     const int some = a.causal ? min(wfirst, pl.len - 1) * a.group : 0;
-    const int whole = a.causal ? min(wfirst + 31, pl.len - 1) * a.group : 0;
+    const int whole = begin + (a.causal ? (min(pl.first + COLS - 1, pl.len - 1) * a.group - begin + 2 * TILE - 1) / (2 * TILE) * (2 * TILE) : 0);
+    const int whole_end = max(whole, begin + (rows - begin) / (2 * TILE) * (2 * TILE));
     const int least = a.causal ? n * a.group : 0;
-    const float c1 = a.tau;
+    const float tau = a.tau;
     RowInfo next = p.info[base + min(begin + lane % TILE, rows - 1)];
+    uint64_t odd = 0;
 
-    walk<E, D>(p.qh + base * D, p.oh + base * D, begin, rows, rows - 1, x0, x1, y0, y1, wave, lane,
-               [&](const u4 *qt, const u4 *ot, int r0) {
+    const auto block = [&](const f16v &s, const f16v &dp, const u4 *qt, const u4 *ot, int r1, int kb, auto masked) {
+        float w[16], x[16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const f4 fx = factors[8 * kb + 2 * j + hh], fy = factors[16 + 8 * kb + 2 * j + hh];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // f_1, and f_2'; 2 f_2 = t^2 + 1
+                const float t = fmaf(s[4 * j + i], tau, 1.0f);
+                const float d = fmaf(O::POWERS ? dp[4 * j + i] * f : dp[4 * j + i], fx[i], -fy[i]);
+                float wi = P == 2 ? fmaf(t, t, 1.0f) * fx[i] : t * fx[i], xi = P == 2 ? t * d : d;
+                if constexpr (decltype(masked)::value) {
+                    const int r = r1 + 8 * j + 4 * hh + i;
+                    const bool see = r >= least && r < rows;
+                    wi = see ? wi : 0.f;
+                    xi = see ? xi : 0.f;
+                }
+                w[4 * j + i] = wi;
+                x[4 * j + i] = xi;
+            }
+        }
+        typename O::Turned xt;
+        O::turn(xt, qt, kb, lane);
+        O::add(dk, xt, x);
+        O::turn(xt, ot, kb, lane);
+        O::add(dv, xt, w);
+    };
+    const auto powers = [&](int r0) {
         const RowInfo info = next;
+        odd |= __ballot(info.ed & 1);
         next = p.info[base + min(r0 + TILE + lane % TILE, rows - 1)];
         float X = info.m, Y = info.m * info.delta;
         if constexpr (O::POWERS) {
-            const int e = wave_max(info.e), d = wave_max(info.ed);
+            const int e = wave_max(info.e), d = wave_max(info.ed >> 1);
             if (e > M || d > F) {
                 const int m = max(M, e), g = max(F, d);
                 scale_down<DT>(dv, M - m);
@@ -214,49 +247,31 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
             ((float *)factors)[lane] = X;
             ((float *)(factors + 16))[lane] = Y;
         }
+    };
+    walk<E, D>(p.qh + base * D, p.oh + base * D, begin, min(whole, rows), min(whole_end, rows), rows, rows - 1, x0, x1, y0, y1, wave, lane,
+               [&](const u4 *qt, const u4 *ot, int r0) {
+        powers(r0);
 #pragma unroll
-        for (int kb = 0; kb < TILE / 32; ++kb) {
-            const int r1 = r0 + 32 * kb;
-            if (r1 + 31 < some || r1 >= rows) continue;
-            const f16v s = O::scores(qt, kb, hh, c32, k), dp = O::scores(ot, kb, hh, c32, v);
-            float w[16], x[16];
+        for (int kb = 0; kb < TILE / 32; ++kb)
+            block(O::scores(qt, kb, hh, c32, k), O::scores(ot, kb, hh, c32, v), qt, ot, r0 + 32 * kb, kb, std::false_type{});
+    },
+               [&](const u4 *qt, const u4 *ot, int r0) {
+        powers(r0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f4 fx = factors[8 * kb + 2 * j + hh], fy = factors[16 + 8 * kb + 2 * j + hh];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float st = fmaf(s[4 * j + i], c1, 1.0f);   // f_1, and f_2'
-                    const float d = fmaf(O::POWERS ? dp[4 * j + i] * f : dp[4 * j + i], fx[i], -fy[i]);
-                    x[4 * j + i] = P == 2 ? st * d : d;
-                    w[4 * j + i] = P == 2 ? fmaf(0.5f * st, st, 0.5f) * fx[i] : st * fx[i];
-                }
-            }
-            typename O::Turned xt;
-            if (r1 >= whole && r1 + 32 <= rows) {
-                O::turn(xt, qt, kb, lane);
-                O::add(dk, xt, x);
-                O::turn(xt, ot, kb, lane);
-                O::add(dv, xt, w);
-                continue;
-            }
-            uint32_t seen = 0;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = r1 + 8 * (i / 4) + 4 * hh + i % 4;
-                const bool see = r >= least && r < rows;
-                w[i] = see ? w[i] : 0.f;
-                x[i] = see ? x[i] : 0.f;
-                seen |= (uint32_t)see << i;
-            }
-            O::turn(xt, qt, kb, lane);
-            add_masked<E, D>(dk, qt, kb, lane, xt, x, seen);
-            O::turn(xt, ot, kb, lane);
-            add_masked<E, D>(dv, ot, kb, lane, xt, w, seen);
-        }
+        for (int kb = 0; kb < TILE / 32; ++kb)
+            if (r0 + 32 * kb + 31 >= some && r0 + 32 * kb < rows)
+                block(O::scores(qt, kb, hh, c32, k), O::scores(ot, kb, hh, c32, v), qt, ot, r0 + 32 * kb, kb, std::true_type{});
     });
 
     scale_up<DT>(dk, a.tau, O::POWERS && M > NO_POWER ? M + (F > NO_POWER ? F : 0) : 0);
-    scale_up<DT>(dv, 1.0f, O::POWERS && M > NO_POWER ? M : 0);
+    scale_up<DT>(dv, P == 2 ? 0.5f : 1.0f, O::POWERS && M > NO_POWER ? M : 0);
+    if (odd)
+        add_odd<T, D>(dv, begin / 64 * 64, rows, lane, [&](int r) { return p.info[base + r].ed & 1; },
+                      [&](int r) {
+                          const int t = r / a.group;
+                          return (const T *)a.dout + ((size_t)(pl.t0 + t) * a.Hq + head * a.group + r - t * a.group) * D;
+                      },
+                      [&](int r) { return r >= least; });
     standardise_back<E, D>(p.kh + (keys + n) * D, p.rk[keys + n], dk, hh);
     if (wfirst + c32 >= pl.len) return;
     const size_t tok = pl.t0 + n;
@@ -264,36 +279,30 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
     store_row<T, D>((T *)a.dv + tok * a.dvs.token + head * a.dvs.head, dv, hh);
 }
 
-// Blocks [0, key_blocks) take keys (the first of a sequence meet the most rows),
-// the others rows.
 template <typename T, int D, int P>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void bwd_kernel(
-    PackedArgs a, Planes<typename plane_of<T>::type> p, unsigned key_blocks, int row_groups)
+__global__ __launch_bounds__(THREADS, D == 128 ? 1 : 2) void bwd_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p)
 {
     using O = Ops<typename plane_of<T>::type, D>;
     __shared__ u4 x0[O::TILE * O::C], x1[O::TILE * O::C], y0[O::TILE * O::C], y1[O::TILE * O::C];
     __shared__ f4 factors[THREADS / 64][32];
     f4 *const mine = factors[scalar(threadIdx.x / 64)];
-    const bool keys = blockIdx.x < key_blocks;
-    const int id = keys ? blockIdx.x : blockIdx.x - key_blocks, head = id % a.Hkv;
-    const Place pl = keys ? place_of(a.starts, a.S, a.T, 1, id / a.Hkv)
-                          : place_of(a.starts, a.S, a.T, a.group, row_groups - 1 - id / a.Hkv);
+    const int head = blockIdx.x % a.Hkv;
+    const Place pl = scalar(p.places[blockIdx.x / a.Hkv]);
     if (pl.len == 0) return;
-    if (keys) keys_block<T, D, P>(a, p, head, pl, x0, x1, y0, y1, mine);
+    if (pl.keys) keys_block<T, D, P>(a, p, head, pl, x0, x1, y0, y1, mine);
     else rows_block<T, D, P>(a, p, head, pl, x0, x1, y0, y1, mine);
 }
 
 template <typename T, int D> static hipError_t launch_bwd(const PackedArgs &a, void *ws, hipStream_t st)
 {
     typedef typename plane_of<T>::type E;
-    const long long kg = workgroups(a.S, a.T, 1), rg = workgroups(a.S, a.T, a.group);
-    if (!grid_fits((kg + rg) * a.Hkv, THREADS)) return hipErrorInvalidConfiguration;
-    const Planes<E> p = planes_at<E>(ws, a.T, a.Hq, a.Hkv, D, 1);
+    const Planes<E> p = planes_at<E>(ws, a, D, 1);
+    const long long blocks = (long long)p.n_places * a.Hkv;
+    if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
     const hipError_t e = prep<T, E>(a, p, D, 1, st);
     if (e != hipSuccess) return e;
-    const unsigned kb = (unsigned)(kg * a.Hkv), blocks = (unsigned)((kg + rg) * a.Hkv);
-    if (a.p == 2) bwd_kernel<T, D, 2><<<blocks, THREADS, 0, st>>>(a, p, kb, (int)rg);
-    else bwd_kernel<T, D, 1><<<blocks, THREADS, 0, st>>>(a, p, kb, (int)rg);
+    if (a.p == 2) bwd_kernel<T, D, 2><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
+    else bwd_kernel<T, D, 1><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
     return hipGetLastError();
 }
 

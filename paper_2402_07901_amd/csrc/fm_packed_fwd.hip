@@ -8,22 +8,87 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fm_internal.h"
 #include "fm_packed.h"
 
 namespace fm {
 namespace packed {
 
-// One thread per 8 channels of a row; blocks [0, kv_blocks): keys and values, the
-// others (backward): queries, dO and O.
-template <typename T, int D, bool BWD>
-__global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p, unsigned kv_blocks)
+// The places in the order that workgroups take them: the ones with the most work
+// first, so that none is left for the end alone (16 sequences of up to 4096 tokens,
+// 12 heads of 64: the last ones of each sequence at any time).  One workgroup counts
+// and sorts up to SORTED of them by their tiles; more of them stay in order, many
+// to every workgroup's turn.
+constexpr int SORTED = 4096, BINS = 512;
+
+template <bool BWD> __device__ __forceinline__ void plan(const PackedArgs &a, Place *out, int n, int sorted)
 {
+    const int rows = (int)((long long)a.T * a.group / COLS + a.S);   // places of rows; then (backward) of keys
+    // its place, and its work: tiles of the other side times the products of a tile
+    const auto get = [&](int i, int &work) {
+        Place p = place_of(a.starts, a.S, a.T, i < rows ? a.group : 1, i < rows ? i : i - rows);
+        p.keys = i >= rows;
+        const long long other = p.keys ? ((long long)p.len - (a.causal ? p.first : 0)) * a.group
+                                       : a.causal ? min((p.first + COLS - 1) / a.group + 1, p.len) : p.len;
+        work = p.len ? (int)min((other + 63) / 64 * (BWD ? p.keys ? 7 : 5 : 4) / 4, (long long)BINS - 2) + 1 : 0;
+        return p;
+    };
+    if (!sorted) {
+        const int i = blockIdx.x * THREADS + threadIdx.x;
+        int work;
+        if (i < n) out[n - 1 - i] = get(i, work);
+        return;
+    }
+    __shared__ int count[BINS];
+    for (int i = threadIdx.x; i < BINS; i += THREADS) count[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        int work;
+        get(i, work);
+        atomicAdd(&count[BINS - 1 - work], 1);
+    }
+    __syncthreads();
+    if (threadIdx.x < 64) {   // where each begins: 8 bins to a lane
+        int sum = 0, mine[BINS / 64];
+#pragma unroll
+        for (int j = 0; j < BINS / 64; ++j) {
+            mine[j] = sum;
+            sum += count[BINS / 64 * threadIdx.x + j];
+        }
+        int before = sum;
+        for (int o = 1; o < 64; o *= 2) {
+            const int x = __shfl_up(before, o);
+            if ((int)threadIdx.x >= o) before += x;
+        }
+#pragma unroll
+        for (int j = 0; j < BINS / 64; ++j) count[BINS / 64 * threadIdx.x + j] = before - sum + mine[j];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        int work;
+        const Place p = get(i, work);
+        out[atomicAdd(&count[BINS - 1 - work], 1)] = p;
+    }
+}
+
+// Blocks [0, plan_blocks): the places.  The others, one thread per 8 channels of a
+// row: keys and values, then (backward) queries, dO and O.
+template <typename T, int D, bool BWD>
+__global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p,
+                                                       unsigned plan_blocks, unsigned kv_blocks)
+{
+    if (blockIdx.x < plan_blocks) {
+        plan<BWD>(a, p.places, p.n_places, p.sorted);
+        return;
+    }
+    const unsigned block = blockIdx.x - plan_blocks;
     typedef typename plane_of<T>::type E;
     constexpr int L = D / 8;
     constexpr bool H = sizeof(E) == 2;
-    const bool keys = !BWD || blockIdx.x < kv_blocks;
-    const long long lane = (long long)(keys ? blockIdx.x : blockIdx.x - kv_blocks) * THREADS + threadIdx.x;
+    const bool keys = !BWD || block < kv_blocks;
+    const long long lane = (long long)(keys ? block : block - kv_blocks) * THREADS + threadIdx.x;
     const int c = (int)(lane % L), heads = keys ? a.Hkv : a.Hq;
     const bool ok = lane / L < (long long)a.T * heads;
     const int row = ok ? (int)(lane / L) : 0, t = row / heads, h = row - t * heads;
@@ -38,26 +103,36 @@ __global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<type
             *(float4 *)(to + 4) = make_float4(x[4], x[5], x[6], x[7]);
         }
     };
-    // x^ into a plane, 1 / std
+    const auto finite = [](float x) { return fabsf(x) <= 3.4028235e38f; };
+    // x^ into a plane, 1 / std; backward: zeros for what is not finite
     const auto standard = [&](const T *from, E *to) {
         m32::RawRow<T, 8> raw;
         raw.load(from + 8 * c, ok);
         const float2 st = pr::row_stats<T, D>(raw);
         float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (raw.get(i) - st.x) * st.y;
+        for (int i = 0; i < 8; ++i) {
+            x[i] = (raw.get(i) - st.x) * st.y;
+            if (BWD && !finite(x[i])) x[i] = 0.f;
+        }
         store(to + 8 * c, x);
         return st.y;
     };
-    // a row times 2^-e, e its power (returned): of its largest finite magnitude
-    const auto scaled = [&](const m32::RawRow<T, 8> &raw, E *to) {
-        float x[8], m = 0.f;
+    // a row times 2^-e, e its power, of its largest finite magnitude; returns 2 e, + 1
+    // if it has what is not finite, which is left or (clean) becomes 0
+    const auto scaled = [&](const m32::RawRow<T, 8> &raw, E *to, bool clean) {
+        float x[8], m = 0.f, odd = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             x[i] = raw.get(i);
-            m = fmaxf(m, fabsf(x[i]) <= 3.4028235e38f ? fabsf(x[i]) : 0.f);
+            if (finite(x[i])) {
+                m = fmaxf(m, fabsf(x[i]));
+            } else {
+                odd = 1.f;
+                if (clean) x[i] = 0.f;
+            }
         }
-        int e = NO_POWER;
+        int e = 0;
         if constexpr (H) {
             e = pr::exp_above(pr::group_max<L>(m));   // NO_EXP: none
             const int shift = e == pr::NO_EXP ? 0 : -e;
@@ -65,7 +140,7 @@ __global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<type
             for (int i = 0; i < 8; ++i) x[i] = __builtin_ldexpf(x[i], shift);
         }
         store(to + 8 * c, x);
-        return e;
+        return 2 * e + (pr::group_max<L>(odd) > 0.f);
     };
 
     if (keys) {
@@ -73,9 +148,9 @@ __global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<type
         const float r = standard((const T *)a.k + t * a.ks.token + h * a.ks.head, p.kh + at * D);
         m32::RawRow<T, 8> rv;
         rv.load((const T *)a.v + t * a.vs.token + h * a.vs.head + 8 * c, ok);
-        const int e = scaled(rv, p.vh + at * D);
+        const int e = scaled(rv, p.vh + at * D, !BWD);   // backward: not contracted
         if (ok && c == 0) {
-            if constexpr (H) p.b[at] = e;
+            p.b[at] = e;
             if constexpr (BWD) p.rk[at] = r;
         }
     } else if constexpr (BWD) {
@@ -85,21 +160,21 @@ __global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<type
         m32::RawRow<T, 8> ro, rd;
         ro.load((const T *)a.out + io, ok);
         rd.load((const T *)a.dout + io, ok);
-        const int e = scaled(rd, p.oh + at * D), shift = H && e != NO_POWER ? e : 0;
+        const int e = scaled(rd, p.oh + at * D, true), shift = e >> 1 == NO_POWER ? 0 : e >> 1;
         float delta = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) delta = fmaf(__builtin_ldexpf(rd.get(i), -shift), ro.get(i), delta);
         delta = pr::group_sum<L>(delta);
         if (ok && c == 0) {
             const float u = 1.0f / a.g[row];
-            RowInfo x{u, 0, delta, 0};
+            RowInfo x{u, 0, delta, e & 1};
             if constexpr (H) {
                 const int eu = pr::exp_above(fabsf(u));
                 if (eu != pr::NO_EXP) {
                     x.m = __builtin_ldexpf(u, -eu);
                     x.e = eu + shift;
                 }
-                x.ed = pr::exp_above(fabsf(delta));
+                x.ed = 2 * pr::exp_above(fabsf(delta)) + (e & 1);
             }
             p.info[at] = x;
             p.rq[at] = r;
@@ -109,19 +184,23 @@ __global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<type
 
 static size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
-template <typename E> Planes<E> planes_at(void *ws, int T, int Hq, int Hkv, int D, int backward)
+// The planes from ws on (ws null: how many bytes).
+template <typename E> static Planes<E> lay_out(char *ws, int S, int T, int Hq, int Hkv, int D, int backward, size_t *bytes)
 {
-    char *at = (char *)ws;
+    size_t at = 0;
     const auto take = [&](size_t n) {
-        char *const x = at;
+        char *const x = ws + at;
         at += up(n);
         return x;
     };
     const size_t keys = (size_t)Hkv * T, rows = (size_t)Hq * T;
     Planes<E> p = {};
+    p.n_places = (int)(places(S, T, Hq / Hkv) + (backward ? places(S, T, 1) : 0));
+    p.sorted = p.n_places <= SORTED;
     p.kh = (E *)take(keys * D * sizeof(E));
     p.vh = (E *)take(keys * D * sizeof(E));
-    p.b = (int *)take(sizeof(E) == 2 ? keys * sizeof(int) : 0);
+    p.b = (int *)take(keys * sizeof(int));
+    p.places = (Place *)take(p.n_places * sizeof(Place));
     if (backward) {
         p.qh = (E *)take(rows * D * sizeof(E));
         p.oh = (E *)take(rows * D * sizeof(E));
@@ -129,27 +208,26 @@ template <typename E> Planes<E> planes_at(void *ws, int T, int Hq, int Hkv, int 
         p.rq = (float *)take(rows * sizeof(float));
         p.info = (RowInfo *)take(rows * sizeof(RowInfo));
     }
+    *bytes = at;
     return p;
 }
-template Planes<float> planes_at(void *, int, int, int, int, int);
-template Planes<_Float16> planes_at(void *, int, int, int, int, int);
 
-size_t planes_bytes(int T, int Hq, int Hkv, int D, int is_bf16, int backward)
+template <typename E> Planes<E> planes_at(void *ws, const PackedArgs &a, int D, int backward)
 {
-    const size_t keys = (size_t)Hkv * T, rows = (size_t)Hq * T, e = is_bf16 ? 2 : 4;
-    size_t n = 2 * up(keys * D * e) + (is_bf16 ? up(keys * sizeof(int)) : 0);
-    if (backward)
-        n += 2 * up(rows * D * e) + up(keys * sizeof(float)) + up(rows * sizeof(float)) + up(rows * sizeof(RowInfo));
-    return n;
+    size_t n;
+    return lay_out<E>((char *)ws, a.S, a.T, a.Hq, a.Hkv, D, backward, &n);
 }
+template Planes<float> planes_at(void *, const PackedArgs &, int, int);
+template Planes<_Float16> planes_at(void *, const PackedArgs &, int, int);
 
 template <typename T, int D, bool BWD>
 static hipError_t prep_d(const PackedArgs &a, const Planes<typename plane_of<T>::type> &p, hipStream_t st)
 {
     const long long kv = ((long long)a.T * a.Hkv * (D / 8) + THREADS - 1) / THREADS;
     const long long q = BWD ? ((long long)a.T * a.Hq * (D / 8) + THREADS - 1) / THREADS : 0;
-    if (!grid_fits(kv + q, THREADS)) return hipErrorInvalidConfiguration;
-    prep_kernel<T, D, BWD><<<(unsigned)(kv + q), THREADS, 0, st>>>(a, p, (unsigned)kv);
+    const long long plan = p.sorted ? 1 : (p.n_places + THREADS - 1) / THREADS;
+    if (!grid_fits(plan + kv + q, THREADS)) return hipErrorInvalidConfiguration;
+    prep_kernel<T, D, BWD><<<(unsigned)(plan + kv + q), THREADS, 0, st>>>(a, p, (unsigned)plan, (unsigned)kv);
     return hipGetLastError();
 }
 
@@ -167,18 +245,17 @@ template hipError_t prep<float, float>(const PackedArgs &, const Planes<float> &
 template hipError_t prep<bf16_t, _Float16>(const PackedArgs &, const Planes<_Float16> &, int, int, hipStream_t);
 
 template <typename T, int D, int P>
-__global__ __launch_bounds__(THREADS, 2) void fwd_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p, int groups)
+__global__ __launch_bounds__(THREADS, 2) void fwd_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p)
 {
     typedef typename plane_of<T>::type E;
     using O = Ops<E, D>;
     constexpr int DT = O::DT, TILE = O::TILE;
     __shared__ u4 x0[TILE * O::C], x1[TILE * O::C], y0[TILE * O::C], y1[TILE * O::C];
-    __shared__ f4 factors[THREADS / 64][TILE / 4];
+    __shared__ h4 factors[THREADS / 64][TILE / 4];
 
-    // the last rows see the most keys and start first; a key head's workgroups
-    // are Hkv apart, on one XCD where 8 divides Hkv
+    // a key head's workgroups are Hkv apart, on one XCD where 8 divides Hkv
     const int head = blockIdx.x % a.Hkv;
-    const Place pl = place_of(a.starts, a.S, a.T, a.group, groups - 1 - blockIdx.x / a.Hkv);
+    const Place pl = scalar(p.places[blockIdx.x / a.Hkv]);
     if (pl.len == 0) return;
     const int wave = scalar(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32, c32 = lane % 32;
     const int rows = pl.len * a.group, wfirst = pl.first + 32 * wave;
@@ -212,24 +289,57 @@ __global__ __launch_bounds__(THREADS, 2) void fwd_kernel(PackedArgs a, Planes<ty
     f16v acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f16v{};
-    float g = 0.f;
+    float g = 0.f;          // second order: of 2 w = (1 + tau s)^2 + 1
     int power = NO_POWER;   // of acc: the largest of the values' so far
 
     const int end = a.causal ? (min(pl.first + COLS, rows) - 1) / a.group + 1 : pl.len;   // keys that some row sees
-    // the wave's: keys before `whole` are seen by all its rows, from `none` on by none
-    const int whole = a.causal ? scalar(min(wfirst, rows - 1) / a.group) + 1 : pl.len;
+    // keys before `whole` are seen by all rows, from `none` on by none of the wave's
+    const int whole = (a.causal ? pl.first / a.group + 1 : pl.len) / (2 * TILE) * (2 * TILE);
     const int none = a.causal ? scalar(min(wfirst + 31, rows - 1) / a.group) + 1 : pl.len;
     const int lim = a.causal ? t : pl.len - 1;
     const size_t keys = (size_t)head * a.T + pl.t0;
-    const float c1 = a.tau, c2 = 0.5f * a.tau * a.tau;
-    int next = 0;   // the next tile's powers, a key to a lane
-    if constexpr (O::POWERS) next = p.b[keys + min(lane, pl.len - 1)];
+    const float tau = a.tau;
+    int next = p.b[keys + min(lane, pl.len - 1)];   // the next tile's powers and marks, a key to a lane
+    uint64_t odd = 0;
 
-    walk<E, D>(p.kh + keys * D, p.vh + keys * D, 0, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
-               [&](const u4 *kt, const u4 *vt, int n0) {
+    // what becomes of the scores of a block of 32 keys; masked: some row does not see
+    // some of them
+    const auto block = [&](const f16v &s, const u4 *vt, int n1, int kb, auto masked) {
+        typename O::Turned v;
+        O::turn(v, vt, kb, lane);
+        float w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            w[i] = fmaf(s[i], tau, 1.0f);
+            if constexpr (P == 2) w[i] = fmaf(w[i], w[i], 1.0f);
+            if constexpr (decltype(masked)::value) w[i] = n1 + 8 * (i / 4) + 4 * hh + i % 4 <= lim ? w[i] : 0.f;
+        }
         if constexpr (O::POWERS) {
-            const int b = next;
-            next = p.b[keys + min(n0 + TILE + lane, pl.len - 1)];
+            // the sum of the rounded weights, as the numerator takes them
+            const pr::h2 one = {(_Float16)1.0f, (_Float16)1.0f};
+            pr::h2 h[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const h4 f = factors[wave][8 * kb + 2 * j + hh];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const pr::h2 x = pr::cvt2(w[4 * j + 2 * i], w[4 * j + 2 * i + 1]);
+                    g = __builtin_amdgcn_fdot2(x, one, g, false);
+                    h[2 * j + i] = x * pr::h2{f[2 * i], f[2 * i + 1]};
+                }
+            }
+            O::add(acc, v, h);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) g += w[i];
+            O::add(acc, v, w);
+        }
+    };
+    const auto powers = [&](int n0) {
+        const int b = next >> 1;
+        odd |= __ballot(next & 1);
+        next = p.b[keys + min(n0 + TILE + lane % TILE, pl.len - 1)];
+        if constexpr (O::POWERS) {
             const int most = wave_max(b);
             if (most > power) {
                 const float f = __builtin_ldexpf(1.0f, max(power - most, -300));
@@ -237,47 +347,26 @@ __global__ __launch_bounds__(THREADS, 2) void fwd_kernel(PackedArgs a, Planes<ty
                 for (int d = 0; d < DT; ++d) acc[d] *= f;
                 power = most;
             }
-            ((float *)factors[wave])[lane] = __builtin_ldexpf(1.0f, b - power);
+            ((_Float16 *)factors[wave])[lane] = (_Float16)__builtin_ldexpf(1.0f, b - power);
         }
+    };
+    walk<E, D>(p.kh + keys * D, p.vh + keys * D, 0, 0, whole, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
+               [&](const u4 *kt, const u4 *vt, int n0) {
+        powers(n0);
+        f16v s[TILE / 32];
 #pragma unroll
-        for (int kb = 0; kb < TILE / 32; ++kb) {
-            const int n1 = n0 + 32 * kb;
-            if (n1 >= none) break;
-            f16v s = O::scores(kt, kb, hh, c32, own);
-            typename O::Turned v;
-            O::turn(v, vt, kb, lane);
-            float w[16];
+        for (int kb = 0; kb < TILE / 32; ++kb) s[kb] = O::scores(kt, kb, hh, c32, own);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = P == 2 ? fmaf(fmaf(s[i], c2, c1), s[i], 1.0f) : fmaf(s[i], c1, 1.0f);
-            uint32_t seen = 0xffffu;
-            const bool all = n1 + 32 <= whole;
-            if (!all) {
-                seen = 0;
+        for (int kb = 0; kb < TILE / 32; ++kb) block(s[kb], vt, n0 + 32 * kb, kb, std::false_type{});
+    },
+               [&](const u4 *kt, const u4 *vt, int n0) {
+        powers(n0);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const bool see = n1 + 8 * (i / 4) + 4 * hh + i % 4 <= lim;
-                    w[i] = see ? w[i] : 0.f;
-                    seen |= (uint32_t)see << i;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) g += w[i];
-            if constexpr (O::POWERS) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const f4 f = factors[wave][8 * kb + 2 * j + hh];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[4 * j + i] *= f[i];
-                }
-            }
-            if (all) O::add(acc, v, w);
-            else add_masked<E, D>(acc, vt, kb, lane, v, w, seen);
-        }
+        for (int kb = 0; kb < TILE / 32; ++kb)
+            if (n0 + 32 * kb < none) block(O::scores(kt, kb, hh, c32, own), vt, n0 + 32 * kb, kb, std::true_type{});
     });
 
     const float G = pr::half_sum(g);
-    if (row >= rows) return;
-    if (a.g && hh == 0) a.g[io] = G;
     // out of the power in two factors: each a normal number
     const float f = 1.0f / G;
     const int e0 = O::POWERS && power > NO_POWER ? power / 2 : 0, e1 = O::POWERS && power > NO_POWER ? power - e0 : 0;
@@ -285,20 +374,25 @@ __global__ __launch_bounds__(THREADS, 2) void fwd_kernel(PackedArgs a, Planes<ty
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = __builtin_ldexpf(__builtin_ldexpf(acc[d][i], e0) * f, e1);
+    if (odd)
+        add_odd<T, D>(acc, 0, none, lane, [&](int n) { return p.b[keys + n] & 1; },
+                      [&](int n) { return (const T *)a.v + (pl.t0 + n) * a.vs.token + head * a.vs.head; },
+                      [&](int n) { return n <= lim; });
+    if (row >= rows) return;
+    if (a.g && hh == 0) a.g[io] = P == 2 ? 0.5f * G : G;
     store_row<T, D>((T *)a.out + io * D, acc, hh);
 }
 
 template <typename T, int D> hipError_t launch(const PackedArgs &a, void *ws, hipStream_t st)
 {
     typedef typename plane_of<T>::type E;
-    const long long groups = workgroups(a.S, a.T, a.group);
-    if (!grid_fits(groups * a.Hkv, THREADS)) return hipErrorInvalidConfiguration;
-    const Planes<E> p = planes_at<E>(ws, a.T, a.Hq, a.Hkv, D, 0);
+    const Planes<E> p = planes_at<E>(ws, a, D, 0);
+    const long long blocks = (long long)p.n_places * a.Hkv;
+    if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
     const hipError_t e = prep<T, E>(a, p, D, 0, st);
     if (e != hipSuccess) return e;
-    const unsigned blocks = (unsigned)(groups * a.Hkv);
-    if (a.p == 2) fwd_kernel<T, D, 2><<<blocks, THREADS, 0, st>>>(a, p, (int)groups);
-    else fwd_kernel<T, D, 1><<<blocks, THREADS, 0, st>>>(a, p, (int)groups);
+    if (a.p == 2) fwd_kernel<T, D, 2><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
+    else fwd_kernel<T, D, 1><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
     return hipGetLastError();
 }
 
@@ -314,9 +408,12 @@ template <typename T> hipError_t launch_d(const PackedArgs &a, int D, void *ws, 
 
 }  // namespace packed
 
-size_t packed_workspace(int T, int Hq, int Hkv, int D, int is_bf16, int backward)
+size_t packed_workspace(int S, int T, int Hq, int Hkv, int D, int is_bf16, int backward)
 {
-    return packed::planes_bytes(T, Hq, Hkv, D, is_bf16, backward);
+    size_t n;
+    if (is_bf16) packed::lay_out<_Float16>(nullptr, S, T, Hq, Hkv, D, backward, &n);
+    else packed::lay_out<float>(nullptr, S, T, Hq, Hkv, D, backward, &n);
+    return n;
 }
 
 hipError_t packed_fwd(const PackedArgs &a, int D, int is_bf16, void *ws, hipStream_t st)

@@ -113,7 +113,7 @@ struct PackedArgs {
     int S, T, Hq, Hkv, group, p, causal;
     float tau;
 };
-size_t packed_workspace(int T, int Hq, int Hkv, int D, int is_bf16, int backward);
+size_t packed_workspace(int S, int T, int Hq, int Hkv, int D, int is_bf16, int backward);
 hipError_t packed_fwd(const PackedArgs &a, int D, int is_bf16, void *ws, hipStream_t st);
 hipError_t packed_bwd(const PackedArgs &a, int D, int is_bf16, void *ws, hipStream_t st);
 

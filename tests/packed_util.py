@@ -45,7 +45,8 @@ class Head:
         ew = (1.0 if p == 1 else 1.0 + np.abs(s) + self.es) * self.es + 6 * U * size
         self.w, self.ew = np.where(self.see, w, 0.0), np.where(self.see, ew, 0.0)
         self.G = self.w.sum(-1, keepdims=True)
-        self.eG = (self.ew + (n + 64) * U * np.abs(self.w)).sum(-1, keepdims=True)
+        # (bf16 calls sum the weights that the products take, rounded to fp16)
+        self.eG = (self.ew + ((n + 64) * U + H[dtype]) * np.abs(self.w)).sum(-1, keepdims=True)
 
     def forward(self):
         """O, its bound before the output's rounding, G, its bound."""
