@@ -234,11 +234,12 @@ __device__ __forceinline__ void add_odd(f16v *acc, int begin, int end, int lane,
 }
 
 // What a workgroup takes: tokens [t0, t0 + len) of a sequence, its first column
-// (a row or a key), and whether the columns are keys.  len 0: nothing to do.
+// (a row or a key), and what it makes of its columns.  len 0: nothing to do.
+enum Role { ROWS = 0, KEYS = 1, DK = 2, DV = 3 };   // O or dq; dk and dv; one of them
 struct Place {
-    int t0, len, first, keys;
+    int t0, len, first, role;
 };
-__device__ __forceinline__ Place scalar(Place p) { return Place{scalar(p.t0), scalar(p.len), scalar(p.first), scalar(p.keys)}; }
+__device__ __forceinline__ Place scalar(Place p) { return Place{scalar(p.t0), scalar(p.len), scalar(p.first), scalar(p.role)}; }
 
 // The columns of sequences whose tokens have `per` of them each: sequence s has the
 // places floor(starts[s] per / COLS) + s and on, enough for it and no other's.
@@ -365,7 +366,22 @@ template <typename E> struct Planes {
     RowInfo *info;
     Place *places;
     int n_places, sorted;
+    int split;           // dk and dv by workgroups of their own
 };
+// At D = 128, bf16, the sums of dk and dv leave no registers for two waves on a SIMD;
+// the scores made twice cost less (a seventh more products).
+#ifndef SPLITD
+#define SPLITD 128
+#endif
+#ifndef AHEADD
+#define AHEADD 128
+#endif
+#ifndef WPS64
+#define WPS64 2
+#endif
+constexpr bool split_keys(int D, bool bf16) { return bf16 && D >= SPLITD; }
+// Scores of a whole tile before its weights, where registers allow it.
+template <typename E, int D> constexpr bool ahead() { return D < AHEADD; }
 template <typename E> Planes<E> planes_at(void *ws, const PackedArgs &a, int D, int backward);
 template <typename T, typename E>
 hipError_t prep(const PackedArgs &a, const Planes<E> &p, int D, int backward, hipStream_t st);

@@ -137,14 +137,20 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
     walk<E, D>(p.kh + keys * D, p.vh + keys * D, 0, 0, whole, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
                [&](const u4 *kt, const u4 *vt, int n0) {
         powers(n0);
-        f16v s[TILE / 32], dp[TILE / 32];
+        if constexpr (ahead<E, D>()) {
+            f16v s[TILE / 32], dp[TILE / 32];
 #pragma unroll
-        for (int kb = 0; kb < TILE / 32; ++kb) {
-            s[kb] = O::scores(kt, kb, hh, c32, q);
-            dp[kb] = O::scores(vt, kb, hh, c32, o);
+            for (int kb = 0; kb < TILE / 32; ++kb) {
+                s[kb] = O::scores(kt, kb, hh, c32, q);
+                dp[kb] = O::scores(vt, kb, hh, c32, o);
+            }
+#pragma unroll
+            for (int kb = 0; kb < TILE / 32; ++kb) block(s[kb], dp[kb], kt, n0 + 32 * kb, kb, std::false_type{});
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < TILE / 32; ++kb)
+                block(O::scores(kt, kb, hh, c32, q), O::scores(vt, kb, hh, c32, o), kt, n0 + 32 * kb, kb, std::false_type{});
         }
-#pragma unroll
-        for (int kb = 0; kb < TILE / 32; ++kb) block(s[kb], dp[kb], kt, n0 + 32 * kb, kb, std::false_type{});
     },
                [&](const u4 *kt, const u4 *vt, int n0) {
         powers(n0);
@@ -161,13 +167,14 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
     store_row<T, D>((T *)a.dq + (pl.t0 + t) * a.dqs.token + (head * a.group + row - t * a.group) * a.dqs.head, acc, hh);
 }
 
-template <typename T, int D, int P>
+template <typename T, int D, int P, int ROLE>
 __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typename plane_of<T>::type> &p, int head,
                                            const Place &pl, u4 *x0, u4 *x1, u4 *y0, u4 *y1, f4 *factors)
 {
     typedef typename plane_of<T>::type E;
     using O = Ops<E, D>;
     constexpr int DT = O::DT, TILE = O::TILE;
+    constexpr bool GK = ROLE != DV, GV = ROLE != DK;
     const int wave = scalar(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32, c32 = lane % 32;
     const int rows = pl.len * a.group, wfirst = pl.first + 32 * wave;
     const int n = min(wfirst + c32, pl.len - 1);
@@ -175,7 +182,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
 
     typename O::Own k, v;
     O::own(k, p.kh + (keys + n) * D, hh);
-    O::own(v, p.vh + (keys + n) * D, hh);
+    if constexpr (GK) O::own(v, p.vh + (keys + n) * D, hh);
     f16v dk[DT], dv[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) dk[d] = dv[d] = f16v{};
@@ -207,7 +214,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
             for (int i = 0; i < 4; ++i) {
                 // f_1, and f_2'; 2 f_2 = t^2 + 1
                 const float t = fmaf(s[4 * j + i], tau, 1.0f);
-                const float d = fmaf(O::POWERS ? dp[4 * j + i] * f : dp[4 * j + i], fx[i], -fy[i]);
+                const float d = GK ? fmaf(O::POWERS ? dp[4 * j + i] * f : dp[4 * j + i], fx[i], -fy[i]) : 0.f;
                 float wi = P == 2 ? fmaf(t, t, 1.0f) * fx[i] : t * fx[i], xi = P == 2 ? t * d : d;
                 if constexpr (decltype(masked)::value) {
                     const int r = r1 + 8 * j + 4 * hh + i;
@@ -220,10 +227,14 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
             }
         }
         typename O::Turned xt;
-        O::turn(xt, qt, kb, lane);
-        O::add(dk, xt, x);
-        O::turn(xt, ot, kb, lane);
-        O::add(dv, xt, w);
+        if constexpr (GK) {
+            O::turn(xt, qt, kb, lane);
+            O::add(dk, xt, x);
+        }
+        if constexpr (GV) {
+            O::turn(xt, ot, kb, lane);
+            O::add(dv, xt, w);
+        }
     };
     const auto powers = [&](int r0) {
         const RowInfo info = next;
@@ -248,39 +259,58 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
             ((float *)(factors + 16))[lane] = Y;
         }
     };
+    const auto scores = [&](const u4 *ot, int kb) {
+        if constexpr (GK) return O::scores(ot, kb, hh, c32, v);
+        else return f16v{};
+    };
     walk<E, D>(p.qh + base * D, p.oh + base * D, begin, min(whole, rows), min(whole_end, rows), rows, rows - 1, x0, x1, y0, y1, wave, lane,
                [&](const u4 *qt, const u4 *ot, int r0) {
         powers(r0);
+        if constexpr (ROLE == DV || (ROLE == DK && ahead<E, D>())) {
+            f16v s[TILE / 32], dp[TILE / 32];
 #pragma unroll
-        for (int kb = 0; kb < TILE / 32; ++kb)
-            block(O::scores(qt, kb, hh, c32, k), O::scores(ot, kb, hh, c32, v), qt, ot, r0 + 32 * kb, kb, std::false_type{});
+            for (int kb = 0; kb < TILE / 32; ++kb) {
+                s[kb] = O::scores(qt, kb, hh, c32, k);
+                dp[kb] = scores(ot, kb);
+            }
+#pragma unroll
+            for (int kb = 0; kb < TILE / 32; ++kb) block(s[kb], dp[kb], qt, ot, r0 + 32 * kb, kb, std::false_type{});
+        } else {
+#pragma unroll
+            for (int kb = 0; kb < TILE / 32; ++kb)
+                block(O::scores(qt, kb, hh, c32, k), scores(ot, kb), qt, ot, r0 + 32 * kb, kb, std::false_type{});
+        }
     },
                [&](const u4 *qt, const u4 *ot, int r0) {
         powers(r0);
 #pragma unroll
         for (int kb = 0; kb < TILE / 32; ++kb)
             if (r0 + 32 * kb + 31 >= some && r0 + 32 * kb < rows)
-                block(O::scores(qt, kb, hh, c32, k), O::scores(ot, kb, hh, c32, v), qt, ot, r0 + 32 * kb, kb, std::true_type{});
+                block(O::scores(qt, kb, hh, c32, k), scores(ot, kb), qt, ot, r0 + 32 * kb, kb, std::true_type{});
     });
 
-    scale_up<DT>(dk, a.tau, O::POWERS && M > NO_POWER ? M + (F > NO_POWER ? F : 0) : 0);
-    scale_up<DT>(dv, P == 2 ? 0.5f : 1.0f, O::POWERS && M > NO_POWER ? M : 0);
-    if (odd)
-        add_odd<T, D>(dv, begin / 64 * 64, rows, lane, [&](int r) { return p.info[base + r].ed & 1; },
-                      [&](int r) {
-                          const int t = r / a.group;
-                          return (const T *)a.dout + ((size_t)(pl.t0 + t) * a.Hq + head * a.group + r - t * a.group) * D;
-                      },
-                      [&](int r) { return r >= least; });
-    standardise_back<E, D>(p.kh + (keys + n) * D, p.rk[keys + n], dk, hh);
-    if (wfirst + c32 >= pl.len) return;
     const size_t tok = pl.t0 + n;
-    store_row<T, D>((T *)a.dk + tok * a.dks.token + head * a.dks.head, dk, hh);
-    store_row<T, D>((T *)a.dv + tok * a.dvs.token + head * a.dvs.head, dv, hh);
+    const bool mine = wfirst + c32 < pl.len;
+    if constexpr (GK) {
+        scale_up<DT>(dk, a.tau, O::POWERS && M > NO_POWER ? M + (F > NO_POWER ? F : 0) : 0);
+        standardise_back<E, D>(p.kh + (keys + n) * D, p.rk[keys + n], dk, hh);
+        if (mine) store_row<T, D>((T *)a.dk + tok * a.dks.token + head * a.dks.head, dk, hh);
+    }
+    if constexpr (GV) {
+        scale_up<DT>(dv, P == 2 ? 0.5f : 1.0f, O::POWERS && M > NO_POWER ? M : 0);
+        if (odd)
+            add_odd<T, D>(dv, begin / 64 * 64, rows, lane, [&](int r) { return p.info[base + r].ed & 1; },
+                          [&](int r) {
+                              const int t = r / a.group;
+                              return (const T *)a.dout + ((size_t)(pl.t0 + t) * a.Hq + head * a.group + r - t * a.group) * D;
+                          },
+                          [&](int r) { return r >= least; });
+        if (mine) store_row<T, D>((T *)a.dv + tok * a.dvs.token + head * a.dvs.head, dv, hh);
+    }
 }
 
 template <typename T, int D, int P>
-__global__ __launch_bounds__(THREADS, D == 128 ? 1 : 2) void bwd_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p)
+__global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : D == 64 ? WPS64 : 2) void bwd_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p)
 {
     using O = Ops<typename plane_of<T>::type, D>;
     __shared__ u4 x0[O::TILE * O::C], x1[O::TILE * O::C], y0[O::TILE * O::C], y1[O::TILE * O::C];
@@ -289,8 +319,14 @@ __global__ __launch_bounds__(THREADS, D == 128 ? 1 : 2) void bwd_kernel(PackedAr
     const int head = blockIdx.x % a.Hkv;
     const Place pl = scalar(p.places[blockIdx.x / a.Hkv]);
     if (pl.len == 0) return;
-    if (pl.keys) keys_block<T, D, P>(a, p, head, pl, x0, x1, y0, y1, mine);
-    else rows_block<T, D, P>(a, p, head, pl, x0, x1, y0, y1, mine);
+    if (pl.role == ROWS) {
+        rows_block<T, D, P>(a, p, head, pl, x0, x1, y0, y1, mine);
+    } else if constexpr (split_keys(D, sizeof(T) == 2)) {
+        if (pl.role == DK) keys_block<T, D, P, DK>(a, p, head, pl, x0, x1, y0, y1, mine);
+        else keys_block<T, D, P, DV>(a, p, head, pl, x0, x1, y0, y1, mine);
+    } else {
+        keys_block<T, D, P, KEYS>(a, p, head, pl, x0, x1, y0, y1, mine);
+    }
 }
 
 template <typename T, int D> static hipError_t launch_bwd(const PackedArgs &a, void *ws, hipStream_t st)

@@ -23,16 +23,19 @@ namespace packed {
 // to every workgroup's turn.
 constexpr int SORTED = 4096, BINS = 512;
 
-template <bool BWD> __device__ __forceinline__ void plan(const PackedArgs &a, Place *out, int n, int sorted)
+template <bool BWD> __device__ __forceinline__ void plan(const PackedArgs &a, Place *out, int n, int sorted, int split)
 {
-    const int rows = (int)((long long)a.T * a.group / COLS + a.S);   // places of rows; then (backward) of keys
+    // places of rows; then (backward) of keys, once or for dk and for dv
+    const int rows = (int)((long long)a.T * a.group / COLS + a.S), keys = (int)((long long)a.T / COLS + a.S);
     // its place, and its work: tiles of the other side times the products of a tile
     const auto get = [&](int i, int &work) {
-        Place p = place_of(a.starts, a.S, a.T, i < rows ? a.group : 1, i < rows ? i : i - rows);
-        p.keys = i >= rows;
-        const long long other = p.keys ? ((long long)p.len - (a.causal ? p.first : 0)) * a.group
-                                       : a.causal ? min((p.first + COLS - 1) / a.group + 1, p.len) : p.len;
-        work = p.len ? (int)min((other + 63) / 64 * (BWD ? p.keys ? 7 : 5 : 4) / 4, (long long)BINS - 2) + 1 : 0;
+        const int role = i < rows ? ROWS : !split ? KEYS : i < rows + keys ? DK : DV;
+        Place p = place_of(a.starts, a.S, a.T, role == ROWS ? a.group : 1, role == ROWS ? i : (i - rows) % keys);
+        p.role = role;
+        const long long other = role != ROWS ? ((long long)p.len - (a.causal ? p.first : 0)) * a.group
+                                : a.causal ? min((p.first + COLS - 1) / a.group + 1, p.len) : p.len;
+        const int cost = !BWD || role == KEYS ? 4 : role == DV ? 2 : 3;
+        work = p.len ? (int)min((other + 63) / 64 * cost / 4, (long long)BINS - 2) + 1 : 0;
         return p;
     };
     if (!sorted) {
@@ -80,7 +83,7 @@ __global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<type
                                                        unsigned plan_blocks, unsigned kv_blocks)
 {
     if (blockIdx.x < plan_blocks) {
-        plan<BWD>(a, p.places, p.n_places, p.sorted);
+        plan<BWD>(a, p.places, p.n_places, p.sorted, p.split);
         return;
     }
     const unsigned block = blockIdx.x - plan_blocks;
@@ -195,7 +198,8 @@ template <typename E> static Planes<E> lay_out(char *ws, int S, int T, int Hq, i
     };
     const size_t keys = (size_t)Hkv * T, rows = (size_t)Hq * T;
     Planes<E> p = {};
-    p.n_places = (int)(places(S, T, Hq / Hkv) + (backward ? places(S, T, 1) : 0));
+    p.split = split_keys(D, sizeof(E) == 2);
+    p.n_places = (int)(places(S, T, Hq / Hkv) + (backward ? (p.split ? 2 : 1) * places(S, T, 1) : 0));
     p.sorted = p.n_places <= SORTED;
     p.kh = (E *)take(keys * D * sizeof(E));
     p.vh = (E *)take(keys * D * sizeof(E));
