@@ -370,18 +370,9 @@ template <typename E> struct Planes {
 };
 // At D = 128, bf16, the sums of dk and dv leave no registers for two waves on a SIMD;
 // the scores made twice cost less (a seventh more products).
-#ifndef SPLITD
-#define SPLITD 128
-#endif
-#ifndef AHEADD
-#define AHEADD 128
-#endif
-#ifndef WPS64
-#define WPS64 2
-#endif
-constexpr bool split_keys(int D, bool bf16) { return bf16 && D >= SPLITD; }
+constexpr bool split_keys(int D, bool bf16) { return bf16 && D == 128; }
 // Scores of a whole tile before its weights, where registers allow it.
-template <typename E, int D> constexpr bool ahead() { return D < AHEADD; }
+template <typename E, int D> constexpr bool ahead() { return D < 128; }
 template <typename E> Planes<E> planes_at(void *ws, const PackedArgs &a, int D, int backward);
 template <typename T, typename E>
 hipError_t prep(const PackedArgs &a, const Planes<E> &p, int D, int backward, hipStream_t st);

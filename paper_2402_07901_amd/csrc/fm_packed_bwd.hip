@@ -310,7 +310,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
 }
 
 template <typename T, int D, int P>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : D == 64 ? WPS64 : 2) void bwd_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p)
+__global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void bwd_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p)
 {
     using O = Ops<typename plane_of<T>::type, D>;
     __shared__ u4 x0[O::TILE * O::C], x1[O::TILE * O::C], y0[O::TILE * O::C], y1[O::TILE * O::C];

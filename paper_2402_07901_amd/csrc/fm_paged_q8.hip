@@ -16,8 +16,11 @@
 // 16, two at a time, straight from the cache into registers, as fm_paged.hip.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "fm_internal.h"
 #include "fm_paged.h"
+#include "fm_pairs_rows.h"
 #include "fm_rows.h"
 #include "fm_serve.h"
 
@@ -119,6 +122,19 @@ template <int N, typename T> __device__ __forceinline__ void ld_row(const T *p, 
 {
 #pragma unroll
     for (int i = 0; i < N; i += 8) rows::ld8(p + i, x + i);
+}
+
+// Largest over a wave's lanes.
+__device__ __forceinline__ int wave_max(int x)
+{
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, true));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x140, 0xF, 0xF, true));
+    const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)x, false, false);
+    x = max((int)a[0], (int)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
+    return scalar(max((int)b[0], (int)b[1]));
 }
 
 // --- few rows -------------------------------------------------------------------
@@ -398,28 +414,43 @@ hipError_t launch_few(const PagedArgs &a, const PagedPlan &plan, float *part, hi
 template <int C> __device__ __forceinline__ int swizzle(int r)
 {
     if constexpr (C >= 8) return (r & 3) << 1 | (r >> 2 & 1);
-    else if constexpr (C == 4) return (r >> 1 & 1) << 1 | (r >> 2 & 1);   // two rows to a line of banks
-    else return r >> 2 & 1;
+    else return (r >> 1 & 1) << 1 | (r >> 2 & 1);   // two rows to a line of banks
 }
 
-__device__ __forceinline__ f16v mma(u4 a, u4 b, f16v c)
+// Four codes as fp16, exactly: 1024 + (128 + code) by its bits, then less 1152.
+__device__ __forceinline__ uint2 codes4(uint32_t w)
 {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+    const pr::h2 off = {(_Float16)1152.0f, (_Float16)1152.0f};
+    w ^= 0x80808080u;
+    const uint32_t lo = __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u), hi = __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u);
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_bit_cast(pr::h2, lo) - off),
+                      __builtin_bit_cast(uint32_t, __builtin_bit_cast(pr::h2, hi) - off));
 }
 
-// MFMA bounds it: 128 rows to a workgroup, 32 to a wave, 64 keys at a time
-// through two LDS buffers, products of 32x32 as fm_paged_chunk.hip (its layouts:
-// lane = 32 hh + c32; accumulator register i: column c32, row 8 (i/4) + 4 hh + i%4).
-// The cache's bytes go through registers, where a workgroup turns the values'
-// codes into bf16 once for its four waves; the keys' stay bytes.
+// Products with fp16 operands of FP parts (bf16 calls: one; float32: two, each the
+// rest of the one before it).  128 rows to a workgroup, 32 to a wave, 64 keys at a
+// time through two LDS buffers, products of 32x32 as fm_paged_chunk.hip (its
+// layouts: lane = 32 hh + c32; accumulator register i: column c32, row 8 (i/4) + 4 hh
+// + i%4).  The cache's bytes go through registers, where a workgroup turns its codes
+// into fp16 once for its four waves.
+//
+// Powers of two keep fp16's range.  A row of q is taken times one of its own (bf16
+// rows stay exact but for what is 2^-17 of their largest); weights times 2^-e, which
+// costs nothing in 1 + x (c1 + c2 x): with |k_n| <= 127 sqrt(D) ks_n a row's largest
+// possible weight stays below 2^14; values times 2^-P.  e and P follow from the largest
+// scales among the tiles so far: a wave that meets a larger one scales its sums.
+// What it takes per pair beside the products: ks x, the weight (2), its conversion,
+// sum and scale in packed halves (4.5 instructions in bf16).
 template <typename T, int D>
-__global__ __launch_bounds__(THREADS, 2) void many_kernel(PagedArgs a, PagedPlan plan, int pieces, float *part)
+__global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void many_kernel(PagedArgs a, PagedPlan plan, int pieces, float *part)
 {
-    constexpr int NP = PARTS<T>, ROWS = CHUNK_ROWS, WR = ROWS / 4, KB = 64;
-    constexpr int KP = D / 16, VP = D / 8, DT = D / 32;       // 16-byte pieces of a key row, a value row; channel tiles
-    constexpr int LN = KB * KP > THREADS ? KB * KP / THREADS : 1, LR = THREADS / KP;   // loads of a thread, rows of one
-    __shared__ u4 keys[2][KB * KP], values[2][KB * VP];
+    constexpr int FP = sizeof(T) == 2 ? 1 : 2, ROWS = CHUNK_ROWS, WR = ROWS / 4, KB = 64, STEP = KB / KT;
+    constexpr int C = D / 8, KS = D / 16, DT = D / 32;        // 16-byte pieces of a row, score steps, channel tiles
+    constexpr int LP = D / 16;                                // 16-byte loads of a row of codes
+    constexpr int LN = KB * LP > THREADS ? KB * LP / THREADS : 1, LR = THREADS / LP;   // loads of a thread, rows of one
+    __shared__ u4 keys0[KB * C], keys1[KB * C], values0[KB * C], values1[KB * C];
     __shared__ f4 kscale[2][KB / 4], vscale[2][KB / 4];
+    __shared__ f4 factors[THREADS / 64][KB / 4];              // of values, a wave's own (bf16: halves)
 
     // Row tiles of one (sequence, key head, split) read the same keys, so every
     // `pieces`th of them go to the same XCD.  Late row tiles see the most keys and
@@ -436,7 +467,7 @@ __global__ __launch_bounds__(THREADS, 2) void many_kernel(PagedArgs a, PagedPlan
     const int rows = seq.count * a.group, page_mask = (1 << a.page_shift) - 1;
     const int8_t *kc = (const int8_t *)a.k + head * a.cache.head, *vc = (const int8_t *)a.v + head * a.cache.head;
     const int32_t *table = a.table + (size_t)s * a.table_cols;
-    const int my_row = threadIdx.x / KP, my_piece = threadIdx.x % KP;   // of a load
+    const int my_row = threadIdx.x / LP, my_piece = threadIdx.x % LP;   // of a load
 
     for (int r0 = row_tile * ROWS; r0 < rows; r0 += plan.tiles * ROWS) {
         const Span sp = scalar(span_of_rows(a, seq, r0, ROWS));
@@ -449,37 +480,49 @@ __global__ __launch_bounds__(THREADS, 2) void many_kernel(PagedArgs a, PagedPlan
         const int row = r0 + wave * WR + c32;           // the lane's own
         const int t = min(row, rows - 1) / a.group, pos = pos0 + t;
         const int q_head = head * a.group + min(row, rows - 1) - t * a.group;
-        u4 q[NP][DT];
-        float c1, c2;
+        u4 q[FP][KS];
+        float size;          // the row's norm times tau 127 sqrt(D): |s| < size ks
+        float qs;            // the row's power of two; NaN: the row is not finite
         {
-            const T *p = (const T *)a.q + (seq.t0 + t) * a.q_token + q_head * a.q_head + 16 * hh;
-            float x[DT][16];
+            const T *p = (const T *)a.q + (seq.t0 + t) * a.q_token + q_head * a.q_head + 8 * hh;
+            float x[KS][8], ss = 0.f;
             uint32_t top = 0;
 #pragma unroll
-            for (int c = 0; c < DT; ++c) {
-                ld_row<16>(p + 32 * c, x[c]);
-                top = max(top, abs_max<16>(x[c]));
+            for (int k = 0; k < KS; ++k) {
+                rows::ld8(p + 16 * k, x[k]);
+                top = max(top, abs_max<8>(x[k]));
             }
-            const float2 f = whole_scale<NP>(halves_max(top));
-            c1 = a.c1 * f.y;
-            c2 = a.c2 * f.y * f.y;
+            top = halves_max(top);
+            const bool odd = top >= 0x7f800000u;
+            const int e = odd || top == 0 ? 0 : (int)(top >> 23) - 126;   // |x| < 2^e
 #pragma unroll
-            for (int c = 0; c < DT; ++c) {
+            for (int k = 0; k < KS; ++k) {
+                pr::h2 hi[4], lo[4];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    x[k][i] = __builtin_ldexpf(x[k][i], 10 - e);
+                    ss = fmaf(x[k][i], x[k][i], ss);
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    uint32_t w[NP];
-                    whole4<NP>(x[c] + 4 * i, f.x, w);
-#pragma unroll
-                    for (int n = 0; n < NP; ++n) q[n][c][i] = w[n];
+                    hi[i] = pr::cvt2(x[k][2 * i], x[k][2 * i + 1]);
+                    lo[i] = pr::cvt2(pr::rest(x[k][2 * i], hi[i][0]), pr::rest(x[k][2 * i + 1], hi[i][1]));
+                    q[0][k][i] = __builtin_bit_cast(uint32_t, hi[i]);
+                    if constexpr (FP == 2) q[1][k][i] = __builtin_bit_cast(uint32_t, lo[i]);
                 }
             }
+            qs = odd ? __builtin_nanf("") : __builtin_ldexpf(1.0f, e - 10);
+            size = odd ? 0.f : a.c1 * __builtin_ldexpf(sqrtf(halves_sum(ss)) * (130.0f * sqrtf((float)D)), e - 10);
         }
         f16v acc[DT];
-        float g = 0.f;
+        float g = 0.f, c0 = 1.f, c1 = 0.f, c2 = 0.f;   // weight c0 + x (c1 + c2 x), times 2^-e
+        int kpower = -1000, vpower = -1000, e = 0;     // the largest of the scales so far; e: see c0
 #pragma unroll
         for (int d = 0; d < DT; ++d) acc[d] = f16v{};
 
         bool bad = seq.cut;
+        // Key tiles [whole, whole_end) exist in full and every row sees all their
+        // keys; elsewhere weights are masked.
         const int shift = sp.low - sp.sink_tiles;   // from a tile's number here to its own
         const int whole = a.window < sp.end ? max(sp.sink_tiles, (last - a.window) / KT + 1 - shift) : 0;
         const int whole_end = min(end, (first + 1) / KT - shift);
@@ -488,7 +531,7 @@ __global__ __launch_bounds__(THREADS, 2) void many_kernel(PagedArgs a, PagedPlan
         // a scale (threads 0 .. 63: of a key, 64 .. 127: of a value).
         u4 kr[LN], vr[LN];
         float sr = 0.f;
-        const bool loads = KB * KP >= THREADS || threadIdx.x < KB * KP;
+        const bool loads = KB * LP >= THREADS || threadIdx.x < KB * LP;
         const auto place_of = [&](int i0, int r) { return sp.tile(min(i0 + r / KT, end - 1)) * KT + r % KT; };
         int page[LN], spage = 0;   // of the next loads' rows, a step ahead
         const auto pages_of = [&](int i0) {
@@ -516,126 +559,178 @@ __global__ __launch_bounds__(THREADS, 2) void many_kernel(PagedArgs a, PagedPlan
             const long long at = (((long long)checked(spage) * a.Hkv + head) << a.page_shift) + (n & page_mask);
             if (threadIdx.x < 2 * KB) sr = (threadIdx.x < KB ? a.k_scale : a.v_scale)[at];
         };
-        const auto store = [&](int b) {
+        const auto store = [&](u4 *k, u4 *v, int b) {
 #pragma unroll
             for (int i = 0; i < LN; ++i) {
                 const int r = my_row + LR * i;
                 if (!loads) continue;
-                keys[b][r * KP + (my_piece ^ swizzle<KP>(r))] = kr[i];
-                u4 x[2];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t w = vr[i][j / 2];
-                    const float lo = (float)(int8_t)(w >> (16 * (j % 2))), hi = (float)(int8_t)(w >> (16 * (j % 2) + 8));
-                    x[j / 4][j % 4] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+                for (int j = 0; j < 2; ++j) {
+                    const int to = r * C + ((2 * my_piece + j) ^ swizzle<C>(r));
+                    const uint2 k0 = codes4(kr[i][2 * j]), k1 = codes4(kr[i][2 * j + 1]);
+                    const uint2 v0 = codes4(vr[i][2 * j]), v1 = codes4(vr[i][2 * j + 1]);
+                    k[to] = u4{k0.x, k0.y, k1.x, k1.y};
+                    v[to] = u4{v0.x, v0.y, v1.x, v1.y};
                 }
-#pragma unroll
-                for (int j = 0; j < 2; ++j) values[b][r * VP + ((2 * my_piece + j) ^ swizzle<VP>(r))] = x[j];
             }
             if (threadIdx.x < 2 * KB) ((float *)(threadIdx.x < KB ? kscale : vscale)[b])[threadIdx.x & (KB - 1)] = sr;
         };
 
-        constexpr int STEP = KB / KT;
-        const auto compute = [&](int b, int i0) {
-            const bool all = i0 >= whole && i0 + STEP <= whole_end;
+        // The step's powers, and its values' factors.
+        const auto powers = [&](int b) {
+            const float ks = ((const float *)kscale[b])[lane], vs = ((const float *)vscale[b])[lane];
+            const int pk = wave_max(pr::exp_above(fabsf(ks))), pv = wave_max(pr::exp_above(fabsf(vs)));
+            if (pk > kpower || pv > vpower) {
+                kpower = max(kpower, pk);
+                const float most = __builtin_ldexpf(size, kpower);
+                const float w = a.c2 == 0.f ? 1.0f + most : fmaf(0.5f * most, most, 1.0f + most);
+                const int to = w < 3e38f ? pr::exp_above(w) - 14 : 114;
+                const int v = max(vpower, pv);
+                const float fg = __builtin_ldexpf(1.0f, max(e - to, -300)), f = __builtin_ldexpf(fg, max(vpower - v, -300));
+                g *= fg;
 #pragma unroll
-            for (int kb = 0; kb < KB / 32; ++kb) {
-                u4 k[DT], va[2][DT];
+                for (int d = 0; d < DT; ++d) acc[d] *= f;
+                e = to;
+                vpower = v;
+                c0 = __builtin_ldexpf(1.0f, -e);
+                c1 = a.c1 * qs * c0;
+                c2 = a.c2 * qs * (qs * c0);
+            }
+            const float f = __builtin_ldexpf(vs, -vpower);
+            if constexpr (FP == 1) ((_Float16 *)factors[wave])[lane] = (_Float16)f;
+            else ((float *)factors[wave])[lane] = f;
+        };
+        const auto scores = [&](const u4 *kt, int kb) {
+            u4 k[KS];
 #pragma unroll
-                for (int i = 0; i < DT; ++i) k[i] = keys[b][(32 * kb + c32) * KP + ((2 * i + hh) ^ swizzle<KP>(c32))];
-                i16v n = i16v{}, l = i16v{};
+            for (int i = 0; i < KS; ++i) k[i] = kt[(32 * kb + c32) * C + ((2 * i + hh) ^ swizzle<C>(c32))];
+            f16v x = f16v{};
 #pragma unroll
-                for (int i = 0; i < DT; ++i)
-                    n = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i4, k[i]), __builtin_bit_cast(i4, q[0][i]), n, 0, 0, 0);
-                n = n << 8;
+            for (int n = FP - 1; n >= 0; --n)
 #pragma unroll
-                for (int i = 0; i < DT; ++i)
-                    n = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i4, k[i]), __builtin_bit_cast(i4, q[1][i]), n, 0, 0, 0);
-                if constexpr (NP == 3) {
+                for (int i = 0; i < KS; ++i)
+                    x = pr::mma(__builtin_bit_cast(pr::h8, k[i]), __builtin_bit_cast(pr::h8, q[n][i]), x);
+            return x;
+        };
+        const auto block = [&](const f16v &x, const u4 *vt, int b, int i0, int kb, auto masked) {
+            u4 va[2][DT];
+            // the value operands: keys {4 hh .. + 3, 8 + 4 hh .. + 3} of 16, channel c32 of 32
+            const s4 *v = (const s4 *)vt;
 #pragma unroll
-                    for (int i = 0; i < DT; ++i)
-                        l = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i4, k[i]), __builtin_bit_cast(i4, q[2][i]), l, 0, 0, 0);
+            for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    typedef s4 __attribute__((address_space(3))) *lp;
+                    const int j = lane >> 2 & 3, r = 32 * kb + 16 * m + 4 * hh + j;
+                    const int c = 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+                    const int at = 2 * (r * C + (c ^ swizzle<C>(4 * hh + j))) + (lane & 1);
+                    const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(v + at));
+                    const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(v + at + 2 * 8 * C));
+                    const uint2 l = __builtin_bit_cast(uint2, lo), h = __builtin_bit_cast(uint2, hi);
+                    va[m][d] = u4{l.x, l.y, h.x, h.y};
                 }
-                // the value operands: keys {4 hh .. + 3, 8 + 4 hh .. + 3} of 16, channel c32 of 32
-                const s4 *v = (const s4 *)values[b];
+            }
+            u4 w[FP][2];
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
+            for (int i = 0; i < 4; ++i) {
+                const f4 ks = kscale[b][8 * kb + 2 * i + hh];
+                float y[4];
+                bool seen[4];
+                // key n0 + n of a tile is seen if n <= lim and (n > lim - window or it
+                // is a first token)
+                const int it = i0 + 2 * kb + i / 2, n0 = sp.tile(min(it, end - 1)) * KT + 4 * hh;
+                const int lim = it < end ? max(pos, -1) - n0 : -1, low = lim - a.window, sinks = a.sinks - n0;
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        typedef s4 __attribute__((address_space(3))) *lp;
-                        const int j = lane >> 2 & 3, r = 32 * kb + 16 * m + 4 * hh + j;
-                        const int c = 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
-                        const int at = 2 * (r * VP + (c ^ swizzle<VP>(4 * hh + j))) + (lane & 1);
-                        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(v + at));
-                        const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(v + at + 2 * 8 * VP));
-                        const uint2 x = __builtin_bit_cast(uint2, lo), y = __builtin_bit_cast(uint2, hi);
-                        va[m][d] = u4{x.x, x.y, y.x, y.y};
-                    }
-                }
-                float w[16];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f4 ks = kscale[b][8 * kb + 2 * i + hh], vs = vscale[b][8 * kb + 2 * i + hh];
-                    // key n0 + e of a tile is seen if e <= lim and (e > lim - window or it
-                    // is a first token)
-                    const int it = i0 + 2 * kb + i / 2, n0 = sp.tile(min(it, end - 1)) * KT + 4 * hh;
-                    const int lim = it < end ? max(pos, -1) - n0 : -1, low = lim - a.window, sinks = a.sinks - n0;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float x = (float)n[4 * i + j];
-                        if constexpr (NP == 3) x = fmaf(x, 256.0f, (float)l[4 * i + j]);
-                        x *= ks[j];
-                        float f = fmaf(fmaf(x, c2, c1), x, 1.0f), fv = f * vs[j];
-                        const int e = 8 * (i % 2) + j;
-                        if (!all && (e > lim || (e <= low && e >= sinks))) f = fv = 0.f;
-                        g += f;
-                        w[4 * i + j] = fv;
-                    }
-                }
-                u4 wp[NP][2];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    uint32_t p[NP];
-                    parts2<NP>(w[2 * i], w[2 * i + 1], p);
-#pragma unroll
-                    for (int x = 0; x < NP; ++x) wp[x][i / 4][i % 4] = p[x];
+                for (int j = 0; j < 4; ++j) {
+                    const float z = x[4 * i + j] * ks[j];
+                    y[j] = fmaf(fmaf(z, c2, c1), z, c0);
+                    const int n = 8 * (i % 2) + j;
+                    // (the scales of a key that is not seen may be NaN)
+                    seen[j] = !decltype(masked)::value || (n <= lim && (n > low || n < sinks));
+                    y[j] = seen[j] ? y[j] : 0.f;
                 }
 #pragma unroll
-                for (int x = NP - 1; x >= 0; --x) {
+                for (int j = 0; j < 2; ++j) {
+                    if constexpr (FP == 1) {
+                        // the sum of the rounded weights, as the numerator takes them
+                        const pr::h2 one = {(_Float16)1.0f, (_Float16)1.0f};
+                        const pr::h2 h = pr::cvt2(y[2 * j], y[2 * j + 1]);
+                        pr::h2 f = ((const pr::h2 *)factors[wave])[(32 * kb + 8 * i + 4 * hh) / 2 + j];
+                        g = __builtin_amdgcn_fdot2(h, one, g, false);
+                        f[0] = seen[2 * j] ? f[0] : (_Float16)0.0f;
+                        f[1] = seen[2 * j + 1] ? f[1] : (_Float16)0.0f;
+                        const pr::h2 o = h * f;
+                        w[0][i / 2][2 * (i % 2) + j] = __builtin_bit_cast(uint32_t, o);
+                    } else {
+                        const f4 f = factors[wave][8 * kb + 2 * i + hh];
+                        g += y[2 * j] + y[2 * j + 1];
+                        float z[2];
 #pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) acc[d] = mma(va[m][d], wp[x][m], acc[d]);
+                        for (int n = 0; n < 2; ++n) z[n] = seen[2 * j + n] ? y[2 * j + n] * f[2 * j + n] : 0.f;
+                        const pr::h2 hi = pr::cvt2(z[0], z[1]), lo = pr::cvt2(pr::rest(z[0], hi[0]), pr::rest(z[1], hi[1]));
+                        w[0][i / 2][2 * (i % 2) + j] = __builtin_bit_cast(uint32_t, hi);
+                        w[FP - 1][i / 2][2 * (i % 2) + j] = __builtin_bit_cast(uint32_t, lo);
                     }
                 }
             }
+#pragma unroll
+            for (int n = FP - 1; n >= 0; --n)
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+                        acc[d] = pr::mma(__builtin_bit_cast(pr::h8, va[m][d]), __builtin_bit_cast(pr::h8, w[n][m]), acc[d]);
         };
-
-        if (begin < end) {
-            pages_of(begin);
-            load(begin);
-            pages_of(begin + STEP);
-            store(0);
-            load(begin + STEP);
-            pages_of(begin + 2 * STEP);
-        }
-        __syncthreads();
-        for (int i0 = begin, b = 0; i0 < end; i0 += STEP, b ^= 1) {
-            compute(b, i0);
-            // the other buffer: every wave is past the step that read it
-            store(b ^ 1);
-            load(i0 + 2 * STEP);
-            pages_of(i0 + 3 * STEP);
+        // (loops of their own for whole and for masked steps: one loop for both moves the
+        // sums between registers)
+        const auto walk = [&](u4 *__restrict__ k0, u4 *__restrict__ k1, u4 *__restrict__ v0, u4 *__restrict__ v1) {
+            if (begin < end) {
+                pages_of(begin);
+                load(begin);
+                pages_of(begin + STEP);
+                store(k0, v0, 0);
+                load(begin + STEP);
+                pages_of(begin + 2 * STEP);
+            }
             __syncthreads();
-        }
+            const auto turn = [&](u4 *k, u4 *v, int b, int i0) {
+                // the other buffer: every wave is past the step that read it
+                store(k, v, b);
+                load(i0 + 2 * STEP);
+                pages_of(i0 + 3 * STEP);
+                __syncthreads();
+            };
+            const auto pairs = [&](int i0, int to, auto masked) {
+                const auto step = [&](const u4 *k, const u4 *v, int b, int i) {
+                    powers(b);
+#pragma unroll
+                    for (int kb = 0; kb < KB / 32; ++kb) block(scores(k, kb), v, b, i, kb, masked);
+                };
+                for (; i0 < to; i0 += 2 * STEP) {
+                    step(k0, v0, 0, i0);
+                    turn(k1, v1, 1, i0);
+                    if (i0 + STEP >= end) return;
+                    step(k1, v1, 1, i0 + STEP);
+                    turn(k0, v0, 0, i0 + STEP);
+                }
+            };
+            const int from = min(begin + max(whole - begin + 2 * STEP - 1, 0) / (2 * STEP) * (2 * STEP), end);
+            const int to = max(from, begin + max(whole_end - begin, 0) / (2 * STEP) * (2 * STEP));
+            pairs(begin, from, std::true_type{});
+            pairs(from, min(to, end), std::false_type{});
+            pairs(min(to, end), end, std::true_type{});
+        };
+        walk(keys0, keys1, values0, values1);
         bad = __syncthreads_or(bad);
 
         float gs = halves_sum(g);
         if (bad && (seq.cut || sees_bad_page(a, table, sp, begin, end, pos))) gs = __builtin_nanf("");
-        const float inv = 1.0f / gs;
         const size_t o = (size_t)(seq.t0 + t) * a.Hq + q_head;
         if (row < rows) {
-            if (plan.splits > 1 && hh == 0) part[(size_t)a.T * a.Hq * plan.splits * D + o * plan.splits + split] = gs;
+            const int v = vpower > -1000 ? vpower : 0;
+            const float inv = 1.0f / gs;
+            if (plan.splits > 1 && hh == 0)
+                part[(size_t)a.T * a.Hq * plan.splits * D + o * plan.splits + split] = __builtin_ldexpf(gs, e);
 #pragma unroll
             for (int n = 0; n < 4 * DT; ++n) {
                 float f[4];
@@ -643,16 +738,20 @@ __global__ __launch_bounds__(THREADS, 2) void many_kernel(PagedArgs a, PagedPlan
                 for (int j = 0; j < 4; ++j) f[j] = acc[n / 4][n % 4 * 4 + j];
                 const int ch = 32 * (n / 4) + 8 * (n % 4) + 4 * hh;
                 if (plan.splits > 1) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[j] = __builtin_ldexpf(f[j], e + v);
                     *(float4 *)(part + (o * plan.splits + split) * D + ch) = make_float4(f[0], f[1], f[2], f[3]);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) f[j] = pos < 0 ? 0.f : f[j] * inv;   // pos < 0: sees no key
+                    for (int j = 0; j < 4; ++j)
+                        f[j] = pos < 0 ? 0.f : __builtin_ldexpf(f[j] * inv, v);   // pos < 0: sees no key
                     T *out = (T *)a.out + o * D + ch;
                     if constexpr (sizeof(T) == 2) *(uint2 *)out = make_uint2(rows::pack2(f[0], f[1]), rows::pack2(f[2], f[3]));
                     else *(float4 *)out = make_float4(f[0], f[1], f[2], f[3]);
                 }
             }
         }
+        __syncthreads();   // the buffers are read: another row tile may fill them
     }
 }
 

@@ -21,7 +21,9 @@ def codes_of(x):
 def attend(q, k, v, pos, p, tau, window, sinks, dtype):
     """serve_util.attend over rows k, v (codes times scales), its bound with q's
     whole numbers (an error of 2^-16 of its largest magnitude, float32: 2^-23)
-    and the scales' products (3 roundings a score, 3 a value) added."""
+    and the scales' products (3 roundings a score, 3 a value) added.  Chunks: the
+    weight, the value's scale and their product are rounded to fp16 (2^-11 each;
+    float32: once to two fp16 parts, 2^-22), and the sum G is of the rounded ones."""
     parts = None if dtype == "f32" else 2
     ref, bound = su.attend(q, k, v, pos, p, tau, window, sinks, parts)
     n = np.arange(len(k))
@@ -34,7 +36,8 @@ def attend(q, k, v, pos, p, tau, window, sinks, dtype):
     off = off + 4 * su.U * tau * np.einsum("tgd,nd->tgn", np.abs(q), np.abs(k))
     w = 1.0 + s + (0.5 * s * s if p == 2 else 0.0)
     e = off * (1.0 + (np.abs(s) if p == 2 else 0.0))
-    e = np.where(see[:, None, :], e + 3 * su.U * np.abs(w), 0.0)
+    e = e + (3 * su.U + (2.0 ** -22 if dtype == "f32" else 3 * 2.0 ** -11)) * np.abs(w)
+    e = np.where(see[:, None, :], e, 0.0)
     G = np.abs(np.where(see[:, None, :], w, 0.0).sum(-1, keepdims=True))
     G = np.where(G > 0, G, 1.0)
     return ref, bound + np.einsum("tgn,nd->tgd", e, np.abs(v)) / G + e.sum(-1, keepdims=True) / G * np.abs(ref)
