@@ -49,7 +49,7 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
-constexpr int THREADS = 256, COLS = 128;   // columns of a workgroup
+constexpr int THREADS = 256;
 constexpr int WAIT_LOADS = 0x0f70;         // vmcnt(0), the other counters at their most
 constexpr int NO_POWER = -1000;            // of a row of zeros
 
@@ -241,20 +241,21 @@ struct Place {
 };
 __device__ __forceinline__ Place scalar(Place p) { return Place{scalar(p.t0), scalar(p.len), scalar(p.first), scalar(p.role)}; }
 
-// The columns of sequences whose tokens have `per` of them each: sequence s has the
-// places floor(starts[s] per / COLS) + s and on, enough for it and no other's.
-inline long long places(int S, int T, int per) { return (long long)T * per / COLS + S; }
+// The columns of sequences whose tokens have `per` of them each, `cols` to a place:
+// sequence s has the places floor(starts[s] per / cols) + s and on, enough for it and
+// no other's.
+inline long long places(int S, int T, int per, int cols) { return (long long)T * per / cols + S; }
 
-__device__ __forceinline__ Place place_of(const int32_t *starts, int S, int T, int per, int idx)
+__device__ __forceinline__ Place place_of(const int32_t *starts, int S, int T, int per, int cols, int idx)
 {
-    const auto at = [&](int s) { return (long long)min(max(starts[s], 0), T) * per / COLS + s; };
+    const auto at = [&](int s) { return (long long)min(max(starts[s], 0), T) * per / cols + s; };
     int lo = 0, hi = S - 1;   // the last sequence that begins at idx or before
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
         if (at(mid) <= idx) lo = mid;
         else hi = mid - 1;
     }
-    const long long first = (idx - at(lo)) * COLS;
+    const long long first = (idx - at(lo)) * cols;
     Place p = {min(max(starts[lo], 0), T), 0, 0, 0};
     const int len = min(max(starts[lo + 1], p.t0), T) - p.t0;
     if (first >= 0 && first < (long long)len * per) {
@@ -267,12 +268,12 @@ __device__ __forceinline__ Place place_of(const int32_t *starts, int S, int T, i
 // Loads tile rows r0 .. r0 + TILE - 1 of two planes (rows past `last` repeat it)
 // into LDS: the loads of a wave are every fourth.  A lane's place in a whole tile
 // does not change: scalar base, 32-bit offset.
-template <typename E, int D>
+template <typename E, int D, int TILE>
 __device__ __forceinline__ void load_tiles(const E *x, const E *y, int r0, int last, u4 *xt, u4 *yt, int wave, int lane)
 {
     using O = Ops<E, D>;
-    constexpr int C = O::C, LR = 64 / C, N = O::TILE / LR;   // rows of a load, loads of a tile
-    const bool in = r0 + O::TILE - 1 <= last;
+    constexpr int C = O::C, LR = 64 / C, N = TILE / LR;   // rows of a load, loads of a tile
+    const bool in = r0 + TILE - 1 <= last;
     const char *const xb = (const char *)(x + (size_t)r0 * D), *const yb = (const char *)(y + (size_t)r0 * D);
 #pragma unroll
     for (int i = 0; i < (2 * N + 3) / 4; ++i) {
@@ -289,21 +290,20 @@ __device__ __forceinline__ void load_tiles(const E *x, const E *y, int r0, int l
 // the next one is on its way.  The tiles of [begin2, end2), whole pairs of them, go to
 // `fast`, the ones before and after to `masked`.  Four LDS arrays, restrict: a load
 // into one buffer need not be waited for before the other is read.
-template <typename E, int D, typename F, typename M>
+template <typename E, int D, int TILE, typename F, typename M>
 __device__ __forceinline__ void walk(const E *x, const E *y, int begin, int begin2, int end2, int end, int last,
                                      u4 *__restrict__ x0, u4 *__restrict__ x1, u4 *__restrict__ y0, u4 *__restrict__ y1,
                                      int wave, int lane, F fast, M masked)
 {
-    constexpr int TILE = Ops<E, D>::TILE;
-    if (begin < end) load_tiles<E, D>(x, y, begin, last, x0, y0, wave, lane);
+    if (begin < end) load_tiles<E, D, TILE>(x, y, begin, last, x0, y0, wave, lane);
     __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
     __syncthreads();
-    if (begin + TILE < end) load_tiles<E, D>(x, y, begin + TILE, last, x1, y1, wave, lane);
+    if (begin + TILE < end) load_tiles<E, D, TILE>(x, y, begin + TILE, last, x1, y1, wave, lane);
     // the next tile is there, and this one's buffer is free
     const auto turn = [&](int r0, u4 *xt, u4 *yt) {
         __builtin_amdgcn_s_waitcnt(WAIT_LOADS);
         __syncthreads();
-        if (r0 + 2 * TILE < end) load_tiles<E, D>(x, y, r0 + 2 * TILE, last, xt, yt, wave, lane);
+        if (r0 + 2 * TILE < end) load_tiles<E, D, TILE>(x, y, r0 + 2 * TILE, last, xt, yt, wave, lane);
     };
     const auto pairs = [&](int r0, int to, auto &compute) {
         for (; r0 < to; r0 += 2 * TILE) {
@@ -318,6 +318,47 @@ __device__ __forceinline__ void walk(const E *x, const E *y, int begin, int begi
     pairs(begin, begin2, masked);
     pairs(begin2, end2, fast);
     pairs(end2, end, masked);
+}
+
+// How a workgroup's four waves share its work: WK = 1, each 32 columns of 128 and all
+// tiles; WK = 4, the same 32 columns and every fourth block of 32 rows, their sums added
+// in LDS at the end.  Calls that would leave CUs idle with 128 columns take 32: one
+// prompt of 777 tokens, 12 heads of 64: 84 workgroups, 300 of a quarter of the steps.
+template <typename E, int D, int WK> struct Cut {
+    static constexpr int COLS = WK == 1 ? 128 : 32;
+    static constexpr int TILE = WK == 1 ? Ops<E, D>::TILE : 128;
+    static constexpr int MINE = WK == 1 ? TILE : 32;    // of a tile, a wave's
+    // two buffers of two tiles fit a CU's LDS
+    static constexpr bool FITS = WK == 1 || 4 * TILE * D * (int)sizeof(E) <= 128 * 1024;
+    static_assert(TILE * D * (int)sizeof(E) >= Ops<E, D>::DT * 16 * 64 * 4 || WK == 1, "an array for a wave's sums");
+};
+
+// Adds the waves' sums (times 2^power of each) in LDS, one array per wave (a tile's: at
+// least 4 KB for 32 channels); power becomes that of the sum.  The caller has made
+// sure that the arrays are free, and puts a barrier between.
+template <int DT>
+__device__ __forceinline__ void join_put(f16v *acc, int &power, int *powers, u4 *mine, int wave, int lane)
+{
+    powers[wave] = power;
+    __syncthreads();
+    const int most = max(max(powers[0], powers[1]), max(powers[2], powers[3]));
+    const float f = __builtin_ldexpf(1.0f, max(power - most, -300));
+    power = most;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) ((float *)mine)[(16 * d + i) * 64 + lane] = acc[d][i] * f;
+}
+template <int DT>
+__device__ __forceinline__ void join_get(f16v *acc, const u4 *a, const u4 *b, const u4 *c, const u4 *e, int lane)
+{
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int j = (16 * d + i) * 64 + lane;
+            acc[d][i] = (((const float *)a)[j] + ((const float *)b)[j]) + (((const float *)c)[j] + ((const float *)e)[j]);
+        }
 }
 
 // Four neighbouring values (n of them where fewer) of a row.
@@ -367,6 +408,7 @@ template <typename E> struct Planes {
     Place *places;
     int n_places, sorted;
     int split;           // dk and dv by workgroups of their own
+    int cols;            // columns of a workgroup
 };
 // At D = 128, bf16, the sums of dk and dv leave no registers for two waves on a SIMD;
 // the scores made twice cost less (a seventh more products).
@@ -374,6 +416,8 @@ constexpr bool split_keys(int D, bool bf16) { return bf16 && D == 128; }
 // Scores of a whole tile before its weights, where registers allow it.
 template <typename E, int D> constexpr bool ahead() { return D < 128; }
 template <typename E> Planes<E> planes_at(void *ws, const PackedArgs &a, int D, int backward);
+// Whether a call takes 32 columns to a workgroup.
+bool small_call(int S, int T, int Hq, int Hkv, int D, int is_bf16, int backward);
 template <typename T, typename E>
 hipError_t prep(const PackedArgs &a, const Planes<E> &p, int D, int backward, hipStream_t st);
 

@@ -74,15 +74,17 @@ __device__ __forceinline__ void scale_down(f16v *acc, int e)
     for (int d = 0; d < DT; ++d) acc[d] *= f;
 }
 
-template <typename T, int D, int P>
+template <typename T, int D, int P, int WK>
 __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typename plane_of<T>::type> &p, int head,
-                                           const Place &pl, u4 *x0, u4 *x1, u4 *y0, u4 *y1, f4 *factors)
+                                           const Place &pl, u4 *x0, u4 *x1, u4 *y0, u4 *y1, f4 *factors, int *wave_powers)
 {
     typedef typename plane_of<T>::type E;
     using O = Ops<E, D>;
-    constexpr int DT = O::DT, TILE = O::TILE;
+    using W = Cut<E, D, WK>;
+    constexpr int DT = O::DT, TILE = W::TILE, MINE = W::MINE, COLS = W::COLS;
     const int wave = scalar(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32, c32 = lane % 32;
-    const int rows = pl.len * a.group, wfirst = pl.first + 32 * wave;
+    const int rows = pl.len * a.group, wfirst = pl.first + (WK == 1 ? 32 * wave : 0);
+    const int at = WK == 1 ? 0 : wave;   // the wave's first block of a tile
     const int row = min(wfirst + c32, rows - 1), t = row / a.group;
     const size_t base = ((size_t)head * a.T + pl.t0) * a.group, keys = (size_t)head * a.T + pl.t0;
 
@@ -101,11 +103,11 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
     const int none = a.causal ? scalar(min(wfirst + 31, rows - 1) / a.group) + 1 : pl.len;
     const int lim = a.causal ? t : pl.len - 1;
     const float tau = a.tau;
-    int next = p.b[keys + min(lane, pl.len - 1)];
+    int next = p.b[keys + min(32 * at + lane % MINE, pl.len - 1)];
 
     const auto block = [&](const f16v &s, const f16v &dp, const u4 *kt, int n1, int kb, auto masked) {
         typename O::Turned k;
-        O::turn(k, kt, kb, lane);
+        O::turn(k, kt, at + kb, lane);
         float w[16];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -124,41 +126,54 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
     const auto powers = [&](int n0) {
         if constexpr (O::POWERS) {
             const int b = next >> 1;
-            next = p.b[keys + min(n0 + TILE + lane, pl.len - 1)];
+            next = p.b[keys + min(n0 + TILE + 32 * at + lane % MINE, pl.len - 1)];
             const int most = wave_max(b);
             if (most > power) {
                 scale_down<DT>(acc, power - most);
                 power = most;
                 delta = __builtin_ldexpf(info.delta, -power);
             }
-            ((float *)factors)[lane] = __builtin_ldexpf(1.0f, b - power);
+            ((float *)factors)[lane % MINE] = __builtin_ldexpf(1.0f, b - power);
         }
     };
-    walk<E, D>(p.kh + keys * D, p.vh + keys * D, 0, 0, whole, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
-               [&](const u4 *kt, const u4 *vt, int n0) {
+    const auto scores = [&](const u4 *kt, const u4 *vt, int kb, f16v &s, f16v &dp) {
+        s = O::scores(kt, at + kb, hh, c32, q);
+        dp = O::scores(vt, at + kb, hh, c32, o);
+    };
+    walk<E, D, TILE>(p.kh + keys * D, p.vh + keys * D, 0, 0, whole, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
+                     [&](const u4 *kt, const u4 *vt, int n0) {
         powers(n0);
         if constexpr (ahead<E, D>()) {
-            f16v s[TILE / 32], dp[TILE / 32];
+            f16v s[MINE / 32], dp[MINE / 32];
 #pragma unroll
-            for (int kb = 0; kb < TILE / 32; ++kb) {
-                s[kb] = O::scores(kt, kb, hh, c32, q);
-                dp[kb] = O::scores(vt, kb, hh, c32, o);
-            }
+            for (int kb = 0; kb < MINE / 32; ++kb) scores(kt, vt, kb, s[kb], dp[kb]);
 #pragma unroll
-            for (int kb = 0; kb < TILE / 32; ++kb) block(s[kb], dp[kb], kt, n0 + 32 * kb, kb, std::false_type{});
+            for (int kb = 0; kb < MINE / 32; ++kb) block(s[kb], dp[kb], kt, n0 + 32 * (at + kb), kb, std::false_type{});
         } else {
 #pragma unroll
-            for (int kb = 0; kb < TILE / 32; ++kb)
-                block(O::scores(kt, kb, hh, c32, q), O::scores(vt, kb, hh, c32, o), kt, n0 + 32 * kb, kb, std::false_type{});
+            for (int kb = 0; kb < MINE / 32; ++kb) {
+                f16v s, dp;
+                scores(kt, vt, kb, s, dp);
+                block(s, dp, kt, n0 + 32 * (at + kb), kb, std::false_type{});
+            }
         }
     },
-               [&](const u4 *kt, const u4 *vt, int n0) {
+                     [&](const u4 *kt, const u4 *vt, int n0) {
         powers(n0);
 #pragma unroll
-        for (int kb = 0; kb < TILE / 32; ++kb)
-            if (n0 + 32 * kb < none)
-                block(O::scores(kt, kb, hh, c32, q), O::scores(vt, kb, hh, c32, o), kt, n0 + 32 * kb, kb, std::true_type{});
+        for (int kb = 0; kb < MINE / 32; ++kb) {
+            if (n0 + 32 * (at + kb) >= none) break;
+            f16v s, dp;
+            scores(kt, vt, kb, s, dp);
+            block(s, dp, kt, n0 + 32 * (at + kb), kb, std::true_type{});
+        }
     });
+    if constexpr (WK > 1) {
+        join_put<DT>(acc, power, wave_powers, wave == 0 ? x0 : wave == 1 ? x1 : wave == 2 ? y0 : y1, wave, lane);
+        __syncthreads();
+        if (wave) return;
+        join_get<DT>(acc, x0, x1, y0, y1, lane);
+    }
 
     if (O::POWERS) scale_up<DT>(acc, tau * info.m, info.e + (power > NO_POWER ? power : 0));
     else scale_up<DT>(acc, tau * info.m, 0);
@@ -167,16 +182,18 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
     store_row<T, D>((T *)a.dq + (pl.t0 + t) * a.dqs.token + (head * a.group + row - t * a.group) * a.dqs.head, acc, hh);
 }
 
-template <typename T, int D, int P, int ROLE>
+template <typename T, int D, int P, int ROLE, int WK>
 __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typename plane_of<T>::type> &p, int head,
-                                           const Place &pl, u4 *x0, u4 *x1, u4 *y0, u4 *y1, f4 *factors)
+                                           const Place &pl, u4 *x0, u4 *x1, u4 *y0, u4 *y1, f4 *factors, int *wave_powers)
 {
     typedef typename plane_of<T>::type E;
     using O = Ops<E, D>;
-    constexpr int DT = O::DT, TILE = O::TILE;
+    using W = Cut<E, D, WK>;
+    constexpr int DT = O::DT, TILE = W::TILE, MINE = W::MINE, COLS = W::COLS;
     constexpr bool GK = ROLE != DV, GV = ROLE != DK;
     const int wave = scalar(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32, c32 = lane % 32;
-    const int rows = pl.len * a.group, wfirst = pl.first + 32 * wave;
+    const int rows = pl.len * a.group, wfirst = pl.first + (WK == 1 ? 32 * wave : 0);
+    const int at = WK == 1 ? 0 : wave;   // the wave's first block of a tile
     const int n = min(wfirst + c32, pl.len - 1);
     const size_t base = ((size_t)head * a.T + pl.t0) * a.group, keys = (size_t)head * a.T + pl.t0;
 
@@ -202,7 +219,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
     const int whole_end = max(whole, begin + (rows - begin) / (2 * TILE) * (2 * TILE));
     const int least = a.causal ? n * a.group : 0;
     const float tau = a.tau;
-    RowInfo next = p.info[base + min(begin + lane % TILE, rows - 1)];
+    RowInfo next = p.info[base + min(begin + 32 * at + lane % MINE, rows - 1)];
     uint64_t odd = 0;
 
     const auto block = [&](const f16v &s, const f16v &dp, const u4 *qt, const u4 *ot, int r1, int kb, auto masked) {
@@ -228,18 +245,18 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
         }
         typename O::Turned xt;
         if constexpr (GK) {
-            O::turn(xt, qt, kb, lane);
+            O::turn(xt, qt, at + kb, lane);
             O::add(dk, xt, x);
         }
         if constexpr (GV) {
-            O::turn(xt, ot, kb, lane);
+            O::turn(xt, ot, at + kb, lane);
             O::add(dv, xt, w);
         }
     };
     const auto powers = [&](int r0) {
         const RowInfo info = next;
         odd |= __ballot(info.ed & 1);
-        next = p.info[base + min(r0 + TILE + lane % TILE, rows - 1)];
+        next = p.info[base + min(r0 + TILE + 32 * at + lane % MINE, rows - 1)];
         float X = info.m, Y = info.m * info.delta;
         if constexpr (O::POWERS) {
             const int e = wave_max(info.e), d = wave_max(info.ed >> 1);
@@ -254,50 +271,69 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
             X = __builtin_ldexpf(info.m, info.e - M);
             Y = X * __builtin_ldexpf(info.delta, -F);
         }
-        if (O::TILE == 64 || lane < 32) {
+        if (MINE == 64 || lane < 32) {
             ((float *)factors)[lane] = X;
             ((float *)(factors + 16))[lane] = Y;
         }
     };
-    const auto scores = [&](const u4 *ot, int kb) {
-        if constexpr (GK) return O::scores(ot, kb, hh, c32, v);
-        else return f16v{};
+    const auto scores = [&](const u4 *qt, const u4 *ot, int kb, f16v &s, f16v &dp) {
+        s = O::scores(qt, at + kb, hh, c32, k);
+        if constexpr (GK) dp = O::scores(ot, at + kb, hh, c32, v);
     };
-    walk<E, D>(p.qh + base * D, p.oh + base * D, begin, min(whole, rows), min(whole_end, rows), rows, rows - 1, x0, x1, y0, y1, wave, lane,
-               [&](const u4 *qt, const u4 *ot, int r0) {
+    walk<E, D, TILE>(p.qh + base * D, p.oh + base * D, begin, min(whole, rows), min(whole_end, rows), rows, rows - 1, x0, x1,
+                     y0, y1, wave, lane,
+                     [&](const u4 *qt, const u4 *ot, int r0) {
         powers(r0);
         if constexpr (ROLE == DV || (ROLE == DK && ahead<E, D>())) {
-            f16v s[TILE / 32], dp[TILE / 32];
+            f16v s[MINE / 32], dp[MINE / 32];
 #pragma unroll
-            for (int kb = 0; kb < TILE / 32; ++kb) {
-                s[kb] = O::scores(qt, kb, hh, c32, k);
-                dp[kb] = scores(ot, kb);
-            }
+            for (int kb = 0; kb < MINE / 32; ++kb) scores(qt, ot, kb, s[kb], dp[kb]);
 #pragma unroll
-            for (int kb = 0; kb < TILE / 32; ++kb) block(s[kb], dp[kb], qt, ot, r0 + 32 * kb, kb, std::false_type{});
+            for (int kb = 0; kb < MINE / 32; ++kb) block(s[kb], dp[kb], qt, ot, r0 + 32 * (at + kb), kb, std::false_type{});
         } else {
 #pragma unroll
-            for (int kb = 0; kb < TILE / 32; ++kb)
-                block(O::scores(qt, kb, hh, c32, k), scores(ot, kb), qt, ot, r0 + 32 * kb, kb, std::false_type{});
+            for (int kb = 0; kb < MINE / 32; ++kb) {
+                f16v s, dp;
+                scores(qt, ot, kb, s, dp);
+                block(s, dp, qt, ot, r0 + 32 * (at + kb), kb, std::false_type{});
+            }
         }
     },
-               [&](const u4 *qt, const u4 *ot, int r0) {
+                     [&](const u4 *qt, const u4 *ot, int r0) {
         powers(r0);
 #pragma unroll
-        for (int kb = 0; kb < TILE / 32; ++kb)
-            if (r0 + 32 * kb + 31 >= some && r0 + 32 * kb < rows)
-                block(O::scores(qt, kb, hh, c32, k), scores(ot, kb), qt, ot, r0 + 32 * kb, kb, std::true_type{});
+        for (int kb = 0; kb < MINE / 32; ++kb) {
+            const int r1 = r0 + 32 * (at + kb);
+            if (r1 + 31 < some || r1 >= rows) continue;
+            f16v s, dp;
+            scores(qt, ot, kb, s, dp);
+            block(s, dp, qt, ot, r1, kb, std::true_type{});
+        }
     });
-
+    // powers of the sums; a wave without a block of its own has none
+    int ek = !O::POWERS ? 0 : M > NO_POWER ? M + (F > NO_POWER ? F : 0) : NO_POWER, ev = O::POWERS ? M : 0;
+    if constexpr (WK > 1) {
+        u4 *const mine = wave == 0 ? x0 : wave == 1 ? x1 : wave == 2 ? y0 : y1;
+        join_put<DT>(dk, ek, wave_powers, mine, wave, lane);
+        odd = __syncthreads_or(odd != 0);
+        if (wave == 0) join_get<DT>(dk, x0, x1, y0, y1, lane);
+        __syncthreads();
+        join_put<DT>(dv, ev, wave_powers, mine, wave, lane);
+        __syncthreads();
+        if (wave > 1) return;
+        if (wave == 1) join_get<DT>(dv, x0, x1, y0, y1, lane);
+    }
+    ek = ek > NO_POWER ? ek : 0;
+    ev = ev > NO_POWER ? ev : 0;
     const size_t tok = pl.t0 + n;
     const bool mine = wfirst + c32 < pl.len;
-    if constexpr (GK) {
-        scale_up<DT>(dk, a.tau, O::POWERS && M > NO_POWER ? M + (F > NO_POWER ? F : 0) : 0);
+    if (GK && (WK == 1 || wave == 0)) {
+        scale_up<DT>(dk, a.tau, ek);
         standardise_back<E, D>(p.kh + (keys + n) * D, p.rk[keys + n], dk, hh);
         if (mine) store_row<T, D>((T *)a.dk + tok * a.dks.token + head * a.dks.head, dk, hh);
     }
-    if constexpr (GV) {
-        scale_up<DT>(dv, P == 2 ? 0.5f : 1.0f, O::POWERS && M > NO_POWER ? M : 0);
+    if (GV && (WK == 1 || wave == 1)) {
+        scale_up<DT>(dv, P == 2 ? 0.5f : 1.0f, ev);
         if (odd)
             add_odd<T, D>(dv, begin / 64 * 64, rows, lane, [&](int r) { return p.info[base + r].ed & 1; },
                           [&](int r) {
@@ -309,23 +345,26 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
     }
 }
 
-template <typename T, int D, int P>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void bwd_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p)
+template <typename T, int D, int P, int WK>
+__global__ __launch_bounds__(THREADS, WK > 1 || (sizeof(T) == 4 && D == 128) ? 1 : 2) void bwd_kernel(
+    PackedArgs a, Planes<typename plane_of<T>::type> p)
 {
-    using O = Ops<typename plane_of<T>::type, D>;
-    __shared__ u4 x0[O::TILE * O::C], x1[O::TILE * O::C], y0[O::TILE * O::C], y1[O::TILE * O::C];
+    typedef typename plane_of<T>::type E;
+    constexpr int N = Cut<E, D, WK>::TILE * Ops<E, D>::C;
+    __shared__ u4 x0[N], x1[N], y0[N], y1[N];
     __shared__ f4 factors[THREADS / 64][32];
+    __shared__ int wave_powers[THREADS / 64];
     f4 *const mine = factors[scalar(threadIdx.x / 64)];
     const int head = blockIdx.x % a.Hkv;
     const Place pl = scalar(p.places[blockIdx.x / a.Hkv]);
     if (pl.len == 0) return;
     if (pl.role == ROWS) {
-        rows_block<T, D, P>(a, p, head, pl, x0, x1, y0, y1, mine);
-    } else if constexpr (split_keys(D, sizeof(T) == 2)) {
-        if (pl.role == DK) keys_block<T, D, P, DK>(a, p, head, pl, x0, x1, y0, y1, mine);
-        else keys_block<T, D, P, DV>(a, p, head, pl, x0, x1, y0, y1, mine);
+        rows_block<T, D, P, WK>(a, p, head, pl, x0, x1, y0, y1, mine, wave_powers);
+    } else if constexpr (WK == 1 && split_keys(D, sizeof(T) == 2)) {
+        if (pl.role == DK) keys_block<T, D, P, DK, WK>(a, p, head, pl, x0, x1, y0, y1, mine, wave_powers);
+        else keys_block<T, D, P, DV, WK>(a, p, head, pl, x0, x1, y0, y1, mine, wave_powers);
     } else {
-        keys_block<T, D, P, KEYS>(a, p, head, pl, x0, x1, y0, y1, mine);
+        keys_block<T, D, P, KEYS, WK>(a, p, head, pl, x0, x1, y0, y1, mine, wave_powers);
     }
 }
 
@@ -337,8 +376,15 @@ template <typename T, int D> static hipError_t launch_bwd(const PackedArgs &a, v
     if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
     const hipError_t e = prep<T, E>(a, p, D, 1, st);
     if (e != hipSuccess) return e;
-    if (a.p == 2) bwd_kernel<T, D, 2><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
-    else bwd_kernel<T, D, 1><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
+    if constexpr (Cut<E, D, 4>::FITS && D < 128) {
+        if (p.cols == 32) {
+            if (a.p == 2) bwd_kernel<T, D, 2, 4><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
+            else bwd_kernel<T, D, 1, 4><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
+            return hipGetLastError();
+        }
+    }
+    if (a.p == 2) bwd_kernel<T, D, 2, 1><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
+    else bwd_kernel<T, D, 1, 1><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
     return hipGetLastError();
 }
 

@@ -23,14 +23,14 @@ namespace packed {
 // to every workgroup's turn.
 constexpr int SORTED = 4096, BINS = 512;
 
-template <bool BWD> __device__ __forceinline__ void plan(const PackedArgs &a, Place *out, int n, int sorted, int split)
+template <bool BWD> __device__ __forceinline__ void plan(const PackedArgs &a, Place *out, int n, int sorted, int split, int COLS)
 {
     // places of rows; then (backward) of keys, once or for dk and for dv
     const int rows = (int)((long long)a.T * a.group / COLS + a.S), keys = (int)((long long)a.T / COLS + a.S);
     // its place, and its work: tiles of the other side times the products of a tile
     const auto get = [&](int i, int &work) {
         const int role = i < rows ? ROWS : !split ? KEYS : i < rows + keys ? DK : DV;
-        Place p = place_of(a.starts, a.S, a.T, role == ROWS ? a.group : 1, role == ROWS ? i : (i - rows) % keys);
+        Place p = place_of(a.starts, a.S, a.T, role == ROWS ? a.group : 1, COLS, role == ROWS ? i : (i - rows) % keys);
         p.role = role;
         const long long other = role != ROWS ? ((long long)p.len - (a.causal ? p.first : 0)) * a.group
                                 : a.causal ? min((p.first + COLS - 1) / a.group + 1, p.len) : p.len;
@@ -83,7 +83,7 @@ __global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<type
                                                        unsigned plan_blocks, unsigned kv_blocks)
 {
     if (blockIdx.x < plan_blocks) {
-        plan<BWD>(a, p.places, p.n_places, p.sorted, p.split);
+        plan<BWD>(a, p.places, p.n_places, p.sorted, p.split, p.cols);
         return;
     }
     const unsigned block = blockIdx.x - plan_blocks;
@@ -187,6 +187,20 @@ __global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<type
 
 static size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
+// 32 columns where 128 leave CUs idle (places of rows, backward of keys, times key
+// heads; forward and backward in us with 32 and with 128): 12 heads of 64, 84 places
+// 19 against 22 and 30 against 35, 204 26 against 33 and the same, 372 the same and 73
+// against 58; 4 heads of 32, 260 53 against 86 and 140 against 166; one key head of 64
+// for 8, 65 places of keys 626 against 1402; float32 4 heads of 32, 124 40 against 84
+// and 80 against 161, 12 of 64, 432 310 against 355 and 912 against 855.  At D = 128 the
+// tiles fill a CU's LDS: 8 heads for 32, 104 26 against 21; 12 for 12, 84 28 against 29.
+bool small_call(int S, int T, int Hq, int Hkv, int D, int is_bf16, int backward)
+{
+    if (D == 128 && (backward || !is_bf16)) return false;   // LDS, registers
+    if (backward) return places(S, T, 1, 128) * Hkv < 320;
+    return places(S, T, Hq / Hkv, 128) * Hkv < (D == 128 ? 96 : 448);
+}
+
 // The planes from ws on (ws null: how many bytes).
 template <typename E> static Planes<E> lay_out(char *ws, int S, int T, int Hq, int Hkv, int D, int backward, size_t *bytes)
 {
@@ -198,8 +212,9 @@ template <typename E> static Planes<E> lay_out(char *ws, int S, int T, int Hq, i
     };
     const size_t keys = (size_t)Hkv * T, rows = (size_t)Hq * T;
     Planes<E> p = {};
-    p.split = split_keys(D, sizeof(E) == 2);
-    p.n_places = (int)(places(S, T, Hq / Hkv) + (backward ? (p.split ? 2 : 1) * places(S, T, 1) : 0));
+    p.cols = small_call(S, T, Hq, Hkv, D, sizeof(E) == 2, backward) ? 32 : 128;
+    p.split = p.cols == 128 && split_keys(D, sizeof(E) == 2);
+    p.n_places = (int)(places(S, T, Hq / Hkv, p.cols) + (backward ? (p.split ? 2 : 1) * places(S, T, 1, p.cols) : 0));
     p.sorted = p.n_places <= SORTED;
     p.kh = (E *)take(keys * D * sizeof(E));
     p.vh = (E *)take(keys * D * sizeof(E));
@@ -248,21 +263,25 @@ hipError_t prep(const PackedArgs &a, const Planes<E> &p, int D, int backward, hi
 template hipError_t prep<float, float>(const PackedArgs &, const Planes<float> &, int, int, hipStream_t);
 template hipError_t prep<bf16_t, _Float16>(const PackedArgs &, const Planes<_Float16> &, int, int, hipStream_t);
 
-template <typename T, int D, int P>
-__global__ __launch_bounds__(THREADS, 2) void fwd_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p)
+template <typename T, int D, int P, int WK>
+__global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArgs a, Planes<typename plane_of<T>::type> p)
 {
     typedef typename plane_of<T>::type E;
     using O = Ops<E, D>;
-    constexpr int DT = O::DT, TILE = O::TILE;
+    using W = Cut<E, D, WK>;
+    constexpr int DT = O::DT, TILE = W::TILE, MINE = W::MINE, COLS = W::COLS;
     __shared__ u4 x0[TILE * O::C], x1[TILE * O::C], y0[TILE * O::C], y1[TILE * O::C];
-    __shared__ h4 factors[THREADS / 64][TILE / 4];
+    __shared__ h4 factors[THREADS / 64][MINE / 4];
+    __shared__ int wave_powers[THREADS / 64];
+    __shared__ float wave_sums[THREADS / 64][64];
 
     // a key head's workgroups are Hkv apart, on one XCD where 8 divides Hkv
     const int head = blockIdx.x % a.Hkv;
     const Place pl = scalar(p.places[blockIdx.x / a.Hkv]);
     if (pl.len == 0) return;
     const int wave = scalar(threadIdx.x / 64), lane = threadIdx.x % 64, hh = lane / 32, c32 = lane % 32;
-    const int rows = pl.len * a.group, wfirst = pl.first + 32 * wave;
+    const int rows = pl.len * a.group, wfirst = pl.first + (WK == 1 ? 32 * wave : 0);
+    const int at = WK == 1 ? 0 : wave;   // the wave's first block of a tile
     const int row = wfirst + c32, t = min(row, rows - 1) / a.group;
     const int qhead = head * a.group + min(row, rows - 1) - t * a.group;
     const size_t io = (size_t)(pl.t0 + t) * a.Hq + qhead;
@@ -303,14 +322,14 @@ __global__ __launch_bounds__(THREADS, 2) void fwd_kernel(PackedArgs a, Planes<ty
     const int lim = a.causal ? t : pl.len - 1;
     const size_t keys = (size_t)head * a.T + pl.t0;
     const float tau = a.tau;
-    int next = p.b[keys + min(lane, pl.len - 1)];   // the next tile's powers and marks, a key to a lane
+    int next = p.b[keys + min(32 * at + lane % MINE, pl.len - 1)];   // the next tile's powers and marks, a key to a lane
     uint64_t odd = 0;
 
     // what becomes of the scores of a block of 32 keys; masked: some row does not see
     // some of them
     const auto block = [&](const f16v &s, const u4 *vt, int n1, int kb, auto masked) {
         typename O::Turned v;
-        O::turn(v, vt, kb, lane);
+        O::turn(v, vt, at + kb, lane);
         float w[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -342,7 +361,7 @@ __global__ __launch_bounds__(THREADS, 2) void fwd_kernel(PackedArgs a, Planes<ty
     const auto powers = [&](int n0) {
         const int b = next >> 1;
         odd |= __ballot(next & 1);
-        next = p.b[keys + min(n0 + TILE + lane % TILE, pl.len - 1)];
+        next = p.b[keys + min(n0 + TILE + 32 * at + lane % MINE, pl.len - 1)];
         if constexpr (O::POWERS) {
             const int most = wave_max(b);
             if (most > power) {
@@ -351,24 +370,34 @@ __global__ __launch_bounds__(THREADS, 2) void fwd_kernel(PackedArgs a, Planes<ty
                 for (int d = 0; d < DT; ++d) acc[d] *= f;
                 power = most;
             }
-            ((_Float16 *)factors[wave])[lane] = (_Float16)__builtin_ldexpf(1.0f, b - power);
+            ((_Float16 *)factors[wave])[lane % MINE] = (_Float16)__builtin_ldexpf(1.0f, b - power);
         }
     };
-    walk<E, D>(p.kh + keys * D, p.vh + keys * D, 0, 0, whole, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
-               [&](const u4 *kt, const u4 *vt, int n0) {
+    walk<E, D, TILE>(p.kh + keys * D, p.vh + keys * D, 0, 0, whole, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
+                     [&](const u4 *kt, const u4 *vt, int n0) {
         powers(n0);
-        f16v s[TILE / 32];
+        f16v s[MINE / 32];
 #pragma unroll
-        for (int kb = 0; kb < TILE / 32; ++kb) s[kb] = O::scores(kt, kb, hh, c32, own);
+        for (int kb = 0; kb < MINE / 32; ++kb) s[kb] = O::scores(kt, at + kb, hh, c32, own);
 #pragma unroll
-        for (int kb = 0; kb < TILE / 32; ++kb) block(s[kb], vt, n0 + 32 * kb, kb, std::false_type{});
+        for (int kb = 0; kb < MINE / 32; ++kb) block(s[kb], vt, n0 + 32 * (at + kb), kb, std::false_type{});
     },
-               [&](const u4 *kt, const u4 *vt, int n0) {
+                     [&](const u4 *kt, const u4 *vt, int n0) {
         powers(n0);
 #pragma unroll
-        for (int kb = 0; kb < TILE / 32; ++kb)
-            if (n0 + 32 * kb < none) block(O::scores(kt, kb, hh, c32, own), vt, n0 + 32 * kb, kb, std::true_type{});
+        for (int kb = 0; kb < MINE / 32; ++kb)
+            if (n0 + 32 * (at + kb) < none)
+                block(O::scores(kt, at + kb, hh, c32, own), vt, n0 + 32 * (at + kb), kb, std::true_type{});
     });
+    if constexpr (WK > 1) {
+        u4 *const mine = wave == 0 ? x0 : wave == 1 ? x1 : wave == 2 ? y0 : y1;   // free: the last tile is behind a barrier
+        wave_sums[wave][lane] = g;
+        join_put<DT>(acc, power, wave_powers, mine, wave, lane);
+        odd = __syncthreads_or(odd != 0);
+        if (wave) return;
+        join_get<DT>(acc, x0, x1, y0, y1, lane);
+        g = (wave_sums[0][lane] + wave_sums[1][lane]) + (wave_sums[2][lane] + wave_sums[3][lane]);
+    }
 
     const float G = pr::half_sum(g);
     // out of the power in two factors: each a normal number
@@ -395,8 +424,15 @@ template <typename T, int D> hipError_t launch(const PackedArgs &a, void *ws, hi
     if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
     const hipError_t e = prep<T, E>(a, p, D, 0, st);
     if (e != hipSuccess) return e;
-    if (a.p == 2) fwd_kernel<T, D, 2><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
-    else fwd_kernel<T, D, 1><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
+    if constexpr (Cut<E, D, 4>::FITS) {
+        if (p.cols == 32) {
+            if (a.p == 2) fwd_kernel<T, D, 2, 4><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
+            else fwd_kernel<T, D, 1, 4><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
+            return hipGetLastError();
+        }
+    }
+    if (a.p == 2) fwd_kernel<T, D, 2, 1><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
+    else fwd_kernel<T, D, 1, 1><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
     return hipGetLastError();
 }
 

@@ -94,6 +94,20 @@ def test_backward(D, dtype, Hq, Hkv):
     backward(x, label, tau=D ** -0.5)
 
 
+@pytest.mark.parametrize("D", [16, 32, 64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_calls_that_fill_the_gpu(D, dtype):
+    """Many heads: workgroups of 128 rows or keys instead of 32."""
+    label = f"packed, many heads, D={D} {dtype}"
+    say(label)
+    x = Packed([33, 0, 128, 300, 1, 129, 400], 64, 32, D, dtype, seed=D, before=2, after=3)
+    forward(x, label)
+    backward(x, label)
+    y = Packed([200, 1, 130, 64], 64, 64, D, dtype, seed=D)
+    forward(y, label, causal=False)
+    backward(y, label, causal=False)
+
+
 def test_long_sequences():
     for dtype in ("bf16", "f32"):
         x = Packed([1100, 700], 4, 2, 64, dtype, seed=1)
