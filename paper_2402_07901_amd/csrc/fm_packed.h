@@ -287,8 +287,8 @@ __device__ __forceinline__ void load_tiles(const E *x, const E *y, int r0, int l
 }
 
 // Walks over the tiles of rows [begin, end) of two planes: tile r0 is worked on while
-// the next one is on its way.  The tiles of [begin2, end2), whole pairs of them, go to
-// `fast`, the ones before and after to `masked`.  Four LDS arrays, restrict: a load
+// the next one is on its way.  The tiles of [begin2, end2) go to `fast`, the ones before
+// and after to `masked`; begin2 and end2 are whole pairs of tiles from begin, or the end.  Four LDS arrays, restrict: a load
 // into one buffer need not be waited for before the other is read.
 template <typename E, int D, int TILE, typename F, typename M>
 __device__ __forceinline__ void walk(const E *x, const E *y, int begin, int begin2, int end2, int end, int last,

@@ -109,6 +109,7 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
         typename O::Turned k;
         O::turn(k, kt, at + kb, lane);
         float w[16];
+        const int left = lim - n1 - 4 * hh;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             f4 f;
@@ -117,7 +118,7 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
             for (int i = 0; i < 4; ++i) {
                 const float d = O::POWERS ? fmaf(dp[4 * j + i], f[i], -delta) : dp[4 * j + i] - delta;
                 float x = P == 2 ? fmaf(s[4 * j + i], tau, 1.0f) * d : d;
-                if constexpr (decltype(masked)::value) x = n1 + 8 * j + 4 * hh + i <= lim ? x : 0.f;
+                if constexpr (decltype(masked)::value) x = 8 * j + i <= left ? x : 0.f;
                 w[4 * j + i] = x;
             }
         }
@@ -199,24 +200,30 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
 
     typename O::Own k, v;
     O::own(k, p.kh + (keys + n) * D, hh);
-    if constexpr (GK) O::own(v, p.vh + (keys + n) * D, hh);
     f16v dk[DT], dv[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) dk[d] = dv[d] = f16v{};
     int b = 0, M = NO_POWER, F = 0;   // the column's power; the largest so far
-    float f = 1.0f;                   // 2^(b - F)
+    // the column's values in the power F
+    const auto own_values = [&] {
+        if constexpr (GK) O::own(v, p.vh + (keys + n) * D, hh);
+        if constexpr (GK && O::POWERS) {
+            const _Float16 f = pr::half2i(b - F);
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) v.x[i] = __builtin_bit_cast(u4, __builtin_bit_cast(h8, v.x[i]) * f);
+        }
+    };
     if constexpr (O::POWERS) {
         b = p.b[keys + n] >> 1;
         F = wave_max(b);
-        f = __builtin_ldexpf(1.0f, b - F);
     }
+    own_values();
 
     // rows of tokens from the workgroup's (the wave's) first key on see it; all keys
     // are seen by rows of the last key's token and later
     const int begin = a.causal ? pl.first * a.group / TILE * TILE : 0;
     const int some = a.causal ? min(wfirst, pl.len - 1) * a.group : 0;
     const int whole = begin + (a.causal ? (min(pl.first + COLS - 1, pl.len - 1) * a.group - begin + 2 * TILE - 1) / (2 * TILE) * (2 * TILE) : 0);
-    const int whole_end = max(whole, begin + (rows - begin) / (2 * TILE) * (2 * TILE));
     const int least = a.causal ? n * a.group : 0;
     const float tau = a.tau;
     RowInfo next = p.info[base + min(begin + 32 * at + lane % MINE, rows - 1)];
@@ -224,6 +231,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
 
     const auto block = [&](const f16v &s, const f16v &dp, const u4 *qt, const u4 *ot, int r1, int kb, auto masked) {
         float w[16], x[16];
+        const int lim = least - r1 - 4 * hh;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const f4 fx = factors[8 * kb + 2 * j + hh], fy = factors[16 + 8 * kb + 2 * j + hh];
@@ -231,11 +239,10 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
             for (int i = 0; i < 4; ++i) {
                 // f_1, and f_2'; 2 f_2 = t^2 + 1
                 const float t = fmaf(s[4 * j + i], tau, 1.0f);
-                const float d = GK ? fmaf(O::POWERS ? dp[4 * j + i] * f : dp[4 * j + i], fx[i], -fy[i]) : 0.f;
+                const float d = GK ? fmaf(dp[4 * j + i], fx[i], -fy[i]) : 0.f;
                 float wi = P == 2 ? fmaf(t, t, 1.0f) * fx[i] : t * fx[i], xi = P == 2 ? t * d : d;
                 if constexpr (decltype(masked)::value) {
-                    const int r = r1 + 8 * j + 4 * hh + i;
-                    const bool see = r >= least && r < rows;
+                    const bool see = 8 * j + i >= lim;
                     wi = see ? wi : 0.f;
                     xi = see ? xi : 0.f;
                 }
@@ -265,12 +272,16 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
                 scale_down<DT>(dv, M - m);
                 scale_down<DT>(dk, M - m + F - g);
                 M = m;
-                F = g;
-                f = __builtin_ldexpf(1.0f, b - F);
+                if (g > F) {
+                    F = g;
+                    own_values();
+                }
             }
             X = __builtin_ldexpf(info.m, info.e - M);
             Y = X * __builtin_ldexpf(info.delta, -F);
         }
+        // rows past the last weigh nothing
+        if (r0 + 32 * at + lane % MINE >= rows) X = Y = 0.f;
         if (MINE == 64 || lane < 32) {
             ((float *)factors)[lane] = X;
             ((float *)(factors + 16))[lane] = Y;
@@ -280,7 +291,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
         s = O::scores(qt, at + kb, hh, c32, k);
         if constexpr (GK) dp = O::scores(ot, at + kb, hh, c32, v);
     };
-    walk<E, D, TILE>(p.qh + base * D, p.oh + base * D, begin, min(whole, rows), min(whole_end, rows), rows, rows - 1, x0, x1,
+    walk<E, D, TILE>(p.qh + base * D, p.oh + base * D, begin, min(whole, rows), rows, rows, rows - 1, x0, x1,
                      y0, y1, wave, lane,
                      [&](const u4 *qt, const u4 *ot, int r0) {
         powers(r0);

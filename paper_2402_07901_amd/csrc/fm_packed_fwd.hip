@@ -331,11 +331,12 @@ __global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArg
         typename O::Turned v;
         O::turn(v, vt, at + kb, lane);
         float w[16];
+        const int left = lim - n1 - 4 * hh;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             w[i] = fmaf(s[i], tau, 1.0f);
             if constexpr (P == 2) w[i] = fmaf(w[i], w[i], 1.0f);
-            if constexpr (decltype(masked)::value) w[i] = n1 + 8 * (i / 4) + 4 * hh + i % 4 <= lim ? w[i] : 0.f;
+            if constexpr (decltype(masked)::value) w[i] = 8 * (i / 4) + i % 4 <= left ? w[i] : 0.f;
         }
         if constexpr (O::POWERS) {
             // the sum of the rounded weights, as the numerator takes them
