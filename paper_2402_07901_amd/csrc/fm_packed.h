@@ -112,6 +112,24 @@ template <int D> struct Ops<_Float16, D> {
             s = pr::mma(__builtin_bit_cast(h8, x[i]), __builtin_bit_cast(h8, o.x[i]), s);
         return s;
     }
+    // Two blocks' scores, product after product in turn (a chain of products into one
+    // sum waits for each).
+    static __device__ __forceinline__ void scores2(const u4 *t0, int kb0, const Own &o0, f16v &s0, const u4 *t1, int kb1,
+                                                   const Own &o1, f16v &s1, int hh, int c32)
+    {
+        u4 x0[KS], x1[KS];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            x0[i] = t0[(32 * kb0 + c32) * C + ((2 * i + hh) ^ swizzle<C>(c32))];
+            x1[i] = t1[(32 * kb1 + c32) * C + ((2 * i + hh) ^ swizzle<C>(c32))];
+        }
+        s0 = s1 = f16v{};
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            s0 = pr::mma(__builtin_bit_cast(h8, x0[i]), __builtin_bit_cast(h8, o0.x[i]), s0);
+            s1 = pr::mma(__builtin_bit_cast(h8, x1[i]), __builtin_bit_cast(h8, o1.x[i]), s1);
+        }
+    }
     // X^T: rows {4 hh .. + 3, 8 + 4 hh .. + 3} of 16, channel c32 of 32 (D = 16: the
     // upper 16 repeat the lower)
     static __device__ __forceinline__ void turn(Turned &a, const u4 *t, int kb, int lane)
@@ -181,6 +199,12 @@ template <int D> struct Ops<float, D> {
             for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], o.x[j][i], s, 0, 0, 0);
         }
         return s;
+    }
+    static __device__ __forceinline__ void scores2(const u4 *t0, int kb0, const Own &o0, f16v &s0, const u4 *t1, int kb1,
+                                                   const Own &o1, f16v &s1, int hh, int c32)
+    {
+        s0 = scores(t0, kb0, hh, c32, o0);
+        s1 = scores(t1, kb1, hh, c32, o1);
     }
     // rows 8 (i/4) + 4 hh + i%4, DT neighbouring channels from c32 DT on (D = 16: the
     // upper lanes repeat the lower)

@@ -138,8 +138,7 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
         }
     };
     const auto scores = [&](const u4 *kt, const u4 *vt, int kb, f16v &s, f16v &dp) {
-        s = O::scores(kt, at + kb, hh, c32, q);
-        dp = O::scores(vt, at + kb, hh, c32, o);
+        O::scores2(kt, at + kb, q, s, vt, at + kb, o, dp, hh, c32);
     };
     walk<E, D, TILE>(p.kh + keys * D, p.vh + keys * D, 0, 0, whole, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
                      [&](const u4 *kt, const u4 *vt, int n0) {
@@ -288,8 +287,8 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
         }
     };
     const auto scores = [&](const u4 *qt, const u4 *ot, int kb, f16v &s, f16v &dp) {
-        s = O::scores(qt, at + kb, hh, c32, k);
-        if constexpr (GK) dp = O::scores(ot, at + kb, hh, c32, v);
+        if constexpr (GK) O::scores2(qt, at + kb, k, s, ot, at + kb, v, dp, hh, c32);
+        else s = O::scores(qt, at + kb, hh, c32, k);
     };
     walk<E, D, TILE>(p.qh + base * D, p.oh + base * D, begin, min(whole, rows), rows, rows, rows - 1, x0, x1,
                      y0, y1, wave, lane,
