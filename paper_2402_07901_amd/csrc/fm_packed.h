@@ -13,9 +13,11 @@
 // bf16 calls work on fp16: q^ and k^ (|x| <= sqrt D) have three bits more than
 // bf16; a row of v (dO) is an exact fp16 row times a power of two of its own,
 // which leaves all but what is 2^-17 of the row's largest.  The powers go into
-// the weights, relative to the largest among the tiles so far: a wave that meets
-// a larger one scales its sums down.  32x32x16 MFMA: one 16-byte LDS read per
-// lane and 16 channels for scores, the transposing read for X^T.
+// the weights, relative to the largest so far: a wave that meets a larger one scales
+// its sums down.  Where every column sees the whole tile, one power serves the wave;
+// in the tiles that the mask cuts every column (lane) has its own, of what it sees: a
+// row keeps its bits beside later tokens of any size.  32x32x16 MFMA: one 16-byte LDS
+// read per lane and 16 channels for scores, the transposing read for X^T.
 // float32 calls: float32 MFMA (32x32x2), operands in full, no powers.
 //
 // Tiles come straight from the planes that the prep kernel writes (k^, v; backward
@@ -84,6 +86,30 @@ __device__ __forceinline__ int wave_max(int x)
     x = max((int)a[0], (int)a[1]);
     const auto b = __builtin_amdgcn_permlane32_swap((uint32_t)x, (uint32_t)x, false, false);
     return scalar(max((int)b[0], (int)b[1]));
+}
+
+__device__ __forceinline__ int wave_min(int x) { return -wave_max(-x); }
+
+// The largest x of the lanes 0 .. i, or i .. N - 1, of every N; none: NO_POWER.
+template <int N> __device__ __forceinline__ int max_to(int x, int lane, int i)
+{
+#pragma unroll
+    for (int o = 1; o < N; o *= 2) {
+        const int y = __shfl_up(x, o, N);
+        x = lane % N >= o ? max(x, y) : x;
+    }
+    const int y = __shfl(x, min(max(i, 0), N - 1), N);
+    return i < 0 ? NO_POWER : y;
+}
+template <int N> __device__ __forceinline__ int max_from(int x, int lane, int i)
+{
+#pragma unroll
+    for (int o = 1; o < N; o *= 2) {
+        const int y = __shfl_down(x, o, N);
+        x = lane % N + o < N ? max(x, y) : x;
+    }
+    const int y = __shfl(x, min(max(i, 0), N - 1), N);
+    return i >= N ? NO_POWER : y;
 }
 
 // What a wave does with rows 32 kb .. 32 kb + 31 of a tile t.
@@ -357,15 +383,15 @@ template <typename E, int D, int WK> struct Cut {
     static_assert(TILE * D * (int)sizeof(E) >= Ops<E, D>::DT * 16 * 64 * 4 || WK == 1, "an array for a wave's sums");
 };
 
-// Adds the waves' sums (times 2^power of each) in LDS, one array per wave (a tile's: at
-// least 4 KB for 32 channels); power becomes that of the sum.  The caller has made
+// Adds the waves' sums (times 2^power of each column) in LDS, one array per wave (a tile's:
+// at least 4 KB for 32 channels); power becomes that of the sum.  The caller has made
 // sure that the arrays are free, and puts a barrier between.
 template <int DT>
-__device__ __forceinline__ void join_put(f16v *acc, int &power, int *powers, u4 *mine, int wave, int lane)
+__device__ __forceinline__ void join_put(f16v *acc, int &power, int (*powers)[64], u4 *mine, int wave, int lane)
 {
-    powers[wave] = power;
+    powers[wave][lane] = power;
     __syncthreads();
-    const int most = max(max(powers[0], powers[1]), max(powers[2], powers[3]));
+    const int most = max(max(powers[0][lane], powers[1][lane]), max(powers[2][lane], powers[3][lane]));
     const float f = __builtin_ldexpf(1.0f, max(power - most, -300));
     power = most;
 #pragma unroll

@@ -13,12 +13,13 @@
 //
 // Powers of two (bf16 calls).  With dO_i = 2^a_i o_i, v_n = 2^b_n x_n and
 // delta_i = 2^a_i d_i:
-//   rows:  T 2^-(a_i + E) / u_i = t (2^(b_n - E) o_i.x_n - 2^-E d_i), E >= every b_n so far
-//          and the wave's d_i, so that t (.) stays below (1 + D)^2 < 2^15;
-//   keys:  u_i 2^a_i = m_i 2^e_i, M >= every e_i so far, F >= the wave's b_n and every d_i
-//          so far:  T 2^-(M + F) = t (X_i 2^(b_n - F) o_i.x_n - Y_i),  X_i = m_i 2^(e_i - M),
+//   rows:  T 2^-(a_i + E) / u_i = t (2^(b_n - E) o_i.x_n - 2^-E d_i), E >= every b_n seen so
+//          far and d_i, so that t (.) stays below (1 + D)^2 < 2^15;
+//   keys:  u_i 2^a_i = m_i 2^e_i, M >= every e_i seen so far, F >= b_n and every d_i seen so
+//          far:  T 2^-(M + F) = t (X_i 2^(b_n - F) o_i.x_n - Y_i),  X_i = m_i 2^(e_i - M),
 //          Y_i = X_i d_i 2^-F,  and w X_i for dv.
-// A wave that meets a larger one scales its sums down.
+// A wave that meets a larger one scales its sums down.  E is a row's own; M and F are a
+// key's own in the tiles that the mask cuts, then the wave's.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -76,7 +77,7 @@ __device__ __forceinline__ void scale_down(f16v *acc, int e)
 
 template <typename T, int D, int P, int WK>
 __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typename plane_of<T>::type> &p, int head,
-                                           const Place &pl, u4 *x0, u4 *x1, u4 *y0, u4 *y1, f4 *factors, int *wave_powers)
+                                           const Place &pl, u4 *x0, u4 *x1, u4 *y0, u4 *y1, f4 *factors, int (*wave_powers)[64])
 {
     typedef typename plane_of<T>::type E;
     using O = Ops<E, D>;
@@ -95,8 +96,8 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
     f16v acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f16v{};
-    int power = O::POWERS ? wave_max(info.ed >> 1) : 0;   // E
-    float delta = O::POWERS ? __builtin_ldexpf(info.delta, -power) : info.delta;
+    int power = O::POWERS ? info.ed >> 1 : 0;   // E
+    float delta = info.delta, up = 1.f;         // delta 2^-R and 2^(R - E), R the tile's power
 
     const int end = a.causal ? (min(pl.first + COLS, rows) - 1) / a.group + 1 : pl.len;
     const int whole = (a.causal ? pl.first / a.group + 1 : pl.len) / (2 * TILE) * (2 * TILE);
@@ -110,6 +111,7 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
         O::turn(k, kt, at + kb, lane);
         float w[16];
         const int left = lim - n1 - 4 * hh;
+        const float tau_up = tau * up;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             f4 f;
@@ -117,24 +119,30 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float d = O::POWERS ? fmaf(dp[4 * j + i], f[i], -delta) : dp[4 * j + i] - delta;
-                float x = P == 2 ? fmaf(s[4 * j + i], tau, 1.0f) * d : d;
+                float x = P == 2 ? fmaf(s[4 * j + i], tau_up, up) * d : O::POWERS ? up * d : d;
                 if constexpr (decltype(masked)::value) x = 8 * j + i <= left ? x : 0.f;
                 w[4 * j + i] = x;
             }
         }
         O::add(acc, k, w);
     };
-    const auto powers = [&](int n0) {
+    const auto powers = [&](int n0, auto masked) {
         if constexpr (O::POWERS) {
             const int b = next >> 1;
             next = p.b[keys + min(n0 + TILE + 32 * at + lane % MINE, pl.len - 1)];
-            const int most = wave_max(b);
-            if (most > power) {
+            const int top = wave_max(b);
+            if (__any(top > power)) {
+                int most = top;
+                if constexpr (decltype(masked)::value) most = max_to<MINE>(b, lane, lim - n0 - 32 * at);
+                most = max(most, power);
                 scale_down<DT>(acc, power - most);
                 power = most;
-                delta = __builtin_ldexpf(info.delta, -power);
             }
-            ((float *)factors)[lane % MINE] = __builtin_ldexpf(1.0f, b - power);
+            // (values 2^60 below E vanish in any case)
+            const int R = max(top, power - 60);
+            delta = __builtin_ldexpf(info.delta, -R);
+            up = __builtin_ldexpf(1.0f, min(R - power, 120));
+            ((float *)factors)[lane % MINE] = __builtin_ldexpf(1.0f, b - top);
         }
     };
     const auto scores = [&](const u4 *kt, const u4 *vt, int kb, f16v &s, f16v &dp) {
@@ -142,7 +150,7 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
     };
     walk<E, D, TILE>(p.kh + keys * D, p.vh + keys * D, 0, 0, whole, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
                      [&](const u4 *kt, const u4 *vt, int n0) {
-        powers(n0);
+        powers(n0, std::false_type{});
         if constexpr (ahead<E, D>()) {
             f16v s[MINE / 32], dp[MINE / 32];
 #pragma unroll
@@ -159,7 +167,7 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
         }
     },
                      [&](const u4 *kt, const u4 *vt, int n0) {
-        powers(n0);
+        powers(n0, std::true_type{});
 #pragma unroll
         for (int kb = 0; kb < MINE / 32; ++kb) {
             if (n0 + 32 * (at + kb) >= none) break;
@@ -184,7 +192,7 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
 
 template <typename T, int D, int P, int ROLE, int WK>
 __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typename plane_of<T>::type> &p, int head,
-                                           const Place &pl, u4 *x0, u4 *x1, u4 *y0, u4 *y1, f4 *factors, int *wave_powers)
+                                           const Place &pl, u4 *x0, u4 *x1, u4 *y0, u4 *y1, f4 *factors, int (*wave_powers)[64])
 {
     typedef typename plane_of<T>::type E;
     using O = Ops<E, D>;
@@ -203,6 +211,8 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
 #pragma unroll
     for (int d = 0; d < DT; ++d) dk[d] = dv[d] = f16v{};
     int b = 0, M = NO_POWER, F = 0;   // the column's power; the largest so far
+    bool shared = false;              // whether M and F are the wave's
+    float cx = 1.f, cy = 1.f;         // 2^-M and 2^-F times the tile's largest
     // the column's values in the power F
     const auto own_values = [&] {
         if constexpr (GK) O::own(v, p.vh + (keys + n) * D, hh);
@@ -213,8 +223,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
         }
     };
     if constexpr (O::POWERS) {
-        b = p.b[keys + n] >> 1;
-        F = wave_max(b);
+        F = b = p.b[keys + n] >> 1;
     }
     own_values();
 
@@ -233,7 +242,11 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
         const int lim = least - r1 - 4 * hh;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const f4 fx = factors[8 * kb + 2 * j + hh], fy = factors[16 + 8 * kb + 2 * j + hh];
+            f4 fx = factors[8 * kb + 2 * j + hh], fy = factors[16 + 8 * kb + 2 * j + hh];
+            if constexpr (O::POWERS && decltype(masked)::value) {
+                fx *= cx;
+                fy = fy * cx * cy;
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 // f_1, and f_2'; 2 f_2 = t^2 + 1
@@ -259,25 +272,53 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
             O::add(dv, xt, w);
         }
     };
-    const auto powers = [&](int r0) {
+    const auto powers = [&](int r0, auto masked) {
         const RowInfo info = next;
         odd |= __ballot(info.ed & 1);
         next = p.info[base + min(r0 + TILE + 32 * at + lane % MINE, rows - 1)];
         float X = info.m, Y = info.m * info.delta;
         if constexpr (O::POWERS) {
-            const int e = wave_max(info.e), d = wave_max(info.ed >> 1);
-            if (e > M || d > F) {
-                const int m = max(M, e), g = max(F, d);
+            const int e = wave_max(info.e), d = GK ? wave_max(info.ed >> 1) : NO_POWER;
+            const auto raise = [&](int m, int f) {
                 scale_down<DT>(dv, M - m);
-                scale_down<DT>(dk, M - m + F - g);
+                if constexpr (GK) scale_down<DT>(dk, M - m + F - f);
                 M = m;
-                if (g > F) {
-                    F = g;
+                if (GK && __any(f > F)) {
+                    F = f;
                     own_values();
                 }
+            };
+            if constexpr (decltype(masked)::value) {
+                if (__any(e > M || d > F)) {
+                    const int from = least - r0 - 32 * at;
+                    const int m = max(M, max_from<MINE>(info.e, lane, from));
+                    const int f = GK ? max(F, max_from<MINE>(info.ed >> 1, lane, from)) : F;
+                    raise(m, f);
+                }
+                cx = __builtin_ldexpf(1.0f, min(e - M, 126));
+                cy = __builtin_ldexpf(1.0f, min(d - F, 126));
+                X = __builtin_ldexpf(info.m, info.e - e);
+                Y = X * __builtin_ldexpf(info.delta, -d);
+            } else {
+                if (!shared) {
+                    // the least of the columns', which keeps all their bits (within
+                    // 2^40, for what the sums have room for)
+                    const int m = max(wave_min(M), wave_max(M) - 40);
+                    const int f = GK ? max(wave_max(b), max(wave_min(F), wave_max(F) - 40)) : F;
+#pragma unroll
+                    for (int x = 0; x < DT; ++x) {
+                        dv[x] *= __builtin_ldexpf(1.0f, max(M - m, -300));
+                        if constexpr (GK) dk[x] *= __builtin_ldexpf(1.0f, max(M - m + F - f, -300));
+                    }
+                    M = m;
+                    F = f;
+                    own_values();
+                    shared = true;
+                }
+                if (scalar(e) > scalar(M) || (GK && scalar(d) > scalar(F))) raise(max(M, e), GK ? max(F, d) : F);
+                X = __builtin_ldexpf(info.m, info.e - M);
+                Y = X * __builtin_ldexpf(info.delta, -F);
             }
-            X = __builtin_ldexpf(info.m, info.e - M);
-            Y = X * __builtin_ldexpf(info.delta, -F);
         }
         // rows past the last weigh nothing
         if (r0 + 32 * at + lane % MINE >= rows) X = Y = 0.f;
@@ -293,7 +334,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
     walk<E, D, TILE>(p.qh + base * D, p.oh + base * D, begin, min(whole, rows), rows, rows, rows - 1, x0, x1,
                      y0, y1, wave, lane,
                      [&](const u4 *qt, const u4 *ot, int r0) {
-        powers(r0);
+        powers(r0, std::false_type{});
         if constexpr (ROLE == DV || (ROLE == DK && ahead<E, D>())) {
             f16v s[MINE / 32], dp[MINE / 32];
 #pragma unroll
@@ -310,7 +351,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
         }
     },
                      [&](const u4 *qt, const u4 *ot, int r0) {
-        powers(r0);
+        powers(r0, std::true_type{});
 #pragma unroll
         for (int kb = 0; kb < MINE / 32; ++kb) {
             const int r1 = r0 + 32 * (at + kb);
@@ -363,7 +404,7 @@ __global__ __launch_bounds__(THREADS, WK > 1 || (sizeof(T) == 4 && D == 128) ? 1
     constexpr int N = Cut<E, D, WK>::TILE * Ops<E, D>::C;
     __shared__ u4 x0[N], x1[N], y0[N], y1[N];
     __shared__ f4 factors[THREADS / 64][32];
-    __shared__ int wave_powers[THREADS / 64];
+    __shared__ int wave_powers[THREADS / 64][64];
     f4 *const mine = factors[scalar(threadIdx.x / 64)];
     const int head = blockIdx.x % a.Hkv;
     const Place pl = scalar(p.places[blockIdx.x / a.Hkv]);

@@ -271,8 +271,8 @@ __global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArg
     using W = Cut<E, D, WK>;
     constexpr int DT = O::DT, TILE = W::TILE, MINE = W::MINE, COLS = W::COLS;
     __shared__ u4 x0[TILE * O::C], x1[TILE * O::C], y0[TILE * O::C], y1[TILE * O::C];
-    __shared__ h4 factors[THREADS / 64][MINE / 4];
-    __shared__ int wave_powers[THREADS / 64];
+    __shared__ f4 factors[THREADS / 64][MINE / 4];   // (whole tiles: halves)
+    __shared__ int wave_powers[THREADS / 64][64];
     __shared__ float wave_sums[THREADS / 64][64];
 
     // a key head's workgroups are Hkv apart, on one XCD where 8 divides Hkv
@@ -313,7 +313,8 @@ __global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArg
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f16v{};
     float g = 0.f;          // second order: of 2 w = (1 + tau s)^2 + 1
-    int power = NO_POWER;   // of acc: the largest of the values' so far
+    int power = NO_POWER;   // of acc: the largest of the values that the row has seen
+    float up = 1.f;         // 2^-power times the tile's largest
 
     const int end = a.causal ? (min(pl.first + COLS, rows) - 1) / a.group + 1 : pl.len;   // keys that some row sees
     // keys before `whole` are seen by all rows, from `none` on by none of the wave's
@@ -344,12 +345,23 @@ __global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArg
             pr::h2 h[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const h4 f = factors[wave][8 * kb + 2 * j + hh];
+                pr::h2 f[2];
+                if constexpr (decltype(masked)::value) {
+                    f4 x = factors[wave][8 * kb + 2 * j + hh];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = 8 * j + i <= left ? x[i] * up : 0.f;
+                    f[0] = pr::cvt2(x[0], x[1]);
+                    f[1] = pr::cvt2(x[2], x[3]);
+                } else {
+                    const h4 x = ((const h4 *)factors[wave])[8 * kb + 2 * j + hh];
+                    f[0] = pr::h2{x[0], x[1]};
+                    f[1] = pr::h2{x[2], x[3]};
+                }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const pr::h2 x = pr::cvt2(w[4 * j + 2 * i], w[4 * j + 2 * i + 1]);
                     g = __builtin_amdgcn_fdot2(x, one, g, false);
-                    h[2 * j + i] = x * pr::h2{f[2 * i], f[2 * i + 1]};
+                    h[2 * j + i] = x * f[i];
                 }
             }
             O::add(acc, v, h);
@@ -359,24 +371,32 @@ __global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArg
             O::add(acc, v, w);
         }
     };
-    const auto powers = [&](int n0) {
+    const auto powers = [&](int n0, auto masked) {
         const int b = next >> 1;
         odd |= __ballot(next & 1);
         next = p.b[keys + min(n0 + TILE + 32 * at + lane % MINE, pl.len - 1)];
         if constexpr (O::POWERS) {
-            const int most = wave_max(b);
-            if (most > power) {
+            const int top = wave_max(b);
+            if (__any(top > power)) {
+                int most = top;
+                if constexpr (decltype(masked)::value) most = max_to<MINE>(b, lane, lim - n0 - 32 * at);
+                most = max(most, power);
                 const float f = __builtin_ldexpf(1.0f, max(power - most, -300));
 #pragma unroll
                 for (int d = 0; d < DT; ++d) acc[d] *= f;
                 power = most;
             }
-            ((_Float16 *)factors[wave])[lane % MINE] = (_Float16)__builtin_ldexpf(1.0f, b - power);
+            if constexpr (decltype(masked)::value) {
+                up = __builtin_ldexpf(1.0f, min(top - power, 126));
+                ((float *)factors[wave])[lane % MINE] = __builtin_ldexpf(1.0f, b - top);
+            } else {
+                ((_Float16 *)factors[wave])[lane % MINE] = (_Float16)__builtin_ldexpf(1.0f, b - power);
+            }
         }
     };
     walk<E, D, TILE>(p.kh + keys * D, p.vh + keys * D, 0, 0, whole, end, pl.len - 1, x0, x1, y0, y1, wave, lane,
                      [&](const u4 *kt, const u4 *vt, int n0) {
-        powers(n0);
+        powers(n0, std::false_type{});
         f16v s[MINE / 32];
 #pragma unroll
         for (int kb = 0; kb < MINE / 32; ++kb) s[kb] = O::scores(kt, at + kb, hh, c32, own);
@@ -384,7 +404,7 @@ __global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArg
         for (int kb = 0; kb < MINE / 32; ++kb) block(s[kb], vt, n0 + 32 * (at + kb), kb, std::false_type{});
     },
                      [&](const u4 *kt, const u4 *vt, int n0) {
-        powers(n0);
+        powers(n0, std::true_type{});
 #pragma unroll
         for (int kb = 0; kb < MINE / 32; ++kb)
             if (n0 + 32 * (at + kb) < none)

@@ -388,3 +388,44 @@ def test_prompts_then_tokens(dtype):
         # about 7e-3 sqrt(2 D) = 8e-2 of |s| ~ sqrt(D) = 8 in each score and 2e-2 of
         # each weight, averaged over the keys; held to four times that
         assert (small.float() - ref).norm() <= 8e-2 * ref.norm()
+
+
+@pytest.mark.parametrize("D", [16, 32, 64, 128])
+@pytest.mark.parametrize("heads", [(4, 2), (120, 120)])   # 32 columns to a workgroup, 128
+@pytest.mark.parametrize("p", [1, 2])
+def test_rows_that_do_not_see_much_larger_ones(D, heads, p):
+    """A token's values 2^90 times the others' leave O and dq of the rows before it
+    as they are, held to the bounds of the sequence without it; one's dO 2^36 times
+    the others' leaves dk and dv of the keys after it."""
+    label = f"packed, unseen rows, D={D} p={p} H={heads}"
+    say(label)
+    tau = 1.0 if p == 2 else 1.0 / D
+    n, at = 400, (70, 333)
+    for a in at:
+        x = Packed([n], *heads, D, "bf16", seed=a)
+        x.v[a] *= 2.0 ** 90
+        out, g = fm.fastmax_packed_fwd(x.q, x.k, x.v, x.starts, p=p, causal=True, scale=tau)
+        dq = fm.fastmax_packed_bwd(x.q, x.k, x.v, x.starts, out, x.dout, g, p=p, causal=True, scale=tau)[0]
+        short = Packed([n], *heads, D, "bf16", seed=a)
+        short.lens, short.start = [a], np.array([0, a])
+        do = su.np64(x.dout)
+        for rows, h, hs, head in short.heads(p, tau, True):
+            if h > 1:
+                break
+            O, eO, G, eG = head.forward()
+            su.check(out[rows, hs], O, OUT["bf16"] * np.abs(O) + 1.01 * eO, (label, a, "O", h))
+            want, bound = head.backward(do[rows, hs], 2 * OUT["bf16"] + eO.max() / np.abs(O).max())[0]
+            su.check(dq[rows, hs], want, OUT["bf16"] * (np.abs(want) + bound) + 1.01 * bound, (label, a, "dq", h))
+
+        y = Packed([n], *heads, D, "bf16", seed=a)
+        y.dout[a] *= 2.0 ** 36
+        out, g = given(y, p, tau, True)
+        _, dk, dv = fm.fastmax_packed_bwd(y.q, y.k, y.v, y.starts, out, y.dout, g, p=p, causal=True, scale=tau)
+        do = su.np64(y.dout)
+        do[:a + 1] = 0
+        for rows, h, hs, head in y.heads(p, tau, True):
+            if h > 1:
+                break
+            for name, got, (want, bound) in zip(("dk", "dv"), (dk, dv), head.backward(do[rows, hs], OUT["bf16"])[1:]):
+                want, bound = want[a + 1:], bound[a + 1:]
+                su.check(got[a + 1:, h], want, OUT["bf16"] * (np.abs(want) + bound) + 1.01 * bound, (label, a, name, h))
