@@ -30,6 +30,7 @@ namespace {
 using namespace paged;
 
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef int i4 __attribute__((ext_vector_type(4)));
 typedef int i16v __attribute__((ext_vector_type(16)));
@@ -440,7 +441,8 @@ __device__ __forceinline__ uint2 codes4(uint32_t w)
 // rows stay exact but for what is 2^-17 of their largest); weights times 2^-e, which
 // costs nothing in 1 + x (c1 + c2 x): with |k_n| <= 127 sqrt(D) ks_n a row's largest
 // possible weight stays below 2^14; values times 2^-P.  e and P follow from the largest
-// scales among the tiles so far: a wave that meets a larger one scales its sums.
+// scales that a row has seen so far (P, where every row sees the whole step, from the
+// wave's): a wave that meets a larger one scales its sums.
 // What it takes per pair beside the products: ks x, the weight (2), its conversion,
 // sum and scale in packed halves (4.5 instructions in bf16).
 template <typename T, int D>
@@ -452,7 +454,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
     constexpr int LN = KB * LP > THREADS ? KB * LP / THREADS : 1, LR = THREADS / LP;   // loads of a thread, rows of one
     __shared__ u4 keys0[KB * C], keys1[KB * C], values0[KB * C], values1[KB * C];
     __shared__ f4 kscale[2][KB / 4], vscale[2][KB / 4];
-    __shared__ f4 factors[THREADS / 64][KB / 4];              // of values, a wave's own (bf16: halves)
+    __shared__ f4 factors[THREADS / 64][KB / 4];              // of values in whole steps, a wave's own (bf16: halves)
 
     // Row tiles of one (sequence, key head, split) read the same keys, so every
     // `pieces`th of them go to the same XCD.  Late row tiles see the most keys and
@@ -518,7 +520,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
         }
         f16v acc[DT];
         float g = 0.f, c0 = 1.f, c1 = 0.f, c2 = 0.f;   // weight c0 + x (c1 + c2 x), times 2^-e
-        int kpower = -1000, vpower = -1000, e = 0;     // the largest of the scales so far; e: see c0
+        int kpower = -1000, vpower = -1000, e = 0;     // the largest of the scales seen so far; e: see c0
+        int all_k = 0, all_v = 0;                      // in whole steps: the least kpower, the wave's vpower
 #pragma unroll
         for (int d = 0; d < DT; ++d) acc[d] = f16v{};
 
@@ -578,29 +581,68 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
             if (threadIdx.x < 2 * KB) ((float *)(threadIdx.x < KB ? kscale : vscale)[b])[threadIdx.x & (KB - 1)] = sr;
         };
 
+        // Which of keys {0 .. 3} + 8 i + 4 hh of 32 the lane's row sees: key n0 + n of a
+        // tile if n <= lim and (n > lim - window or it is a first token).
+        struct Limits { int lim, low, sinks; };
+        const auto limits = [&](int i0, int kb, int i) {
+            const int it = i0 + 2 * kb + i / 2, n0 = sp.tile(min(it, end - 1)) * KT + 4 * hh;
+            const int lim = it < end ? max(pos, -1) - n0 : -1;
+            return Limits{lim, lim - a.window, a.sinks - n0};
+        };
+        const auto sees = [&](const Limits &l, int n) { return n <= l.lim && (n > l.low || n < l.sinks); };
         // The step's powers, and its values' factors.
-        const auto powers = [&](int b) {
-            const float ks = ((const float *)kscale[b])[lane], vs = ((const float *)vscale[b])[lane];
-            const int pk = wave_max(pr::exp_above(fabsf(ks))), pv = wave_max(pr::exp_above(fabsf(vs)));
-            if (pk > kpower || pv > vpower) {
-                kpower = max(kpower, pk);
-                const float most = __builtin_ldexpf(size, kpower);
-                const float w = a.c2 == 0.f ? 1.0f + most : fmaf(0.5f * most, most, 1.0f + most);
-                const int to = w < 3e38f ? pr::exp_above(w) - 14 : 114;
-                const int v = max(vpower, pv);
-                const float fg = __builtin_ldexpf(1.0f, max(e - to, -300)), f = __builtin_ldexpf(fg, max(vpower - v, -300));
-                g *= fg;
+        const auto raise = [&](int pk, int from, int v) {
+            kpower = max(kpower, pk);
+            const float most = __builtin_ldexpf(size, kpower);
+            const float w = a.c2 == 0.f ? 1.0f + most : fmaf(0.5f * most, most, 1.0f + most);
+            const int to = w < 3e38f ? pr::exp_above(w) - 14 : 114;
+            const float fg = __builtin_ldexpf(1.0f, max(e - to, -300)), f = __builtin_ldexpf(fg, max(from - v, -300));
+            g *= fg;
 #pragma unroll
-                for (int d = 0; d < DT; ++d) acc[d] *= f;
-                e = to;
-                vpower = v;
-                c0 = __builtin_ldexpf(1.0f, -e);
-                c1 = a.c1 * qs * c0;
-                c2 = a.c2 * qs * (qs * c0);
+            for (int d = 0; d < DT; ++d) acc[d] *= f;
+            e = to;
+            c0 = __builtin_ldexpf(1.0f, -e);
+            c1 = a.c1 * qs * c0;
+            c2 = a.c2 * qs * (qs * c0);
+        };
+        const auto powers = [&](int b, int i0, auto masked) {
+            if constexpr (decltype(masked)::value) {
+                // by step, then, if that is more than a row's so far, by what each row sees
+                // (what none sees may be anything)
+                const float ks = ((const float *)kscale[b])[lane], vs = ((const float *)vscale[b])[lane];
+                const int pk = wave_max(pr::exp_above(fabsf(ks))), pv = wave_max(pr::exp_above(fabsf(vs)));
+                if (__any(pk > kpower || pv > vpower)) {
+                    uint32_t k = 0, v = 0;
+#pragma unroll 1
+                    for (int j = 0; j < KB / 8; ++j) {
+                        const f4 k4 = kscale[b][2 * j + hh], v4 = vscale[b][2 * j + hh];
+                        const Limits l = limits(i0, j / 4, j % 4);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t x = __float_as_uint(fabsf(k4[i])), y = __float_as_uint(fabsf(v4[i]));
+                            const bool see = sees(l, 8 * (j % 2) + i);
+                            k = see && x < 0x7f800000u ? max(k, x) : k;
+                            v = see && y < 0x7f800000u ? max(v, y) : v;
+                        }
+                    }
+                    const int seen_k = pr::exp_above(__uint_as_float(halves_max(k))),
+                              seen_v = pr::exp_above(__uint_as_float(halves_max(v)));
+                    const int to = max(vpower, seen_v);
+                    raise(seen_k, vpower, to);
+                    vpower = to;
+                }
+            } else {
+                const float ks = ((const float *)kscale[b])[lane], vs = ((const float *)vscale[b])[lane];
+                const int pk = wave_max(pr::exp_above(fabsf(ks))), pv = wave_max(pr::exp_above(fabsf(vs)));
+                if (pk > all_k || pv > all_v) {
+                    raise(pk, all_v, max(all_v, pv));
+                    all_k = max(all_k, pk);
+                    all_v = max(all_v, pv);
+                }
+                const float f = __builtin_ldexpf(vs, -all_v);
+                if constexpr (FP == 1) ((_Float16 *)factors[wave])[lane] = (_Float16)f;
+                else ((float *)factors[wave])[lane] = f;
             }
-            const float f = __builtin_ldexpf(vs, -vpower);
-            if constexpr (FP == 1) ((_Float16 *)factors[wave])[lane] = (_Float16)f;
-            else ((float *)factors[wave])[lane] = f;
         };
         const auto scores = [&](const u4 *kt, int kb) {
             u4 k[KS];
@@ -637,19 +679,32 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
             for (int i = 0; i < 4; ++i) {
                 const f4 ks = kscale[b][8 * kb + 2 * i + hh];
                 float y[4];
-                bool seen[4];
-                // key n0 + n of a tile is seen if n <= lim and (n > lim - window or it
-                // is a first token)
-                const int it = i0 + 2 * kb + i / 2, n0 = sp.tile(min(it, end - 1)) * KT + 4 * hh;
-                const int lim = it < end ? max(pos, -1) - n0 : -1, low = lim - a.window, sinks = a.sinks - n0;
+                f4 f;
+                pr::h2 fh[2];
+                Limits l;
+                if constexpr (decltype(masked)::value) {
+                    f = vscale[b][8 * kb + 2 * i + hh];
+                    l = limits(i0, kb, i);
+                } else if constexpr (FP == 1) {
+                    const h4 x = ((const h4 *)factors[wave])[8 * kb + 2 * i + hh];
+                    fh[0] = pr::h2{x[0], x[1]};
+                    fh[1] = pr::h2{x[2], x[3]};
+                } else {
+                    f = factors[wave][8 * kb + 2 * i + hh];
+                }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float z = x[4 * i + j] * ks[j];
                     y[j] = fmaf(fmaf(z, c2, c1), z, c0);
-                    const int n = 8 * (i % 2) + j;
-                    // (the scales of a key that is not seen may be NaN)
-                    seen[j] = !decltype(masked)::value || (n <= lim && (n > low || n < sinks));
-                    y[j] = seen[j] ? y[j] : 0.f;
+                    if constexpr (decltype(masked)::value) {
+                        const bool see = sees(l, 8 * (i % 2) + j);
+                        y[j] = see ? y[j] : 0.f;
+                        f[j] = see ? __builtin_ldexpf(f[j], -vpower) : 0.f;
+                    }
+                }
+                if constexpr (FP == 1 && decltype(masked)::value) {
+                    fh[0] = pr::cvt2(f[0], f[1]);
+                    fh[1] = pr::cvt2(f[2], f[3]);
                 }
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
@@ -657,18 +712,14 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
                         // the sum of the rounded weights, as the numerator takes them
                         const pr::h2 one = {(_Float16)1.0f, (_Float16)1.0f};
                         const pr::h2 h = pr::cvt2(y[2 * j], y[2 * j + 1]);
-                        pr::h2 f = ((const pr::h2 *)factors[wave])[(32 * kb + 8 * i + 4 * hh) / 2 + j];
                         g = __builtin_amdgcn_fdot2(h, one, g, false);
-                        f[0] = seen[2 * j] ? f[0] : (_Float16)0.0f;
-                        f[1] = seen[2 * j + 1] ? f[1] : (_Float16)0.0f;
-                        const pr::h2 o = h * f;
+                        const pr::h2 o = h * fh[j];
                         w[0][i / 2][2 * (i % 2) + j] = __builtin_bit_cast(uint32_t, o);
                     } else {
-                        const f4 f = factors[wave][8 * kb + 2 * i + hh];
                         g += y[2 * j] + y[2 * j + 1];
                         float z[2];
 #pragma unroll
-                        for (int n = 0; n < 2; ++n) z[n] = seen[2 * j + n] ? y[2 * j + n] * f[2 * j + n] : 0.f;
+                        for (int n = 0; n < 2; ++n) z[n] = y[2 * j + n] * f[2 * j + n];
                         const pr::h2 hi = pr::cvt2(z[0], z[1]), lo = pr::cvt2(pr::rest(z[0], hi[0]), pr::rest(z[1], hi[1]));
                         w[0][i / 2][2 * (i % 2) + j] = __builtin_bit_cast(uint32_t, hi);
                         w[FP - 1][i / 2][2 * (i % 2) + j] = __builtin_bit_cast(uint32_t, lo);
@@ -704,7 +755,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
             };
             const auto pairs = [&](int i0, int to, auto masked) {
                 const auto step = [&](const u4 *k, const u4 *v, int b, int i) {
-                    powers(b);
+                    powers(b, i, masked);
 #pragma unroll
                     for (int kb = 0; kb < KB / 32; ++kb) block(scores(k, kb), v, b, i, kb, masked);
                 };
@@ -719,7 +770,17 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
             const int from = min(begin + max(whole - begin + 2 * STEP - 1, 0) / (2 * STEP) * (2 * STEP), end);
             const int to = max(from, begin + max(whole_end - begin, 0) / (2 * STEP) * (2 * STEP));
             pairs(begin, from, std::true_type{});
-            pairs(from, min(to, end), std::false_type{});
+            if (from < min(to, end)) {
+                // values by one power for the wave: the least of the rows', which keeps all
+                // their bits (within 2^80, for what the sums have room for)
+                all_v = max(-wave_max(-vpower), wave_max(vpower) - 80);
+                all_k = -wave_max(-kpower);
+                const float f = __builtin_ldexpf(1.0f, max(vpower - all_v, -300));
+#pragma unroll
+                for (int d = 0; d < DT; ++d) acc[d] *= f;
+                pairs(from, min(to, end), std::false_type{});
+                vpower = all_v;
+            }
             pairs(min(to, end), end, std::true_type{});
         };
         walk(keys0, keys1, values0, values1);

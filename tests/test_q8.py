@@ -361,3 +361,39 @@ def test_captured_steps():
         assert torch.equal(out, step(twin)), i
         for a, b in zip(c.cache, twin):
             assert torch.equal(torch.nan_to_num(a.float(), nan=9.0), torch.nan_to_num(b.float(), nan=9.0))
+
+
+@pytest.mark.parametrize("D", [16, 64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (40, 2), (300, 0)])
+def test_what_no_row_sees_may_be_anything(D, dtype, window, sinks):
+    """Scales of slots behind the sequences, of any size, and values of a later
+    token of the chunk 2^40 times the others': the rows that see neither keep their
+    bits."""
+    import torch
+    label = f"paged q8 unseen slots D={D} {dtype} window={window}"
+    say(label)
+    kw = {"window": window, "sinks": sinks}
+    for news in ([1, 1, 1], [150, 33, 400]):
+        c = Cache([203, 40, 777], news, 4, 2, D, 64, dtype, seed=D)
+        free = torch.isnan(c.ks)
+        want = c.run(max_q=max(news), **kw)
+        c.check(want, label, **kw)
+        for x in (1e38, float("inf"), -1e30):
+            c.ks[free], c.vs[free] = x, -x
+            assert torch.equal(c.run(max_q=max(news), **kw), want), (label, x)
+        if max(news) == 1:
+            continue
+        for s, back in ((0, 20), (2, 310)):   # a token that many before the end
+            at, (page, place) = c.lens_h[s] - back, c.at(s, c.lens_h[s] - back)
+            kept = c.vs[page, :, place].clone()
+            c.vs[page, :, place] *= 2.0 ** 40
+            got = c.run(max_q=max(news), **kw)
+            pos = at - c.lens_h[s] + news[s]      # its row in the chunk
+            rows = torch.arange(c.start[-1], device="cuda") - int(c.start[s])
+            sees = (rows >= pos) & (rows < news[s])
+            if window and pos + c.lens_h[s] - news[s] >= sinks:
+                sees &= rows < pos + window
+            assert torch.equal(got[~sees], want[~sees]), (label, s, back)
+            assert (got[sees].abs().amax((1, 2)) > 2.0 ** 20).all()
+            c.vs[page, :, place] = kept
