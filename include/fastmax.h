@@ -469,11 +469,14 @@ int fastmax_paged_fwd(const void *q, const fastmax_strides_t *q_strides, const v
  * slot may be asked for more than once.
  *
  * fastmax_paged_fwd_q8 is fastmax_paged_fwd over such a cache, dt the type of q
- * and out.  q is taken as whole numbers of 16 bits (float32: 24) under a scale
- * of its row, off by at most 2^-16 (2^-23) of the row's largest magnitude.  A
+ * and out.  Few rows of a key head (single tokens) take q as whole numbers of 16
+ * bits (float32: 24) under a scale of its row, off by at most 2^-16 (2^-23) of the
+ * row's largest magnitude, and weights in 16 (24) bits.  Many rows (chunks) take q
+ * under a power of two of its row, and weights, in 11 bits (float32: 22), and keep
+ * that beside values up to 2^12 larger that they see, and any that they do not.  A
  * row of q that is not finite gives NaN, and so does a key or value row that
- * is, in the rows that see it and in no others.  Workspace:
- * fastmax_paged_q8_workspace_bytes with the same sizes.
+ * is, in the rows that see it and in no others; what slots hold that no row sees
+ * is not used.  Workspace: fastmax_paged_q8_workspace_bytes with the same sizes.
  */
 int fastmax_cache_append_q8(const void *q, const void *k, const void *v,
                             const fastmax_strides_t *strides, void *q_out, int8_t *k_cache,
@@ -517,7 +520,9 @@ int fastmax_paged_fwd_q8(const void *q, const fastmax_strides_t *q_strides, cons
  * touch it, not finite values among it; a value that is not finite makes its
  * channel of the rows that see it not finite.  bf16: v's rows (backward: dout's
  * too) enter fp16 products under a power of two each, outputs and gradients
- * keep bf16's accuracy beside rows up to 2^12 larger; float32: float32 products.
+ * keep bf16's accuracy beside rows up to 2^12 larger that they see, and rows of
+ * any size that they do not (gradients of k and v: dout rows up to 2^40 larger);
+ * float32: float32 products.
  *
  * Backward: gradients of sum(dout * O), from the forward's out and g.
  *   dout       : [T, Hq, D] contiguous

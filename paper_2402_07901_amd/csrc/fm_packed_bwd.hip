@@ -11,6 +11,11 @@
 // over the rows (dk and dv, which share their scores).  No atomics: every output
 // row has one owner, equal calls give equal bits.
 //
+// Five products a pair of rows and keys (seven where the scores are made for dq, dk and
+// dv each) and, beside them, the weights and T: 16 sequences of up to 4096, 12 heads of
+// 64, bf16, 615 us, 440 TFLOP/s of the five; 5 of up to 4095, 32 heads to 8 of 128, 960 us,
+// 510; the prep kernel is 75 us of the first.  float32, D = 128: 86 of 153 TFLOP/s.
+//
 // Powers of two (bf16 calls).  With dO_i = 2^a_i o_i, v_n = 2^b_n x_n and
 // delta_i = 2^a_i d_i:
 //   rows:  T 2^-(a_i + E) / u_i = t (2^(b_n - E) o_i.x_n - 2^-E d_i), E >= every b_n seen so

@@ -2,18 +2,25 @@
 // ks_n c_n, value n is vs_n e_n with codes c_n, e_n of -127 .. 127 and a float32
 // scale each (fm_paged.hip has the formulas and what a row sees).
 //
-// Scores take the codes as they are: q^ of a row becomes one 16-bit (float32: 24-bit)
-// whole number per channel under a scale of its row, cut in signed bytes, and
-// int8 MFMA gives exact sums,
-//     q^ = qs (256 a + b)  ->  s = qs ks (256 a.c + b.c),
-// two products of int8 at the price of one in bf16; q^ is off by at most 2^-16
-// (2^-23) of the row's largest magnitude.  Values: weights times vs in two bf16
-// parts (float32: three) against the codes, which bf16 holds exactly.  A code is
-// always a number, so what unseen slots hold needs no care beyond their scales,
-// which a select keeps out.
+// A code is always a number, so what unseen slots hold needs no care beyond their
+// scales, which a select keeps out.
 //
-// Single tokens: HBM bounds it, D + 4 bytes a row.  A wave walks over key tiles of
-// 16, two at a time, straight from the cache into registers, as fm_paged.hip.
+// Few rows (single tokens).  HBM bounds it, D + 4 bytes a row: 4.8 TB/s at even
+// lengths, 61 sequences of up to 8192 tokens, 32 heads to 8 of 128, 100 us (3.8 TB/s,
+// the longest end alone).  A wave walks over key tiles of 16, two at a time, straight
+// from the cache into registers, as fm_paged.hip.  Scores take the codes as they are:
+// q^ of a row becomes one 16-bit (float32: 24-bit) whole number per channel under a
+// scale of its row, cut in signed bytes, and int8 MFMA gives exact sums,
+//     q^ = qs (256 a + b)  ->  s = qs ks (256 a.c + b.c),
+// two products of int8 at the price of one in bf16 and no conversion of keys; q^ is off
+// by at most 2^-16 (2^-23) of the row's largest magnitude.  Values: weights times vs in
+// two bf16 parts (float32: three) against the codes, which bf16 holds exactly.
+//
+// Many rows (chunks).  The matrix pipe and the instructions beside it bound it: four
+// chunks of up to 2048 tokens over up to 8192, 32 heads to 8 of 128, 580 to 600 us, 590
+// TFLOP/s.  There the few rows' scheme took 766: each wave converted every code for
+// itself, and weights entered as two parts.  So codes become fp16 once a workgroup, on
+// their way into LDS, and one fp16 product (11 bits) does for weights and scores.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
