@@ -458,7 +458,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
     constexpr int FP = sizeof(T) == 2 ? 1 : 2, ROWS = CHUNK_ROWS, WR = ROWS / 4, KB = 64, STEP = KB / KT;
     constexpr int C = D / 8, KS = D / 16, DT = D / 32;        // 16-byte pieces of a row, score steps, channel tiles
     constexpr int LP = D / 16;                                // 16-byte loads of a row of codes
-    constexpr int LN = KB * LP > THREADS ? KB * LP / THREADS : 1, LR = THREADS / LP;   // loads of a thread, rows of one
+    constexpr int LN = KT * LP > 64 ? KT * LP / 64 : 1, LR = 64 / LP;   // loads of a lane, rows of one
+    static_assert(STEP == THREADS / 64, "a wave loads a key tile of a step");
     __shared__ u4 keys0[KB * C], keys1[KB * C], values0[KB * C], values1[KB * C];
     __shared__ f4 kscale[2][KB / 4], vscale[2][KB / 4];
     __shared__ f4 factors[THREADS / 64][KB / 4];              // of values in whole steps, a wave's own (bf16: halves)
@@ -478,7 +479,12 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
     const int rows = seq.count * a.group, page_mask = (1 << a.page_shift) - 1;
     const int8_t *kc = (const int8_t *)a.k + head * a.cache.head, *vc = (const int8_t *)a.v + head * a.cache.head;
     const int32_t *table = a.table + (size_t)s * a.table_cols;
-    const int my_row = threadIdx.x / LP, my_piece = threadIdx.x % LP;   // of a load
+    // A wave loads one key tile of a step, whose page is a scalar: a lane's place in it
+    // does not change.
+    const int my_row = KT * wave + lane / LP, my_piece = lane % LP;
+    const bool loads = KT * LP >= 64 || lane < KT * LP;
+    const int token = (int)a.cache.token, my_at = lane / LP * token + 16 * my_piece;
+    const float *const my_scale = (lane < KT ? a.k_scale : a.v_scale) + lane % KT;
 
     for (int r0 = row_tile * ROWS; r0 < rows; r0 += plan.tiles * ROWS) {
         const Span sp = scalar(span_of_rows(a, seq, r0, ROWS));
@@ -539,53 +545,46 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
         const int whole = a.window < sp.end ? max(sp.sink_tiles, (last - a.window) / KT + 1 - shift) : 0;
         const int whole_end = min(end, (first + 1) / KT - shift);
 
-        // A step's bytes in registers: this thread's pieces of keys and values, and
-        // a scale (threads 0 .. 63: of a key, 64 .. 127: of a value).
+        // A step's bytes in registers: this lane's pieces of keys and values, and a
+        // scale (lanes 0 .. 15: of a key, 16 .. 31: of a value).
         u4 kr[LN], vr[LN];
         float sr = 0.f;
-        const bool loads = KB * LP >= THREADS || threadIdx.x < KB * LP;
-        const auto place_of = [&](int i0, int r) { return sp.tile(min(i0 + r / KT, end - 1)) * KT + r % KT; };
-        int page[LN], spage = 0;   // of the next loads' rows, a step ahead
-        const auto pages_of = [&](int i0) {
-#pragma unroll
-            for (int i = 0; i < LN; ++i)
-                page[i] = table[place_of(i0, (my_row + LR * i) & (KB - 1)) >> a.page_shift];
-            spage = table[place_of(i0, threadIdx.x & (KB - 1)) >> a.page_shift];
-        };
-        const auto checked = [&](int p) {
-            if ((unsigned)p < (unsigned)a.pages) return p;
-            bad = true;
-            return 0;
-        };
+        const auto tile_of = [&](int i0) { return scalar(sp.tile(min(i0 + wave, end - 1)) * KT); };
+        int page = 0;   // of the next load's tile, a step ahead
+        const auto page_of = [&](int i0) { page = table[tile_of(i0) >> a.page_shift]; };
         const auto load = [&](int i0) {
+            const int place = tile_of(i0) & page_mask;
+            int pg = scalar(page);
+            if ((unsigned)pg >= (unsigned)a.pages) {
+                bad = true;
+                pg = 0;
+            }
+            const long long at = pg * a.cache.batch + place * a.cache.token;
+            if (loads) {
 #pragma unroll
-            for (int i = 0; i < LN; ++i) {
-                const int n = place_of(i0, (my_row + LR * i) & (KB - 1));
-                const long long at = checked(page[i]) * a.cache.batch + (n & page_mask) * a.cache.token + 16 * my_piece;
-                if (loads) {
-                    kr[i] = *(const u4 *)(kc + at);
-                    vr[i] = *(const u4 *)(vc + at);
+                for (int i = 0; i < LN; ++i) {
+                    kr[i] = *(const u4 *)(kc + at + (my_at + LR * i * token));
+                    vr[i] = *(const u4 *)(vc + at + (my_at + LR * i * token));
                 }
             }
-            const int n = place_of(i0, threadIdx.x & (KB - 1));
-            const long long at = (((long long)checked(spage) * a.Hkv + head) << a.page_shift) + (n & page_mask);
-            if (threadIdx.x < 2 * KB) sr = (threadIdx.x < KB ? a.k_scale : a.v_scale)[at];
+            if (lane < 2 * KT) sr = my_scale[(((long long)pg * a.Hkv + head) << a.page_shift) + place];
         };
         const auto store = [&](u4 *k, u4 *v, int b) {
+            if (loads) {
 #pragma unroll
-            for (int i = 0; i < LN; ++i) {
-                const int r = my_row + LR * i;
-                if (!loads) continue;
+                for (int i = 0; i < LN; ++i) {
+                    const int r = my_row + LR * i;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int to = r * C + ((2 * my_piece + j) ^ swizzle<C>(r));
-                    const uint2 k0 = codes4(kr[i][2 * j]), k1 = codes4(kr[i][2 * j + 1]);
-                    const uint2 v0 = codes4(vr[i][2 * j]), v1 = codes4(vr[i][2 * j + 1]);
-                    k[to] = u4{k0.x, k0.y, k1.x, k1.y};
-                    v[to] = u4{v0.x, v0.y, v1.x, v1.y};
+                    for (int j = 0; j < 2; ++j) {
+                        const int to = r * C + ((2 * my_piece + j) ^ swizzle<C>(r));
+                        const uint2 k0 = codes4(kr[i][2 * j]), k1 = codes4(kr[i][2 * j + 1]);
+                        const uint2 v0 = codes4(vr[i][2 * j]), v1 = codes4(vr[i][2 * j + 1]);
+                        k[to] = u4{k0.x, k0.y, k1.x, k1.y};
+                        v[to] = u4{v0.x, v0.y, v1.x, v1.y};
+                    }
                 }
             }
-            if (threadIdx.x < 2 * KB) ((float *)(threadIdx.x < KB ? kscale : vscale)[b])[threadIdx.x & (KB - 1)] = sr;
+            if (lane < 2 * KT) ((float *)(lane < KT ? kscale : vscale)[b])[KT * wave + lane % KT] = sr;
         };
 
         // Which of keys {0 .. 3} + 8 i + 4 hh of 32 the lane's row sees: key n0 + n of a
@@ -640,8 +639,10 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
                 }
             } else {
                 const float ks = ((const float *)kscale[b])[lane], vs = ((const float *)vscale[b])[lane];
-                const int pk = wave_max(pr::exp_above(fabsf(ks))), pv = wave_max(pr::exp_above(fabsf(vs)));
-                if (pk > all_k || pv > all_v) {
+                int pk = pr::exp_above(fabsf(ks)), pv = pr::exp_above(fabsf(vs));
+                if (__any(pk > all_k || pv > all_v)) {
+                    pk = wave_max(pk);
+                    pv = wave_max(pv);
                     raise(pk, all_v, max(all_v, pv));
                     all_k = max(all_k, pk);
                     all_v = max(all_v, pv);
@@ -745,19 +746,19 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
         // sums between registers)
         const auto walk = [&](u4 *__restrict__ k0, u4 *__restrict__ k1, u4 *__restrict__ v0, u4 *__restrict__ v1) {
             if (begin < end) {
-                pages_of(begin);
+                page_of(begin);
                 load(begin);
-                pages_of(begin + STEP);
+                page_of(begin + STEP);
                 store(k0, v0, 0);
                 load(begin + STEP);
-                pages_of(begin + 2 * STEP);
+                page_of(begin + 2 * STEP);
             }
             __syncthreads();
             const auto turn = [&](u4 *k, u4 *v, int b, int i0) {
                 // the other buffer: every wave is past the step that read it
                 store(k, v, b);
                 load(i0 + 2 * STEP);
-                pages_of(i0 + 3 * STEP);
+                page_of(i0 + 3 * STEP);
                 __syncthreads();
             };
             const auto pairs = [&](int i0, int to, auto masked) {
