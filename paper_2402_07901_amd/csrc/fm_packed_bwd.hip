@@ -102,7 +102,15 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f16v{};
     int power = O::POWERS ? info.ed >> 1 : 0;   // E
-    float delta = info.delta, up = 1.f;         // delta 2^-R and 2^(R - E), R the tile's power
+    int all = NO_POWER;                         // the tiles' so far
+    float delta = info.delta, up = 1.f;         // delta 2^-R and 2^(R - E), R what the factors are relative to
+    const auto relative = [&](int to) {
+        // (values 2^60 below E vanish in any case)
+        const int R = max(to, power - 60);
+        delta = __builtin_ldexpf(info.delta, -R);
+        up = __builtin_ldexpf(1.0f, min(R - power, 120));
+    };
+    if constexpr (O::POWERS) relative(all);
 
     const int end = a.causal ? (min(pl.first + COLS, rows) - 1) / a.group + 1 : pl.len;
     const int whole = (a.causal ? pl.first / a.group + 1 : pl.len) / (2 * TILE) * (2 * TILE);
@@ -135,19 +143,21 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
         if constexpr (O::POWERS) {
             const int b = next >> 1;
             next = p.b[keys + min(n0 + TILE + 32 * at + lane % MINE, pl.len - 1)];
-            const int top = wave_max(b);
-            if (__any(top > power)) {
-                int most = top;
-                if constexpr (decltype(masked)::value) most = max_to<MINE>(b, lane, lim - n0 - 32 * at);
+            const auto raise = [&](int most) {
                 most = max(most, power);
                 scale_down<DT>(acc, power - most);
                 power = most;
+            };
+            if constexpr (decltype(masked)::value) {
+                all = wave_max(b);
+                if (__any(all > power)) raise(max_to<MINE>(b, lane, lim - n0 - 32 * at));
+                relative(all);
+            } else if (__any(b > all)) {
+                all = max(all, wave_max(b));
+                if (__any(all > power)) raise(all);
+                relative(all);
             }
-            // (values 2^60 below E vanish in any case)
-            const int R = max(top, power - 60);
-            delta = __builtin_ldexpf(info.delta, -R);
-            up = __builtin_ldexpf(1.0f, min(R - power, 120));
-            ((float *)factors)[lane % MINE] = __builtin_ldexpf(1.0f, b - top);
+            ((float *)factors)[lane % MINE] = __builtin_ldexpf(1.0f, b - all);
         }
     };
     const auto scores = [&](const u4 *kt, const u4 *vt, int kb, f16v &s, f16v &dp) {
@@ -283,7 +293,6 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
         next = p.info[base + min(r0 + TILE + 32 * at + lane % MINE, rows - 1)];
         float X = info.m, Y = info.m * info.delta;
         if constexpr (O::POWERS) {
-            const int e = wave_max(info.e), d = GK ? wave_max(info.ed >> 1) : NO_POWER;
             const auto raise = [&](int m, int f) {
                 scale_down<DT>(dv, M - m);
                 if constexpr (GK) scale_down<DT>(dk, M - m + F - f);
@@ -294,6 +303,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
                 }
             };
             if constexpr (decltype(masked)::value) {
+                const int e = wave_max(info.e), d = GK ? wave_max(info.ed >> 1) : NO_POWER;
                 if (__any(e > M || d > F)) {
                     const int from = least - r0 - 32 * at;
                     const int m = max(M, max_from<MINE>(info.e, lane, from));
@@ -320,7 +330,8 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
                     own_values();
                     shared = true;
                 }
-                if (scalar(e) > scalar(M) || (GK && scalar(d) > scalar(F))) raise(max(M, e), GK ? max(F, d) : F);
+                if (__any(info.e > M || (GK && info.ed >> 1 > F)))
+                    raise(max(M, wave_max(info.e)), GK ? max(F, wave_max(info.ed >> 1)) : F);
                 X = __builtin_ldexpf(info.m, info.e - M);
                 Y = X * __builtin_ldexpf(info.delta, -F);
             }

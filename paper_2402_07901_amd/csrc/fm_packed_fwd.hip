@@ -383,20 +383,20 @@ __global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArg
         odd |= __ballot(next & 1);
         next = p.b[keys + min(n0 + TILE + 32 * at + lane % MINE, pl.len - 1)];
         if constexpr (O::POWERS) {
-            const int top = wave_max(b);
-            if (__any(top > power)) {
-                int most = top;
-                if constexpr (decltype(masked)::value) most = max_to<MINE>(b, lane, lim - n0 - 32 * at);
+            const auto raise = [&](int most) {
                 most = max(most, power);
                 const float f = __builtin_ldexpf(1.0f, max(power - most, -300));
 #pragma unroll
                 for (int d = 0; d < DT; ++d) acc[d] *= f;
                 power = most;
-            }
+            };
             if constexpr (decltype(masked)::value) {
+                const int top = wave_max(b);
+                if (__any(top > power)) raise(max_to<MINE>(b, lane, lim - n0 - 32 * at));
                 up = __builtin_ldexpf(1.0f, min(top - power, 126));
                 ((float *)factors[wave])[lane % MINE] = __builtin_ldexpf(1.0f, b - top);
             } else {
+                if (__any(b > power)) raise(wave_max(b));
                 ((_Float16 *)factors[wave])[lane % MINE] = (_Float16)__builtin_ldexpf(1.0f, b - power);
             }
         }
