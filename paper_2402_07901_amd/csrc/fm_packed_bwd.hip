@@ -443,7 +443,7 @@ template <typename T, int D> static hipError_t launch_bwd(const PackedArgs &a, v
     if (!grid_fits(blocks, THREADS)) return hipErrorInvalidConfiguration;
     const hipError_t e = prep<T, E>(a, p, D, 1, st);
     if (e != hipSuccess) return e;
-    if constexpr (Cut<E, D, 4>::FITS && D < 128) {
+    if constexpr (Cut<E, D, 4>::FITS) {
         if (p.cols == 32) {
             if (a.p == 2) bwd_kernel<T, D, 2, 4><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);
             else bwd_kernel<T, D, 1, 4><<<(unsigned)blocks, THREADS, 0, st>>>(a, p);

@@ -200,11 +200,13 @@ static size_t up(size_t n) { return (n + 255) / 256 * 256; }
 // against 58; 4 heads of 32, 260 53 against 86 and 140 against 166; one key head of 64
 // for 8, 65 places of keys 626 against 1402; float32 4 heads of 32, 124 40 against 84
 // and 80 against 161, 12 of 64, 432 310 against 355 and 912 against 855.  At D = 128 the
-// tiles fill a CU's LDS: 8 heads for 32, 104 26 against 21; 12 for 12, 84 28 against 29.
+// tiles fill a CU's LDS: 8 heads for 32, 104 26 against 21; 12 for 12, 84 28 against 29;
+// backward, places of keys, one head for 8, 33 439 against 907; 8 for 32, 56 90 against
+// 117; 4 for 4, 68 69 against 80; 12 for 12, 84 64 against 48; 8 for 32, 136 320 against 280.
 bool small_call(int S, int T, int Hq, int Hkv, int D, int is_bf16, int backward)
 {
-    if (D == 128 && (backward || !is_bf16)) return false;   // LDS, registers
-    if (backward) return places(S, T, 1, 128) * Hkv < 320;
+    if (D == 128 && !is_bf16) return false;   // LDS
+    if (backward) return places(S, T, 1, 128) * Hkv < (D == 128 ? 80 : 320);
     return places(S, T, Hq / Hkv, 128) * Hkv < (D == 128 ? 96 : 448);
 }
 

@@ -17,8 +17,8 @@
 // two bf16 parts (float32: three) against the codes, which bf16 holds exactly.
 //
 // Many rows (chunks).  The matrix pipe and the instructions beside it bound it: four
-// chunks of up to 2048 tokens over up to 8192, 32 heads to 8 of 128, 580 to 600 us, 590
-// TFLOP/s.  There the few rows' scheme took 766: each wave converted every code for
+// chunks of up to 2048 tokens over up to 8192, 32 heads to 8 of 128, 465 to 545 us, 650
+// TFLOP/s and more (cards differ).  There the few rows' scheme took 766: each wave converted every code for
 // itself, and weights entered as two parts.  So codes become fp16 once a workgroup, on
 // their way into LDS, and one fp16 product (11 bits) does for weights and scores.
 #include <hip/hip_runtime.h>
@@ -480,7 +480,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 && D == 128 ? 1 : 2) void m
     const int8_t *kc = (const int8_t *)a.k + head * a.cache.head, *vc = (const int8_t *)a.v + head * a.cache.head;
     const int32_t *table = a.table + (size_t)s * a.table_cols;
     // A wave loads one key tile of a step, whose page is a scalar: a lane's place in it
-    // does not change.
+    // does not change.  (Places and pages by lane, for 64 rows shared out evenly: 603 us
+    // where this takes 541.)
     const int my_row = KT * wave + lane / LP, my_piece = lane % LP;
     const bool loads = KT * LP >= 64 || lane < KT * LP;
     const int token = (int)a.cache.token, my_at = lane / LP * token + 16 * my_piece;
