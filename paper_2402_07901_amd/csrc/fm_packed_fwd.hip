@@ -280,7 +280,7 @@ __global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArg
     using W = Cut<E, D, WK>;
     constexpr int DT = O::DT, TILE = W::TILE, MINE = W::MINE, COLS = W::COLS;
     __shared__ u4 x0[TILE * O::C], x1[TILE * O::C], y0[TILE * O::C], y1[TILE * O::C];
-    __shared__ f4 factors[THREADS / 64][MINE / 4];   // (whole tiles: halves)
+    __shared__ f4 factors[THREADS / 64][MINE / 4];   // whole tiles: halves; cut ones: the keys' powers
     __shared__ int wave_powers[THREADS / 64][64];
     __shared__ float wave_sums[THREADS / 64][64];
 
@@ -323,7 +323,7 @@ __global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArg
     for (int d = 0; d < DT; ++d) acc[d] = f16v{};
     float g = 0.f;          // second order: of 2 w = (1 + tau s)^2 + 1
     int power = NO_POWER;   // of acc: the largest of the values that the row has seen
-    float up = 1.f;         // 2^-power times the tile's largest
+    float down = 1.f;       // 2^-power
 
     const int end = a.causal ? (min(pl.first + COLS, rows) - 1) / a.group + 1 : pl.len;   // keys that some row sees
     // keys before `whole` are seen by all rows, from `none` on by none of the wave's
@@ -356,9 +356,12 @@ __global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArg
             for (int j = 0; j < 4; ++j) {
                 pr::h2 f[2];
                 if constexpr (decltype(masked)::value) {
-                    f4 x = factors[wave][8 * kb + 2 * j + hh];
+                    // 2^b 2^-power a row: one factor for all of them times one of the row's own
+                    // would leave float32's range between a row's values and an unseen key's
+                    const i4 b = ((const i4 *)factors[wave])[8 * kb + 2 * j + hh];
+                    float x[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = 8 * j + i <= left ? x[i] * up : 0.f;
+                    for (int i = 0; i < 4; ++i) x[i] = 8 * j + i <= left ? __builtin_ldexpf(down, b[i]) : 0.f;
                     f[0] = pr::cvt2(x[0], x[1]);
                     f[1] = pr::cvt2(x[2], x[3]);
                 } else {
@@ -393,10 +396,9 @@ __global__ __launch_bounds__(THREADS, WK == 1 ? 2 : 1) void fwd_kernel(PackedArg
                 power = most;
             };
             if constexpr (decltype(masked)::value) {
-                const int top = wave_max(b);
-                if (__any(top > power)) raise(max_to<MINE>(b, lane, lim - n0 - 32 * at));
-                up = __builtin_ldexpf(1.0f, min(top - power, 126));
-                ((float *)factors[wave])[lane % MINE] = __builtin_ldexpf(1.0f, b - top);
+                if (__any(wave_max(b) > power)) raise(max_to<MINE>(b, lane, lim - n0 - 32 * at));
+                down = power > NO_POWER ? __builtin_ldexpf(1.0f, -power) : 1.f;
+                ((int *)factors[wave])[lane % MINE] = b;
             } else {
                 if (__any(b > power)) raise(wave_max(b));
                 ((_Float16 *)factors[wave])[lane % MINE] = (_Float16)__builtin_ldexpf(1.0f, b - power);

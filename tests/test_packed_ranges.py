@@ -1,0 +1,63 @@
+"""GPU tests of the packed attention's powers of two (bf16 calls), against float64:
+rows beside values of any size that they do not see."""
+import numpy as np
+import pytest
+
+from paper_2402_07901_amd import fastmax as fm
+
+import serve_util as su
+from gpu_util import say
+from packed_util import OUT, Head, Packed
+
+pytestmark = pytest.mark.gpu
+LARGEST = (2.0 - 2.0 ** -7) * 2.0 ** 127                       # of bf16
+HEADS = [(4, 2), (120, 120)]                                   # 32 columns to a workgroup, 128
+SIZES = [(2, 1.0), (2, 0.02), (1, 0.02), (2, 2.0 ** -60)]      # p, the values' deviation
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    fm.lib()
+    yield
+    torch.cuda.synchronize()
+
+
+def tau_of(p, D):
+    return 1.0 if p == 2 else 1.0 / D
+
+
+def heads_of(x, a, b, p, causal=True):
+    """(key head, query heads, Head) of the tokens a .. b - 1 as a sequence, for the
+    first two key heads."""
+    for h in range(2):
+        hs = slice(h * x.group, (h + 1) * x.group)
+        yield h, hs, Head(su.np64(x.q[a:b, hs]), su.np64(x.k[a:b, h]), su.np64(x.v[a:b, h]), p,
+                          tau_of(p, x.D), causal, x.dtype)
+
+
+@pytest.mark.parametrize("D", [16, 32, 64, 128])
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("p,size", SIZES)
+def test_outputs_beside_the_largest_value(D, heads, p, size):
+    """A token's values are the largest that bf16 has: O of the rows before it is held
+    to the bounds of the sequence without it, G of all rows and O of the ones that see
+    it to the whole sequence's."""
+    label = f"packed O beside the largest, D={D} p={p} H={heads} size={size}"
+    say(label)
+    n = 400
+    for a in (70, 333):
+        x = Packed([n], *heads, D, "bf16", seed=a, size=size)
+        x.v[a] = LARGEST
+        x.v[a, :, ::2] *= -1
+        out, g = fm.fastmax_packed_fwd(x.q, x.k, x.v, x.starts, p=p, causal=True, scale=tau_of(p, D))
+        for h, hs, head in heads_of(x, 0, n, p):
+            O, eO, G, eG = head.forward()
+            su.check(g[:, hs], G, 1.01 * eG, (label, a, "G", h))
+            if p == 2:      # (weights of both signs: an O may be larger than the values)
+                su.check(out[a:, hs], O[a:], OUT["bf16"] * np.abs(O[a:]) + 1.01 * eO[a:], (label, a, "later", h))
+        for h, hs, head in heads_of(x, 0, a, p):
+            O, eO, _, _ = head.forward()
+            su.check(out[:a, hs], O, OUT["bf16"] * np.abs(O) + 1.01 * eO, (label, a, "O", h))
