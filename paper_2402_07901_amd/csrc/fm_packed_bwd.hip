@@ -103,7 +103,9 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
     for (int d = 0; d < DT; ++d) acc[d] = f16v{};
     int power = O::POWERS ? info.ed >> 1 : 0;   // E
     int all = NO_POWER;                         // the tiles' so far
-    float delta = info.delta, up = 1.f;         // delta 2^-R and 2^(R - E), R what the factors are relative to
+    // whole tiles: delta 2^-R and 2^(R - E), R what the factors are relative to; cut ones:
+    // delta 2^-E and 2^-E
+    float delta = info.delta, up = 1.f;
     const auto relative = [&](int to) {
         // (values 2^60 below E vanish in any case)
         const int R = max(to, power - 60);
@@ -124,15 +126,24 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
         O::turn(k, kt, at + kb, lane);
         float w[16];
         const int left = lim - n1 - 4 * hh;
-        const float tau_up = tau * up;
+        // (in a cut tile a row's own factors: 2^b 2^-E has no part that an unseen key's
+        // power could take out of float32's range)
+        constexpr bool OWN = O::POWERS && decltype(masked)::value;
+        const float t1 = OWN ? 1.f : up, tau1 = OWN ? tau : tau * up;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             f4 f;
-            if constexpr (O::POWERS) f = factors[8 * kb + 2 * j + hh];
+            if constexpr (OWN) {
+                const i4 b = ((const i4 *)factors)[8 * kb + 2 * j + hh];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f[i] = __builtin_ldexpf(up, b[i]);
+            } else if constexpr (O::POWERS) {
+                f = factors[8 * kb + 2 * j + hh];
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float d = O::POWERS ? fmaf(dp[4 * j + i], f[i], -delta) : dp[4 * j + i] - delta;
-                float x = P == 2 ? fmaf(s[4 * j + i], tau_up, up) * d : O::POWERS ? up * d : d;
+                float x = P == 2 ? fmaf(s[4 * j + i], tau1, t1) * d : O::POWERS ? t1 * d : d;
                 if constexpr (decltype(masked)::value) x = 8 * j + i <= left ? x : 0.f;
                 w[4 * j + i] = x;
             }
@@ -149,15 +160,18 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
                 power = most;
             };
             if constexpr (decltype(masked)::value) {
-                all = wave_max(b);
-                if (__any(all > power)) raise(max_to<MINE>(b, lane, lim - n0 - 32 * at));
-                relative(all);
-            } else if (__any(b > all)) {
-                all = max(all, wave_max(b));
-                if (__any(all > power)) raise(all);
-                relative(all);
+                if (__any(wave_max(b) > power)) raise(max_to<MINE>(b, lane, lim - n0 - 32 * at));
+                up = power > NO_POWER ? __builtin_ldexpf(1.0f, -power) : 1.f;
+                delta = power > NO_POWER ? __builtin_ldexpf(info.delta, -power) : info.delta;
+                ((int *)factors)[lane % MINE] = b;
+            } else {
+                if (__any(b > all)) {
+                    all = max(all, wave_max(b));
+                    if (__any(all > power)) raise(all);
+                    relative(all);
+                }
+                ((float *)factors)[lane % MINE] = __builtin_ldexpf(1.0f, b - all);
             }
-            ((float *)factors)[lane % MINE] = __builtin_ldexpf(1.0f, b - all);
         }
     };
     const auto scores = [&](const u4 *kt, const u4 *vt, int kb, f16v &s, f16v &dp) {

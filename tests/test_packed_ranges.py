@@ -61,3 +61,36 @@ def test_outputs_beside_the_largest_value(D, heads, p, size):
         for h, hs, head in heads_of(x, 0, a, p):
             O, eO, _, _ = head.forward()
             su.check(out[:a, hs], O, OUT["bf16"] * np.abs(O) + 1.01 * eO, (label, a, "O", h))
+
+
+def given(x, a, b, p, causal=True):
+    """O and G of the tokens a .. b - 1 as a sequence: the definition's for the first
+    two key heads, the call's for the others."""
+    import torch
+    starts = torch.tensor([a, b], dtype=torch.int32, device="cuda")
+    out, g = fm.fastmax_packed_fwd(x.q, x.k, x.v, starts, p=p, causal=causal, scale=tau_of(p, x.D))
+    for _, hs, head in heads_of(x, a, b, p, causal):
+        O, _, G, _ = head.forward()
+        out[a:b, hs], g[a:b, hs] = torch.from_numpy(O).cuda().to(x.tdt), torch.from_numpy(G).cuda().float()
+    return out, g
+
+
+@pytest.mark.parametrize("D", [16, 32, 64, 128])
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("p,size", SIZES)
+def test_gradients_beside_the_largest_value(D, heads, p, size):
+    """The same for dq of the rows before that token."""
+    label = f"packed dq beside the largest, D={D} p={p} H={heads} size={size}"
+    say(label)
+    n = 400
+    for a in (70, 333):
+        x = Packed([n], *heads, D, "bf16", seed=a, size=size)
+        x.v[a] = LARGEST
+        x.v[a, :, ::2] *= -1
+        out, g = given(x, 0, n, p)
+        dq = fm.fastmax_packed_bwd(x.q, x.k, x.v, x.starts, out, x.dout, g, p=p, causal=True,
+                                   scale=tau_of(p, D))[0]
+        do = su.np64(x.dout)
+        for h, hs, head in heads_of(x, 0, a, p):
+            want, bound = head.backward(do[:a, hs], OUT["bf16"])[0]
+            su.check(dq[:a, hs], want, OUT["bf16"] * (np.abs(want) + bound) + 1.01 * bound, (label, a, h))
