@@ -447,7 +447,7 @@ __device__ __forceinline__ void store_row(T *row, const f16v *acc, int hh)
 // and, for the backward, per row (key head, token, head in its group):
 struct RowInfo {
     float m;        // 1 / G times 2^a is m 2^e, a the power of dO; float32: 1 / G
-    int e;
+    int e;          // NO_POWER: dO is zeros
     float delta;    // dO.O 2^-a
     int ed;         // twice the least power above it, + 1 if dO has what is not finite
 };

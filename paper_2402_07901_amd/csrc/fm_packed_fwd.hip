@@ -177,12 +177,14 @@ __global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<type
         delta = pr::group_sum<L>(delta);
         if (ok && c == 0) {
             const float u = 1.0f / a.g[row];
-            RowInfo x{u, 0, delta, e & 1};
+            // (a row of zeros, or one whose G is not finite, has no power: it takes none
+            // of the others' bits)
+            RowInfo x{u, NO_POWER, delta, e & 1};
             if constexpr (H) {
                 const int eu = pr::exp_above(fabsf(u));
                 if (eu != pr::NO_EXP) {
                     x.m = __builtin_ldexpf(u, -eu);
-                    x.e = eu + shift;
+                    if (e >> 1 != NO_POWER) x.e = eu + shift;
                 }
                 x.ed = 2 * pr::exp_above(fabsf(delta)) + (e & 1);
             }

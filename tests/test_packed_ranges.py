@@ -1,5 +1,7 @@
 """GPU tests of the packed attention's powers of two (bf16 calls), against float64:
 rows beside values of any size that they do not see."""
+import copy
+
 import numpy as np
 import pytest
 
@@ -94,3 +96,46 @@ def test_gradients_beside_the_largest_value(D, heads, p, size):
         for h, hs, head in heads_of(x, 0, a, p):
             want, bound = head.backward(do[:a, hs], OUT["bf16"])[0]
             su.check(dq[:a, hs], want, OUT["bf16"] * (np.abs(want) + bound) + 1.01 * bound, (label, a, h))
+
+
+def rows_only(head, live):
+    """The rows `live` of a Head: what the others add to dk and dv is zero."""
+    some = copy.copy(head)
+    for name in ("q", "rq", "see", "es", "t", "et", "w", "ew", "G", "eG"):
+        x = getattr(head, name)
+        setattr(some, name, x[live] if len(x) == len(live) else x)
+    return some
+
+
+@pytest.mark.parametrize("D", [16, 32, 64, 128])
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("power", [0, -16, -24, -30, -90])
+def test_gradients_beside_rows_of_zeros(D, heads, causal, power):
+    """Tokens without a loss have rows of zeros in dout, the others gradients of any
+    size (a mean over many tokens): the zeros are without effect.  The first half of a
+    sequence and then every third row, one sequence of nothing else and one of
+    nothing but gradients."""
+    import torch
+    label = f"packed, zero rows of dout, D={D} H={heads} causal={causal} 2^{power}"
+    say(label)
+    x = Packed([300, 70, 40], *heads, D, "bf16", seed=D)
+    zero = torch.zeros(x.T, dtype=torch.bool, device="cuda")
+    zero[:150] = zero[:300:3] = zero[300:370] = True
+    x.dout *= 2.0 ** power
+    x.dout[zero] = 0
+    out, g = fm.fastmax_packed_fwd(x.q, x.k, x.v, x.starts, causal=causal)
+    for a, b in zip(x.start, x.start[1:]):
+        here, gh = given(x, int(a), int(b), 2, causal)
+        out[a:b], g[a:b] = here[a:b], gh[a:b]
+    dq, dk, dv = fm.fastmax_packed_bwd(x.q, x.k, x.v, x.starts, out, x.dout, g, causal=causal)
+    assert (dq[zero] == 0).all() and (dk[300:370] == 0).all() and (dv[300:370] == 0).all()
+    do, live = su.np64(x.dout), ~zero.cpu().numpy()
+    for a, b in ((0, 300), (370, 410)):
+        for h, hs, head in heads_of(x, a, b, 2, causal):
+            keep = live[a:b]
+            ref = rows_only(head, keep).backward(do[a:b, hs][keep], OUT["bf16"])
+            gots = (dq[a:b, hs][~zero[a:b]], dk[a:b, h], dv[a:b, h])
+            for name, got, (want, bound) in zip(("dq", "dk", "dv"), gots, ref):
+                tol = OUT["bf16"] * (np.abs(want) + bound) + 1.01 * bound
+                su.check(got, want, tol, (label, name, a, h))
