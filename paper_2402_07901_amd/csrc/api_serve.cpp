@@ -214,6 +214,10 @@ size_t paged_bytes(bool q8, int S, int T, int Hq, int Hkv, int D, int max_q, int
     return fm::paged_workspace(plan_of(q8, S, Hq, Hkv, D, max_q, max_len, window, sinks, dt), T, Hq, D);
 }
 
+// Sequences and rows of a packed call (a row's number is an int, with room for a
+// workgroup's beyond the last).
+bool packed_fits(int S, int T, int Hq) { return S >= 1 && S <= (1 << 20) && (long long)T * Hq <= 1 << 30; }
+
 // The packed attention's arguments (backward: with dout, dq, dk, dv).
 int check_packed(fm::PackedArgs *a, const void *q, const void *k, const void *v, const fastmax_strides_t *strides,
                  const int32_t *starts, const void *out, const float *g, int S, int T, int Hq, int Hkv, int D, int p,
@@ -221,7 +225,7 @@ int check_packed(fm::PackedArgs *a, const void *q, const void *k, const void *v,
 {
     int rc = check_sizes(T, Hq, Hkv, D, dt);
     if (rc != FASTMAX_OK) return rc;
-    if (S < 1 || S > (1 << 20) || (long long)T * Hq > INT_MAX / 2) return FASTMAX_EINVAL;
+    if (!packed_fits(S, T, Hq)) return FASTMAX_EINVAL;
     if ((p != 1 && p != 2) || (causal != 0 && causal != 1)) return FASTMAX_EINVAL;
     if (!(qk_scale > 0.0f && qk_scale <= 1.0f)) return FASTMAX_EINVAL;
     if ((rc = check_rows(strides, 3, 1, T, Hq, Hkv, D, dt, false, &a->qs, &a->ks, &a->vs)) != FASTMAX_OK) return rc;
@@ -399,7 +403,7 @@ int fastmax_paged_fwd_q8(const void *q, const fastmax_strides_t *q_strides, cons
 size_t fastmax_packed_workspace_bytes(int S, int T, int Hq, int Hkv, int D, fastmax_dtype_t dt_arg, int backward)
 {
     const int dt = dt_bits(&dt_arg);
-    if (check_sizes(T, Hq, Hkv, D, dt) != FASTMAX_OK || S < 1 || S > (1 << 20) || (long long)T * Hq > INT_MAX / 2) return 0;
+    if (check_sizes(T, Hq, Hkv, D, dt) != FASTMAX_OK || !packed_fits(S, T, Hq)) return 0;
     return fm::packed_workspace(S, T, Hq, Hkv, D, dt == FASTMAX_BF16, backward);
 }
 

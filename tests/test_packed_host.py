@@ -39,6 +39,21 @@ def test_sizes(kw, code):
     assert bwd([0] + [A] * 9, **kw) == code
 
 
+@pytest.mark.parametrize("Hq,Hkv", [(4, 2), (1, 1), (64, 1)])
+def test_most_rows_and_sequences(Hq, Hkv):
+    """T * Hq = 2^30 and S = 2^20 pass the checks (a NULL q ends the calls), one more
+    does not; the size call agrees."""
+    most = (1 << 30) // Hq
+    for kw, ok in ((dict(T=most), True), (dict(T=most + 1), False), (dict(S=1 << 20), True),
+                   (dict(S=(1 << 20) + 1), False), (dict(T=most, S=1 << 20), True)):
+        kw = dict(Hq=Hq, Hkv=Hkv, **kw)
+        assert fwd([0] + [A] * 4, **kw) == (fm.ENULL if ok else fm.EINVAL)
+        assert bwd([0] + [A] * 9, **kw) == (fm.ENULL if ok else fm.EINVAL)
+        for backward in (False, True):
+            need = fm.packed_workspace_bytes(kw.get("S", 2), kw.get("T", 8), Hq, Hkv, 64, fm.BF16, backward)
+            assert (need > 0) == ok
+
+
 def test_pointers():
     for call, n in ((fwd, 5), (bwd, 10)):
         for i in range(n):
