@@ -514,6 +514,12 @@ def _rope_of(q, tokens, pos, cos, sin, wq, wk, eps, sections, interleaved):
     return Rope(c, s, p, rows, rot, axes, parts, 1 if interleaved else 0, gq, gk, eps)
 
 
+def _of(name, given, n):
+    """Checks that the caller's outputs, if there are any, are n tensors."""
+    if given is not None and len(given) != n:
+        raise ValueError(f"{name} must be {n} tensors, got {len(given)}")
+
+
 def _on_gpu(q, dims, what):
     if q.dim() != dims:
         raise ValueError(f"q must be {what}, got shape {tuple(q.shape)}")
@@ -577,6 +583,7 @@ def fastmax_rope_fwd(q, k, v, pos, cos, sin, wq=None, wk=None, eps=1e-6, section
     int32 [B, N] or [B, N, axes] with ``sections`` pairs per axis; all None: no
     rotation), key and value heads repeated.  Returns three contiguous
     [B, Hq, N, D] tensors (``out``: the same, the caller's)."""
+    _of("out", out, 3)
     _on_gpu(q, 4, "[B, N, Hq, D]")
     B, N, Hq, D = q.shape
     dtype, dev, dt = q.dtype, q.get_device(), _dtype_code(q)
@@ -608,6 +615,7 @@ def fastmax_rope_bwd(q, k, gq, gk, gv, pos, cos, sin, wq=None, wk=None, eps=1e-6
     norm only).  Returns (dq, dk, dv, dwq, dwk), dq [B, N, Hq, D], dk and dv
     [B, N, Hkv, D] (``out``: these three, the caller's, strided as they like),
     dwq and dwk float32 [D] (None without a norm)."""
+    _of("out", out, 3)
     _on_gpu(q, 4, "[B, N, Hq, D]")
     B, N, Hq, D = q.shape
     dtype, dev, dt = q.dtype, q.get_device(), _dtype_code(q)
@@ -773,6 +781,7 @@ def fastmax_cache_read_q8(k_cache, v_cache, k_scale, v_scale, slots, dtype=None,
     ``dtype`` (float32 or bfloat16, the default; ``out``: the same two, the
     caller's)."""
     torch = _torch()
+    _of("out", out, 2)
     _on_gpu(k_cache, 4, "[pages, Hkv, page, D]")
     _, Hkv, _, D = k_cache.shape
     dev = k_cache.get_device()
@@ -887,6 +896,7 @@ def fastmax_packed_bwd(q, k, v, starts, out, dout, g, p=2, causal=False, grads=N
     """Backward of fastmax_packed_fwd from its outputs: (dq [T, Hq, D], dk and dv
     [T, Hkv, D]) of sum(dout * O); ``grads``: the same three, the caller's, strided
     as they like.  Rows of no sequence stay as they are."""
+    _of("grads", grads, 3)
     S, T, Hq, Hkv, D, dt, st = _packed_of(q, k, v, starts)
     torch, dtype, dev = _torch(), q.dtype, q.get_device()
     _whole("out", out, (T, Hq, D), dtype, dev, q)
