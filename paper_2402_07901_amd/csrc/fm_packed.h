@@ -55,6 +55,7 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 constexpr int THREADS = 256;
 constexpr int WAIT_LOADS = 0x0f70;         // vmcnt(0), the other counters at their most
 constexpr int NO_POWER = -1000;            // of a row of zeros
+constexpr int ROOM = 8;                    // D values of up to 2^128 add up to less than 2^(128 + ROOM)
 
 template <typename T> struct plane_of { typedef float type; };
 template <> struct plane_of<bf16_t> { typedef _Float16 type; };
@@ -448,7 +449,7 @@ __device__ __forceinline__ void store_row(T *row, const f16v *acc, int hh)
 struct RowInfo {
     float m;        // 1 / G times 2^a is m 2^e, a the power of dO; float32: 1 / G
     int e;          // NO_POWER: dO is zeros
-    float delta;    // dO.O 2^-a
+    float delta;    // dO.O 2^-(a + ROOM); float32: dO.O
     int ed;         // twice the least power above it, + 1 if dO has what is not finite
 };
 template <typename E> struct Planes {

@@ -109,7 +109,7 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
     const auto relative = [&](int to) {
         // (values 2^60 below E vanish in any case)
         const int R = max(to, power - 60);
-        delta = __builtin_ldexpf(info.delta, -R);
+        delta = __builtin_ldexpf(info.delta, ROOM - R);
         up = __builtin_ldexpf(1.0f, min(R - power, 120));
     };
     if constexpr (O::POWERS) relative(all);
@@ -162,7 +162,7 @@ __device__ __forceinline__ void rows_block(const PackedArgs &a, const Planes<typ
             if constexpr (decltype(masked)::value) {
                 if (__any(wave_max(b) > power)) raise(max_to<MINE>(b, lane, lim - n0 - 32 * at));
                 up = power > NO_POWER ? __builtin_ldexpf(1.0f, -power) : 1.f;
-                delta = power > NO_POWER ? __builtin_ldexpf(info.delta, -power) : info.delta;
+                delta = power > NO_POWER ? __builtin_ldexpf(info.delta, ROOM - power) : info.delta;
                 ((int *)factors)[lane % MINE] = b;
             } else {
                 if (__any(b > all)) {
@@ -327,7 +327,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
                 cx = __builtin_ldexpf(1.0f, min(e - M, 126));
                 cy = __builtin_ldexpf(1.0f, min(d - F, 126));
                 X = __builtin_ldexpf(info.m, info.e - e);
-                Y = X * __builtin_ldexpf(info.delta, -d);
+                Y = X * __builtin_ldexpf(info.delta, ROOM - d);
             } else {
                 if (!shared) {
                     // the least of the columns', which keeps all their bits (within
@@ -347,7 +347,7 @@ __device__ __forceinline__ void keys_block(const PackedArgs &a, const Planes<typ
                 if (__any(info.e > M || (GK && info.ed >> 1 > F)))
                     raise(max(M, wave_max(info.e)), GK ? max(F, wave_max(info.ed >> 1)) : F);
                 X = __builtin_ldexpf(info.m, info.e - M);
-                Y = X * __builtin_ldexpf(info.delta, -F);
+                Y = X * __builtin_ldexpf(info.delta, ROOM - F);
             }
         }
         // rows past the last weigh nothing

@@ -173,7 +173,8 @@ __global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<type
         const int e = scaled(rd, p.oh + at * D, true), shift = e >> 1 == NO_POWER ? 0 : e >> 1;
         float delta = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) delta = fmaf(__builtin_ldexpf(rd.get(i), -shift), ro.get(i), delta);
+        for (int i = 0; i < 8; ++i)
+            delta = fmaf(__builtin_ldexpf(rd.get(i), -shift), H ? __builtin_ldexpf(ro.get(i), -ROOM) : ro.get(i), delta);
         delta = pr::group_sum<L>(delta);
         if (ok && c == 0) {
             const float u = 1.0f / a.g[row];
@@ -186,7 +187,8 @@ __global__ __launch_bounds__(THREADS) void prep_kernel(PackedArgs a, Planes<type
                     x.m = __builtin_ldexpf(u, -eu);
                     if (e >> 1 != NO_POWER) x.e = eu + shift;
                 }
-                x.ed = 2 * pr::exp_above(fabsf(delta)) + (e & 1);
+                const int d = pr::exp_above(fabsf(delta));
+                x.ed = 2 * (d == pr::NO_EXP ? NO_POWER : d + ROOM) + (e & 1);
             }
             p.info[at] = x;
             p.rq[at] = r;

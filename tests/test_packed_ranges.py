@@ -139,3 +139,29 @@ def test_gradients_beside_rows_of_zeros(D, heads, causal, power):
             for name, got, (want, bound) in zip(("dq", "dk", "dv"), gots, ref):
                 tol = OUT["bf16"] * (np.abs(want) + bound) + 1.01 * bound
                 su.check(got, want, tol, (label, name, a, h))
+
+
+@pytest.mark.parametrize("D", [16, 32, 64, 128])
+@pytest.mark.parametrize("heads", HEADS)
+@pytest.mark.parametrize("causal", [True, False])
+def test_gradients_of_the_largest_values(D, heads, causal):
+    """Values up to bf16's largest, dout along them and small enough for gradients in
+    range: dO.O of a row passes float32's range in dO's own power."""
+    import torch
+    label = f"packed, largest values, D={D} H={heads} causal={causal}"
+    say(label)
+    x = Packed([1, 2, 150, 40], *heads, D, "bf16", seed=D)
+    x.v.copy_((x.v.float() * 2.0 ** 126).clamp(-LARGEST, LARGEST))
+    x.dout.copy_((x.dout.abs() * 2.0 ** -30) * x.v.sign().repeat_interleave(x.group, 1))
+    out, g = fm.fastmax_packed_fwd(x.q, x.k, x.v, x.starts, causal=causal)
+    spans = [(int(a), int(b)) for a, b in zip(x.start, x.start[1:])]
+    for a, b in spans:
+        here, gh = given(x, a, b, 2, causal)
+        out[a:b], g[a:b] = here[a:b], gh[a:b]
+    dq, dk, dv = fm.fastmax_packed_bwd(x.q, x.k, x.v, x.starts, out, x.dout, g, causal=causal)
+    do = su.np64(x.dout)
+    for a, b in spans:
+        for h, hs, head in heads_of(x, a, b, 2, causal):
+            ref = head.backward(do[a:b, hs], OUT["bf16"])
+            for name, got, (want, bound) in zip(("dq", "dk", "dv"), (dq[a:b, hs], dk[a:b, h], dv[a:b, h]), ref):
+                su.check(got, want, OUT["bf16"] * (np.abs(want) + bound) + 1.01 * bound, (label, name, a, h))
