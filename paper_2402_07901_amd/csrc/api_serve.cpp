@@ -167,7 +167,7 @@ fm::PagedPlan plan_of(bool q8, int S, int Hq, int Hkv, int D, int max_q, int max
 {
     const int wide = window && window < NO_WINDOW ? window : NO_WINDOW;
     const int bf16 = dt == FASTMAX_BF16;
-    if (q8) return fm::paged_q8_plan(S, Hq, Hkv, D, bf16, max_q, max_len, wide, sinks);
+    if (q8) return fm::paged_q8_plan(S, Hq, Hkv, D, max_q, max_len, wide, sinks);
     return fm::paged_plan(S, Hq, Hkv, D, bf16, max_q, max_len, wide, sinks, !bf16 && D == 128 ? 32 : 64);
 }
 

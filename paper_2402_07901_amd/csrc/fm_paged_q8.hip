@@ -869,9 +869,21 @@ template <typename T> hipError_t launch_d(const PagedArgs &a, const PagedPlan &p
 
 }  // namespace
 
-PagedPlan paged_q8_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int max_len, int window, int sinks)
+// The plan is the one of a bf16 cache, whatever the type of q: none of its own has been
+// fitted.  Where chunks change kernels, us of the few rows' against many_kernel, 8 sequences
+// of 4096 keys, 8 key heads of 4 query heads, in graphs:
+//              32 rows            64 rows            128 rows
+//   bf16   32  15 29              22 29              32 31
+//          64  19 31              27 32              38 35
+//         128  26 43              33 45              59 50
+//   f32    32  16 30              24 31              37 34
+//          64  21 36              41 37              62 43
+//         128  37 67              51 70              94 80
+// so that many_kernel, which takes over past 32 rows at D = 64 and 128 and past 64 at
+// D = 32, comes too early at 64 rows: bf16 5 us at D = 64 and 12 at D = 128, float32 19 at
+// D = 128.
+PagedPlan paged_q8_plan(int S, int Hq, int Hkv, int D, int max_q, int max_len, int window, int sinks)
 {
-    (void)is_bf16;
     return paged_plan(S, Hq, Hkv, D, 1, max_q, max_len, window, sinks, D == 128 ? 32 : 64);
 }
 

@@ -94,7 +94,7 @@ hipError_t paged_fwd(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf
 // Adds the splits' sums of a call (part: its workspace).
 hipError_t paged_join(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, const float *part, hipStream_t st);
 // The same attention over a cache of 8-bit rows (fm_paged_q8.hip).
-PagedPlan paged_q8_plan(int S, int Hq, int Hkv, int D, int is_bf16, int max_q, int max_len, int window, int sinks);
+PagedPlan paged_q8_plan(int S, int Hq, int Hkv, int D, int max_q, int max_len, int window, int sinks);
 hipError_t paged_q8_fwd(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, void *ws, hipStream_t st);
 constexpr int CHUNK_ROWS = 128;    // rows of a workgroup of the chunk kernel
 hipError_t paged_chunk(const PagedArgs &a, const PagedPlan &plan, int D, int is_bf16, float *part,
