@@ -439,7 +439,7 @@ int fastmax_cache_append(const void *q, const void *k, const void *v,
  * read.  A row that sees a key whose entry is not a page is NaN, and so is
  * every row with a key of a sequence whose lens[s] is more than table_cols
  * pages hold.
- * table_cols * page_size <= 2^30, S <= 65535.
+ * table_cols * page_size <= 2^30, S <= 65535, T * Hq < 2^30.
  */
 size_t fastmax_paged_workspace_bytes(int S, int T, int Hq, int Hkv, int D, int max_q, int max_len,
                                      int window, int sinks, fastmax_dtype_t dt);

@@ -16,7 +16,8 @@
 // the weights, relative to the largest so far: a wave that meets a larger one scales
 // its sums down.  Where every column sees the whole tile, one power serves the wave;
 // in the tiles that the mask cuts every column (lane) has its own, of what it sees: a
-// row keeps its bits beside later tokens of any size.  32x32x16 MFMA: one 16-byte LDS
+// row keeps its bits beside later tokens of any size (O and dq; dk and dv: of dO's rows up
+// to 2^40 larger).  32x32x16 MFMA: one 16-byte LDS
 // read per lane and 16 channels for scores, the transposing read for X^T.
 // float32 calls: float32 MFMA (32x32x2), operands in full, no powers.
 //

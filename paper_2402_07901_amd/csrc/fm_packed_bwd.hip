@@ -11,10 +11,12 @@
 // over the rows (dk and dv, which share their scores).  No atomics: every output
 // row has one owner, equal calls give equal bits.
 //
-// Five products a pair of rows and keys (seven where the scores are made for dq, dk and
-// dv each) and, beside them, the weights and T: 16 sequences of up to 4096, 12 heads of
-// 64, bf16, 615 us, 440 TFLOP/s of the five; 5 of up to 4095, 32 heads to 8 of 128, 960 us,
-// 510; the prep kernel is 75 us of the first.  float32, D = 128: 86 of 153 TFLOP/s.
+// Seven products a pair of rows and keys (scores, dO.v and dq for the rows; scores, dO.v,
+// dk and dv for the keys), eight where dk and dv have workgroups of their own (3 + 3 + 2),
+// and, beside them, the weights and T, made as often as the scores; five products and one
+// making would do if all sums had one owner.  16 sequences of up to 4096, 12 heads of 64,
+// bf16, 615 us, 440 TFLOP/s of the five; 5 of up to 4095, 32 heads to 8 of 128, 960 us, 510;
+// the prep kernel is 75 us of the first.  float32, D = 128: 86 of 153 TFLOP/s.
 //
 // Powers of two (bf16 calls).  With dO_i = 2^a_i o_i, v_n = 2^b_n x_n and
 // delta_i = 2^a_i d_i:
@@ -24,7 +26,7 @@
 //          far:  T 2^-(M + F) = t (X_i 2^(b_n - F) o_i.x_n - Y_i),  X_i = m_i 2^(e_i - M),
 //          Y_i = X_i d_i 2^-F,  and w X_i for dv.
 // A wave that meets a larger one scales its sums down.  E is a row's own; M and F are a
-// key's own in the tiles that the mask cuts, then the wave's.
+// key's own in the tiles that the mask cuts, then the wave's.  A row of zeros has no e_i.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -7,7 +7,7 @@
 //
 // Few rows (single tokens).  HBM bounds it, D + 4 bytes a row: 4.8 TB/s at even
 // lengths, 61 sequences of up to 8192 tokens, 32 heads to 8 of 128, 100 us (3.8 TB/s,
-// the longest end alone).  A wave walks over key tiles of 16, two at a time, straight
+// the longest end alone), float32 102.  A wave walks over key tiles of 16, two at a time, straight
 // from the cache into registers, as fm_paged.hip.  Scores take the codes as they are:
 // q^ of a row becomes one 16-bit (float32: 24-bit) whole number per channel under a
 // scale of its row, cut in signed bytes, and int8 MFMA gives exact sums,
@@ -17,8 +17,8 @@
 // two bf16 parts (float32: three) against the codes, which bf16 holds exactly.
 //
 // Many rows (chunks).  The matrix pipe and the instructions beside it bound it: four
-// chunks of up to 2048 tokens over up to 8192, 32 heads to 8 of 128, 465 to 545 us, 650
-// TFLOP/s and more (cards differ).  There the few rows' scheme took 766: each wave converted every code for
+// chunks of up to 2048 tokens over up to 8192, 32 heads to 8 of 128, 456 to 545 us, 650
+// TFLOP/s and more (cards differ); float32, with twice the products, 855.  There the few rows' scheme took 766: each wave converted every code for
 // itself, and weights entered as two parts.  So codes become fp16 once a workgroup, on
 // their way into LDS, and one fp16 product (11 bits) does for weights and scores.
 #include <hip/hip_runtime.h>
